@@ -1,0 +1,573 @@
+"""Operators of a training step beyond the bf16 path: quantisation to 8-bit floating point, products of such operands,
+dropout whose mask is computed again instead of stored, and a gated linear recurrence over a sequence.
+
+Where `own` is false every operator is written out in elementary torch operations; where it is true the calls go to
+the library's entry points, as a training program makes them.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+_TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
+_F8 = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+_F8_TOP = {"e4m3": 8, "e5m2": 15}       # the largest value of either format is 1.75 * 2^top
+
+
+# ---- the cases ---------------------------------------------------------------------------------------------------
+
+def listed():
+    return [
+        # first feed-forward product of the measured 12-layer LM, all of its tokens
+        {"name": "gemm_8192x8192x2048", "family": "gemm", "m": 8192, "n": 8192, "k": 2048, "a": "e4m3", "b": "e4m3",
+         "epilogue": "bias", "out": "bf16"},
+        # the weight gradient that goes with it: contraction over the tokens, gradients in the wider-range format
+        {"name": "gemm_2048x8192x8192", "family": "gemm", "m": 2048, "n": 8192, "k": 8192, "a": "e4m3", "b": "e5m2",
+         "epilogue": "store", "out": "f32"},
+        # a projection into the residual stream at sizes that fit no tile
+        {"name": "gemm_1000x760x1040", "family": "gemm", "m": 1000, "n": 760, "k": 1040, "a": "e4m3", "b": "e4m3",
+         "epilogue": "residual", "out": "f32"},
+        # one token through the same first product: the weights are read once
+        {"name": "gemm_1x8192x2048", "family": "gemm", "m": 1, "n": 8192, "k": 2048, "a": "e4m3", "b": "e4m3",
+         "epilogue": "bias", "out": "bf16"},
+        # activations for the forward product and, transposed, for the weight gradient
+        {"name": "quant_8192x2048", "family": "quant", "rows": 8192, "cols": 2048, "dtype": "bf16", "format": "e4m3",
+         "block": 1, "both": True},
+        # master weights, once a step, for both directions
+        {"name": "quant_w_2048x8192", "family": "quant", "rows": 2048, "cols": 8192, "dtype": "f32", "format": "e4m3",
+         "block": 128, "both": True},
+        # gradients of a few odd rows
+        {"name": "quant_333x500", "family": "quant", "rows": 333, "cols": 500, "dtype": "bf16", "format": "e5m2",
+         "block": 1, "both": False},
+        # a branch of the measured LM into its residual stream, forward and backward
+        {"name": "dropout_8192x2048", "family": "dropout", "rows": 8192, "cols": 2048, "dtype": "bf16", "res": True, "p": 0.1},
+        # a small odd one in single precision
+        {"name": "dropout_37x1003", "family": "dropout", "rows": 37, "cols": 1003, "dtype": "f32", "res": False, "p": 0.3},
+        # sequence mixing in the place of the measured LM's attention, forward and backward
+        {"name": "scan_8x1024x2048", "family": "scan", "batch": 8, "steps": 1024, "width": 2048, "dtype": "bf16",
+         "ragged": False, "backward": True},
+        # one long sequence of few channels
+        {"name": "scan_1x16384x512", "family": "scan", "batch": 1, "steps": 16384, "width": 512, "dtype": "bf16",
+         "ragged": False, "backward": True},
+        # one token for each of eight sequences
+        {"name": "scan_8x1x2048", "family": "scan", "batch": 8, "steps": 1, "width": 2048, "dtype": "bf16", "ragged": False,
+         "backward": False},
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    family = rng.choice(["gemm", "gemm", "quant", "dropout", "scan", "scan"])
+    if family == "gemm":
+        m, n, k = _log(rng, 1, 8192), _log(rng, 64, 8192), max(16, _log(rng, 128, 8192) // 16 * 16)
+        while m * n * k > 8192 * 8192 * 2048:
+            m = m // 2 + 1
+        out = rng.choice(["bf16", "f32"])
+        epilogues = ["store", "bias", "gelu", "gelu_bwd"] if out == "bf16" else ["store", "bias", "residual", "add"]
+        return {"family": family, "m": m, "n": n, "k": k, "a": rng.choice(["e4m3", "e5m2"]), "b": rng.choice(["e4m3", "e5m2"]),
+                "epilogue": rng.choice(epilogues), "out": out}
+    dtype = rng.choice(["bf16", "bf16", "f32"])
+    if family == "quant":
+        rows = _log(rng, 1, 8192)
+        cols = _log(rng, 16, min(8192, (1 << 24) // rows))
+        return {"family": family, "rows": rows, "cols": cols, "dtype": dtype, "format": rng.choice(["e4m3", "e5m2"]),
+                "block": rng.choice([1, 1, 128]), "both": rng.random() < 0.6}
+    if family == "dropout":
+        rows = _log(rng, 1, 8192)
+        cols = _log(rng, 16, min(8192, (1 << 24) // rows))
+        return {"family": family, "rows": rows, "cols": cols, "dtype": dtype, "res": rng.random() < 0.6,
+                "p": round(rng.uniform(0.0, 0.9), 3)}
+    steps = _log(rng, 1, 16384)
+    width = _log(rng, 16, min(4096, (1 << 24) // steps))
+    return {"family": family, "batch": _log(rng, 1, max(1, min(16, (1 << 24) // (steps * width)))), "steps": steps, "width": width,
+            "dtype": dtype, "ragged": rng.random() < 0.4, "backward": rng.random() < 0.7}
+
+
+# ---- inputs ------------------------------------------------------------------------------------------------------
+
+class _Draw:
+    """Seeded values on the GPU; the order of the calls is part of the recipe."""
+
+    def __init__(self, seed):
+        self.g = torch.Generator(device="cuda")
+        self.g.manual_seed(int(seed) * 6271 + 29)
+
+    def normal(self, *shape, std=1.0, mean=0.0, dtype=torch.float32):
+        t = torch.randn(*shape, generator=self.g, device="cuda", dtype=torch.float32)
+        return t.mul_(std).add_(mean).to(dtype)
+
+    def uneven(self, rows, cols, dtype=torch.float32):
+        """Rows and column groups of different sizes, as activations and gradients have."""
+        r = torch.exp(self.normal(rows, 1)) * torch.exp(self.normal(1, cols, std=0.5))
+        return (self.normal(rows, cols) * r).to(dtype)
+
+    def integers(self, lo, hi, *shape, dtype=torch.int64):
+        return torch.randint(lo, hi, shape, generator=self.g, device="cuda", dtype=dtype)
+
+
+def _up(n, m):
+    return -(-n // m) * m
+
+
+def prepare(case, seed):
+    c, r, fam = dict(case), _Draw(seed), case["family"]
+    s = {"case": c}
+    if fam == "gemm":
+        m, n, k = c["m"], c["n"], c["k"]
+        # a weight (128 x 128 blocks) where both operands are e4m3, else activations and gradients (a scale for each row)
+        s["a"], s["a_scale"] = _quantised(r.uneven(m, k), c["a"], 1)
+        s["b"], s["b_scale"] = _quantised(r.uneven(n, k) * (0.02 if c["b"] == "e4m3" else 1e-3), c["b"],
+                                          128 if c["a"] == c["b"] == "e4m3" else 1)
+        ldc = _up(n, 8)                    # rows of outputs start on 16 bytes
+        if c["epilogue"] in ("bias", "residual", "gelu"):
+            s["bias"] = r.normal(n, std=0.5)
+        if c["epilogue"] == "residual":
+            s["aux"] = r.normal(m, ldc)
+        if c["epilogue"] == "gelu_bwd":
+            s["aux"] = r.normal(m, ldc, dtype=torch.bfloat16)
+        s["c"] = r.normal(m, ldc, dtype=_TORCH[c["out"]]) if c["epilogue"] == "add" else \
+            torch.zeros(m, ldc, dtype=_TORCH[c["out"]], device="cuda")
+        if c["epilogue"] == "add":
+            s["c0"] = s["c"].clone()       # a pass adds into what is there: every pass starts from this
+    elif fam == "quant":
+        s["x"] = r.uneven(c["rows"], c["cols"], dtype=_TORCH[c["dtype"]])
+        if c["block"] == 128:
+            s["x"].mul_(0.02)
+    elif fam == "dropout":
+        rows, cols, t = c["rows"], c["cols"], _TORCH[c["dtype"]]
+        s["x"], s["bias"] = r.normal(rows, cols, dtype=t), r.normal(cols, std=0.1)
+        if c["res"]:
+            s["res"] = r.normal(rows, cols)
+        s["dy"] = r.normal(rows, cols, std=1e-2, dtype=torch.float32 if c["res"] else t)
+        s["seed"], s["site"], s["step"] = (int(seed) * 0x9E3779B97F4A7C15 + 12345) % (1 << 64), 7, 1000 + int(seed) % 1000
+    else:
+        b, n, d, t = c["batch"], c["steps"], c["width"], _TORCH[c["dtype"]]
+        fx = r.normal(b * n, 2 * d, dtype=t)          # one projection gives gates and values side by side
+        fx[:, :d].add_(2.0)                           # gates of a model that remembers: a about 0.88
+        s["fx"], s["h0"] = fx, r.normal(b, d)
+        s["lens"] = r.integers(0, n + 1, b, dtype=torch.int32) if c["ragged"] else None
+        if c["backward"]:
+            s["dy"], s["dh_end"] = r.normal(b * n, d, std=1e-2, dtype=t), r.normal(b, d, std=1e-2)
+    return s
+
+
+# ---- the plain forms ---------------------------------------------------------------------------------------------
+
+def _two_to(e):
+    """2^e in 64 bits, put together from its bits: pow() and ldexp() are not exact on every device."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
+def _scale_index(rows, blocks, device):
+    """Where the scale of (row, block) is: groups of 64 rows, the four rows r, r + 16, r + 32, r + 48 side by side."""
+    r, b = torch.arange(rows, device=device)[:, None], torch.arange(blocks, device=device)[None, :]
+    return b * _up(rows, 64) + r // 64 * 64 + r % 16 * 4 + r % 64 // 16
+
+
+def _exponents(amax, fmt):
+    """Smallest e in [-127, 127] with amax <= 1.75 * 2^(top + e)."""
+    m, k = torch.frexp(amax.double())                 # amax = 2 m * 2^(k - 1)
+    e = k.long() - 1 - _F8_TOP[fmt] + (2 * m > 1.75).long()
+    return torch.where(amax == 0, torch.full_like(e, -127), e).clamp(-127, 127)
+
+
+def _blocked(x, fmt, block):
+    """(values of the format, exponents [rows, blocks]) of x in blocks of 128 columns."""
+    rows, cols = x.shape
+    nb = _up(cols, 128) // 128
+    xp = torch.zeros(_up(rows, block), nb * 128, dtype=torch.float32, device=x.device)
+    xp[:rows, :cols] = x
+    fin = torch.where(torch.isfinite(xp), xp.abs(), torch.zeros_like(xp))
+    amax = fin.view(-1, block, nb, 128).amax(dim=(1, 3))
+    e = _exponents(amax, fmt).repeat_interleave(block, 0)[:rows]
+    y = (xp[:rows].view(rows, nb, 128) * _two_to(-e)[:, :, None]).view(rows, -1).float()
+    return y.to(_F8[fmt])[:, :_up(cols, 16)].contiguous(), e
+
+
+def _table(e):
+    """Exponents [rows, blocks] as bytes, laid out as the product reads them; rows that do not exist have 0."""
+    rows, nb = e.shape
+    t = torch.zeros(_up(rows, 64) * nb, dtype=torch.uint8, device=e.device)
+    t[_scale_index(rows, nb, e.device).reshape(-1)] = (e + 127).to(torch.uint8).reshape(-1)
+    return t
+
+
+def _quantised(x, fmt, block):
+    q, e = _blocked(x, fmt, block)
+    return q, _table(e)
+
+
+def _plain_quant(s, c):
+    x = s["x"].float()
+    q, e = _blocked(x, c["format"], c["block"])
+    out = {"q": q, "scale": _table(e).view(torch.float8_e8m0fnu)}
+    if c["both"]:
+        if c["block"] == 128:             # the same blocks, seen from the other side
+            et = e[::128].T.repeat_interleave(128, 0)[:c["cols"]]
+            xt = torch.zeros(c["cols"], et.shape[1] * 128, device=x.device)
+            xt[:, :c["rows"]] = x.T
+            qt = (xt.view(c["cols"], -1, 128) * _two_to(-et)[:, :, None]).view(c["cols"], -1).float()
+            qt = qt.to(_F8[c["format"]])[:, :_up(c["rows"], 16)].contiguous()
+        else:
+            qt, et = _blocked(x.T, c["format"], 1)
+        out.update(qt=qt, scale_t=_table(et).view(torch.float8_e8m0fnu))
+    return out
+
+
+def _values(q, table):
+    rows, k = q.shape
+    nb = _up(k, 128) // 128
+    scale = _two_to(table[_scale_index(rows, nb, q.device)].long() - 127).float()
+    return q.float() * scale.repeat_interleave(128, 1)[:, :k]
+
+
+def _gelu_parts(u):
+    z = math.sqrt(2 / math.pi) * (u + 0.044715 * u * u * u)
+    return z, torch.tanh(z), math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * u * u)
+
+
+def _plain_gemm(s, c):
+    n, epi, t = c["n"], c["epilogue"], _TORCH[c["out"]]
+    v = _values(s["a"], s["a_scale"]) @ _values(s["b"], s["b_scale"]).T
+    if epi in ("bias", "residual", "gelu"):
+        v = v + s["bias"]
+    if epi == "residual":
+        v = v + s["aux"][:, :n]
+    elif epi == "gelu":
+        z, th, _ = _gelu_parts(v)
+        return {"u": v.to(t), "h": (0.5 * v * (1 + th)).to(t)}
+    elif epi == "gelu_bwd":
+        u = s["aux"][:, :n].float()
+        z, th, dz = _gelu_parts(u)
+        v = v * (0.5 * (1 + th) + 0.5 * u * (1 - th * th) * dz)
+    elif epi == "add":
+        v = v + s["c0"][:, :n]
+    return {"c": v.to(t)}
+
+
+def _mul_hi_lo(a, b):
+    p = a * b                              # wraps at 64 bits: the bits are right
+    return (p >> 32) & 0xFFFFFFFF, p & 0xFFFFFFFF
+
+
+def _keep_words(rows, cols, seed, site, step):
+    """The 16-bit word of every element: Philox4x32-10 of (column / 8, row, site, step) under the seed."""
+    c0 = torch.arange(_up(cols, 8) // 8, device="cuda")[None, :].expand(rows, -1).contiguous()
+    c1 = torch.arange(rows, device="cuda")[:, None].expand_as(c0).contiguous()
+    c2, c3 = torch.full_like(c0, site), torch.full_like(c0, step)
+    k0, k1 = seed & 0xFFFFFFFF, seed >> 32
+    for _ in range(10):
+        h0, l0 = _mul_hi_lo(c0, 0xD2511F53)
+        h1, l1 = _mul_hi_lo(c2, 0xCD9E8D57)
+        c0, c1, c2, c3 = h1 ^ c1 ^ k0, l1, h0 ^ c3 ^ k1, l0
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    w = torch.stack([c0, c1, c2, c3], -1)
+    return torch.stack([w & 0xFFFF, w >> 16], -1).view(rows, -1)[:, :cols]
+
+
+def _plain_dropout(s, c):
+    t = round(c["p"] * 65536)
+    keep = _keep_words(c["rows"], c["cols"], s["seed"], s["site"], s["step"]) >= t
+    scale = 65536 / (65536 - t) if t < 65536 else 0.0
+    zero = torch.zeros((), device="cuda")
+    y = torch.where(keep, (s["x"].float() + s["bias"]) * scale, zero)
+    if c["res"]:
+        y = y + s["res"]
+    dx = torch.where(keep, s["dy"].float() * scale, zero)
+    return {"y": y.to(s["dy"].dtype), "dx": dx.to(s["x"].dtype), "dbias": dx.double().sum(0).float()}
+
+
+def _scan(p, v):
+    """h_t = p_t h_(t-1) + v_t along dim 1 with h = 0 in front, by doubling."""
+    d, n = 1, v.shape[1]
+    while d < n:
+        v = torch.cat([v[:, :d], v[:, d:] + p[:, d:] * v[:, :-d]], 1)
+        p = torch.cat([p[:, :d], p[:, d:] * p[:, :-d]], 1)
+        d *= 2
+    return v
+
+
+def _plain_scan(s, c):
+    b, n, d, t = c["batch"], c["steps"], c["width"], _TORCH[c["dtype"]]
+    f, x = s["fx"][:, :d].float().view(b, n, d), s["fx"][:, d:].float().view(b, n, d)
+    a, z = torch.sigmoid(f), torch.sigmoid(-f)        # z = 1 - a without its cancellation
+    on = torch.ones(b, n, 1, dtype=torch.bool, device="cuda") if s["lens"] is None else \
+        (torch.arange(n, device="cuda")[None, :] < s["lens"][:, None])[:, :, None]
+    keep = torch.where(on, a, torch.ones_like(a))     # behind the end of a sequence the state stays
+    zero = torch.zeros((), device="cuda")
+    v = torch.where(on, z * x, zero)
+    v = torch.cat([v[:, :1] + keep[:, :1] * s["h0"][:, None], v[:, 1:]], 1)
+    h = _scan(keep, v)
+    out = {"y": torch.where(on, h, zero).to(t).view(b * n, d), "h_end": h[:, -1].clone()}
+    if c["backward"]:
+        dy = torch.where(on, s["dy"].float().view(b, n, d), zero)
+        dy = torch.cat([dy[:, :-1], dy[:, -1:] + s["dh_end"][:, None]], 1)
+        p = torch.cat([keep[:, 1:], torch.ones_like(keep[:, :1])], 1)
+        g = _scan(p.flip(1), dy.flip(1)).flip(1)
+        before = torch.cat([s["h0"][:, None], h[:, :-1]], 1)
+        out["df"] = torch.where(on, g * (before - x) * a * z, zero).to(t).view(b * n, d)
+        out["dx"] = torch.where(on, g * z, zero).to(t).view(b * n, d)
+        out["dh0"] = keep[:, 0] * g[:, 0]
+    return out
+
+
+# ---- the library's calls -----------------------------------------------------------------------------------------
+
+_context = _stream = None
+
+
+def _ctx():
+    """One context per program, as in any program that uses the library, on a stream of the program's."""
+    global _context, _stream
+    if _context is None:
+        from paper_2203_12533_amd import binding
+        _stream = torch.cuda.Stream()
+        _context = binding.Context(0, _stream.cuda_stream)
+    return _context
+
+
+def _buffers(s, c):
+    """What a program allocates once per size: outputs and workspaces."""
+    from paper_2203_12533_amd import binding as pwb
+    new = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device="cuda")  # noqa: E731
+    fam = c["family"]
+    dt = {"f32": pwb.PW_F32, "bf16": pwb.PW_BF16}
+    f8 = {"e4m3": pwb.PW_E4M3, "e5m2": pwb.PW_E5M2}
+    p = lambda x: x.data_ptr() if x is not None else None  # noqa: E731
+    if fam == "gemm":
+        epi = {"store": pwb.PW_EPI_STORE, "add": pwb.PW_EPI_STORE, "bias": pwb.PW_EPI_BIAS, "residual": pwb.PW_EPI_BIAS_RESIDUAL,
+               "gelu": pwb.PW_EPI_BIAS_GELU, "gelu_bwd": pwb.PW_EPI_GELU_BWD}[c["epilogue"]]
+        c2 = torch.empty_like(s["c"]) if c["epilogue"] == "gelu" else None
+        args = pwb.F8GemmArgs(a_format=f8[c["a"]], b_format=f8[c["b"]], M=c["m"], N=c["n"], K=c["k"], lda=s["a"].shape[1],
+                              ldb=s["b"].shape[1], ldc=s["c"].shape[1], epilogue=epi, out_dtype=dt[c["out"]],
+                              accumulate=int(c["epilogue"] == "add"), A=p(s["a"]), B=p(s["b"]), a_scale=p(s["a_scale"]),
+                              b_scale=p(s["b_scale"]), bias=p(s.get("bias")), aux=p(s.get("aux")), C=p(s["c"]), C2=p(c2))
+        return {"args": args, "c2": c2}
+    if fam == "quant":
+        rows, cols, t = c["rows"], c["cols"], _F8[c["format"]]
+        o = {"q": new(rows, _up(cols, 16), dtype=t), "scale": new(pwb.f8_scale_bytes(rows, cols), dtype=torch.uint8)}
+        if c["both"]:
+            o.update(qt=new(cols, _up(rows, 16), dtype=t), scale_t=new(pwb.f8_scale_bytes(cols, rows), dtype=torch.uint8))
+        o["args"] = pwb.F8QuantizeArgs(dtype=dt[c["dtype"]], format=f8[c["format"]], block_rows=c["block"], x=p(s["x"]), rows=rows,
+                                       cols=cols, ldx=cols, q=p(o["q"]), ldq=_up(cols, 16), q_scale=p(o["scale"]),
+                                       qt=p(o.get("qt")), ldqt=_up(rows, 16), qt_scale=p(o.get("scale_t")))
+        return o
+    if fam == "dropout":
+        rows, cols = c["rows"], c["cols"]
+        return {"y": torch.empty_like(s["dy"]), "dx": torch.empty_like(s["x"]), "dbias": new(cols),
+                "ws": new(pwb.dropout_bwd_ws_floats(rows, cols)),
+                "args": pwb.DropoutArgs(dtype=dt[c["dtype"]], out_dtype=pwb.PW_F32 if c["res"] else dt[c["dtype"]], rows=rows, cols=cols,
+                                        ldx=cols, ldy=cols, p=c["p"], seed=s["seed"], site=s["site"], step=s["step"])}
+    b, n, d, t = c["batch"], c["steps"], c["width"], _TORCH[c["dtype"]]
+    es = s["fx"].element_size()
+    o = {"y": new(b * n, d, dtype=t), "h_end": new(b, d), "ws": new(max(1, pwb.scan_ws_floats(b, n, d))),
+         "args": pwb.ScanArgs(dtype=dt[c["dtype"]], f=p(s["fx"]), x=p(s["fx"]) + d * es, ldf=2 * d, ldx=2 * d, B=b, T=n, D=d,
+                              h0=p(s["h0"]), lens=p(s["lens"]))}
+    if c["backward"]:
+        o.update(states=new(pwb.scan_state_floats(b, n, d)), dfx=new(b * n, 2 * d, dtype=t), dh0=new(b, d))
+    return o
+
+
+def _own_run(s, c):
+    if "own" not in s:
+        s["own"] = _buffers(s, c)
+    o, ctx, fam = s["own"], _ctx(), c["family"]
+    p = lambda x: x.data_ptr() if x is not None else None  # noqa: E731
+    if fam == "gemm":
+        if c["epilogue"] == "add":
+            with torch.cuda.stream(_stream):
+                s["c"].copy_(s["c0"])
+        ctx.f8_gemm(o["args"])
+        out = s["c"][:, :c["n"]]
+        return {"u": out, "h": o["c2"][:, :c["n"]]} if c["epilogue"] == "gelu" else {"c": out}
+    if fam == "quant":
+        ctx.f8_quantize(o["args"])
+        out = {"q": o["q"], "scale": o["scale"].view(torch.float8_e8m0fnu)}
+        if c["both"]:
+            out.update(qt=o["qt"], scale_t=o["scale_t"].view(torch.float8_e8m0fnu))
+        return out
+    if fam == "dropout":
+        ctx.dropout_fwd(o["args"], p(s["x"]), p(s["bias"]), p(s.get("res")), p(o["y"]))
+        ctx.dropout_bwd(o["args"], p(s["dy"]), p(o["dx"]), p(o["dbias"]), p(o["ws"]))
+        return {k: o[k] for k in ("y", "dx", "dbias")}
+    d, es = c["width"], s["fx"].element_size()
+    ctx.scan_fwd(o["args"], p(o["y"]), d, p(o["h_end"]), p(o.get("states")), p(o["ws"]))
+    out = {k: o[k] for k in ("y", "h_end")}
+    if c["backward"]:
+        ctx.scan_bwd(o["args"], p(s["dy"]), d, p(s["dh_end"]), p(o["states"]), p(o["dfx"]), 2 * d, p(o["dfx"]) + d * es, 2 * d,
+                     p(o["dh0"]), p(o["ws"]))
+        out.update(df=o["dfx"][:, :d], dx=o["dfx"][:, d:], dh0=o["dh0"])
+    return out
+
+
+_PLAIN = {"gemm": _plain_gemm, "quant": _plain_quant, "dropout": _plain_dropout, "scan": _plain_scan}
+
+
+def run(state):
+    c = state["case"]
+    if own:
+        return _own_run(state, c)
+    return _PLAIN[c["family"]](state, c)
+
+
+# ---- the definitions in 64 bits ----------------------------------------------------------------------------------
+
+def _decode(fmt):
+    """The value of each of the 256 bytes."""
+    mant, bias = (3, 7) if fmt == "e4m3" else (2, 15)
+    v = []
+    for i in range(256):
+        e, f = (i & 127) >> mant, i & ((1 << mant) - 1)
+        x = math.ldexp(f, 1 - bias - mant) if e == 0 else math.ldexp((1 << mant) + f, e - bias - mant)
+        if fmt == "e4m3" and i & 127 == 127:
+            x = math.nan
+        if fmt == "e5m2" and e == 31:
+            x = math.nan if f else math.inf
+        v.append(-x if i & 128 else x)
+    return torch.tensor(v, dtype=torch.float64, device="cuda")
+
+
+_POWERS = [math.ldexp(1.0, i - 300) for i in range(601)]
+
+
+def _power(e):
+    return torch.tensor(_POWERS, dtype=torch.float64, device="cuda")[e.long() + 300]
+
+
+def _exact_operand(q, table, fmt):
+    rows, k = q.shape
+    v = _decode(fmt)[q.view(torch.uint8).long()]
+    t = table.view(-1, _up(rows, 64) // 64, 16, 4).permute(1, 3, 2, 0).reshape(-1, table.numel() // _up(rows, 64))[:rows]
+    for b in range(t.shape[1]):
+        v[:, 128 * b:128 * b + 128] *= _power(t[:, b:b + 1].long() - 127)
+    return v
+
+
+def _exact_gemm(s, c):
+    v = torch.matmul(_exact_operand(s["a"], s["a_scale"], c["a"]), _exact_operand(s["b"], s["b_scale"], c["b"]).T.contiguous())
+    epi, n = c["epilogue"], c["n"]
+    gelu = lambda u: u / (1 + torch.exp(-2 * math.sqrt(2 / math.pi) * (u + 0.044715 * u ** 3)))  # noqa: E731
+    if epi == "bias":
+        v += s["bias"].double()
+    elif epi == "residual":
+        v += s["bias"].double() + s["aux"][:, :n].double()
+    elif epi == "add":
+        v += s["c0"][:, :n].double()
+    elif epi == "gelu":
+        v += s["bias"].double()
+        return {"u": v, "h": gelu(v)}
+    elif epi == "gelu_bwd":
+        u = s["aux"][:, :n].double()
+        k = 2 * math.sqrt(2 / math.pi)
+        e = 1 / (1 + torch.exp(-k * (u + 0.044715 * u ** 3)))
+        v *= e + u * e * (1 - e) * k * (1 + 0.134145 * u ** 2)
+    return {"c": v}
+
+
+def _exact_rows(x, fmt, block):
+    """Nearest values of the format, by looking among all of them."""
+    rows, cols = x.shape
+    top = 448.0 if fmt == "e4m3" else 57344.0
+    v = _decode(fmt)
+    grid = torch.unique(v[torch.isfinite(v) & (v >= 0)])
+    even = torch.arange(grid.numel(), device="cuda") % 2 == 0      # codes count up: ties go to the even one
+    q, sc = torch.zeros(rows, _up(cols, 16), dtype=torch.float64, device="cuda"), []
+    for j in range(0, cols, 128):
+        part = x[:, j:j + 128]
+        peak = part.abs().amax(1)
+        peak = torch.cat([peak[i:i + block].amax().expand(min(block, rows - i)) for i in range(0, rows, block)]) if block > 1 else peak
+        e = torch.ceil(torch.log2(peak / top)).clamp(-127, 127)
+        e = torch.where(peak <= top * _power(e - 1), e - 1, torch.where(peak > top * _power(e), e + 1, e)).clamp(-127, 127)
+        y = part / _power(e)[:, None]
+        at = torch.searchsorted(grid, y.abs().contiguous()).clamp(1, grid.numel() - 1)
+        lo, hi = y.abs() - grid[at - 1], grid[at] - y.abs()
+        near = torch.where((lo < hi) | ((lo == hi) & even[at - 1]), grid[at - 1], grid[at])
+        q[:, j:j + 128][:, :part.shape[1]] = torch.copysign(near, y)
+        sc.append(torch.cat([_power(e), torch.full((_up(rows, 64) - rows,), 2.0 ** -127, dtype=torch.float64, device="cuda")])
+                  .view(-1, 4, 16).transpose(1, 2).reshape(-1))
+    return q, torch.cat(sc)
+
+
+def _exact_quant(s, c):
+    x = s["x"].double()
+    q, sc = _exact_rows(x, c["format"], c["block"])
+    out = {"q": q, "scale": sc}
+    if c["both"]:
+        out["qt"], out["scale_t"] = _exact_rows(x.T.contiguous(), c["format"], c["block"])
+    return out
+
+
+def _exact_dropout(s, c):
+    rows, cols = c["rows"], c["cols"]
+    u32, u64 = np.uint32, np.uint64
+    groups = -(-cols // 8)
+    ctr = [np.tile(np.arange(groups, dtype=u32), rows), np.repeat(np.arange(rows, dtype=u32), groups),
+           np.full(rows * groups, s["site"], u32), np.full(rows * groups, s["step"], u32)]
+    key = [s["seed"] % (1 << 32), s["seed"] >> 32]
+    for i in range(10):
+        k = [(key[0] + i * 0x9E3779B9) % (1 << 32), (key[1] + i * 0xBB67AE85) % (1 << 32)]
+        p0, p1 = ctr[0].astype(u64) * u64(0xD2511F53), ctr[2].astype(u64) * u64(0xCD9E8D57)
+        ctr = [(p1 >> u64(32)).astype(u32) ^ ctr[1] ^ u32(k[0]), p1.astype(u32), (p0 >> u64(32)).astype(u32) ^ ctr[3] ^ u32(k[1]), p0.astype(u32)]
+    words = np.stack(ctr, 1).view(np.uint16).reshape(rows, -1)[:, :cols]
+    t = round(c["p"] * 65536)
+    m = torch.from_numpy((words >= t).astype(np.float64)).cuda() * (65536 / (65536 - t))
+    y = (s["x"].double() + s["bias"].double()) * m
+    dx = s["dy"].double() * m
+    return {"y": y + s["res"].double() if c["res"] else y, "dx": dx, "dbias": dx.sum(0)}
+
+
+def _exact_scan(s, c):
+    b, n, d = c["batch"], c["steps"], c["width"]
+    f, x = (s["fx"][:, k * d:k * d + d].double().view(b, n, d) for k in (0, 1))
+    lens = torch.full((b,), n, device="cuda") if s["lens"] is None else s["lens"].long()
+    a, z = 1 / (1 + torch.exp(-f)), 1 / (1 + torch.exp(f))
+    on = (torch.arange(n, device="cuda")[None] < lens[:, None])[:, :, None].double()
+    h, hs = s["h0"].double(), []
+    for t in range(n):
+        hs.append(h)                                   # the state in front of step t
+        h = torch.where(on[:, t] > 0, a[:, t] * h + z[:, t] * x[:, t], h)
+    out = {"y": (torch.stack(hs[1:] + [h], 1) * on).reshape(b * n, d), "h_end": h}
+    if c["backward"]:
+        dy = s["dy"].double().view(b, n, d)
+        gs, back = [], s["dh_end"].double()            # gradient of the state behind step t
+        for t in reversed(range(n)):
+            g = torch.where(on[:, t] > 0, dy[:, t] + back, back)
+            gs.append(g)
+            back = torch.where(on[:, t] > 0, a[:, t] * g, g)
+        g = torch.stack(gs[::-1], 1) * on
+        out.update(df=(g * (torch.stack(hs, 1) - x) * a * z).reshape(b * n, d), dx=(g * z).reshape(b * n, d), dh0=back)
+    return out
+
+
+_EXACT = {"gemm": _exact_gemm, "quant": _exact_quant, "dropout": _exact_dropout, "scan": _exact_scan}
+
+
+def exact(case, seed):
+    return _EXACT[case["family"]](prepare(case, seed), case)
+
+
+# ---- what a pass cannot do without -------------------------------------------------------------------------------
+
+def work(case):
+    c, fam = case, case["family"]
+    if fam == "gemm":
+        m, n, k = c["m"], c["n"], c["k"]
+        es = 2 if c["out"] == "bf16" else 4
+        out = m * n * es * (2 if c["epilogue"] == "gelu" else 1)
+        extra = m * n * {"residual": 4, "add": 4, "gelu_bwd": 2}.get(c["epilogue"], 0)
+        return {"bytes": float((m + n) * k * (1 + 1 / 128) + out + extra + 4 * n), "flops": 2.0 * m * n * k}
+    es = 2 if c["dtype"] == "bf16" else 4
+    if fam == "quant":
+        n = c["rows"] * c["cols"]
+        return {"bytes": float(n * (es + (2 if c["both"] else 1) * (1 + 1 / 128))), "flops": 4.0 * n}
+    if fam == "dropout":
+        n, ey = c["rows"] * c["cols"], 4 if c["res"] else es
+        return {"bytes": float(n * (es + (4 if c["res"] else 0) + ey + ey + es) + 8 * c["cols"]), "flops": 8.0 * n}
+    n, states = c["batch"] * c["steps"] * c["width"], c["batch"] * c["width"]
+    return {"bytes": float(n * es * (8 if c["backward"] else 3) + 8 * states + (8 * states if c["backward"] else 0)),
+            "flops": float(n * (30 if c["backward"] else 10))}
