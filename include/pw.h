@@ -531,6 +531,120 @@ pw_status pw_op_sgd(pw_ctx* ctx, float* w, const float* g, int64_t n, float lr);
 pw_status pw_op_adam(pw_ctx* ctx, float* w, float* m, float* v, const float* g, void* w_bf16, int64_t n,
                      float lr, float beta1, float beta2, float eps, int t);
 
+/* ---- operands in 8-bit floating point -------------------------------------------------------------
+ * Values are e4m3 (4 exponent bits, largest 448, NaN, no infinity) or e5m2 (largest 57344, infinities and NaN), with a scale
+ * 2^e for each block of 128 elements along the contraction, stored as the byte e + 127.  An operand of `rows` rows of `cols`
+ * elements is an array of bytes [rows][ld] and a scale table of pw_f8_scale_bytes(rows, cols) bytes: block b (columns 128 b ..
+ * 128 b + 127) of row r has its byte at
+ *     b * R + (r / 64) * 64 + (r % 16) * 4 + (r % 64) / 16,   R = rows rounded up to a multiple of 64.
+ * Bytes of rows that do not exist are written as 0 and matter nowhere; the byte 255 (no number) makes its block NaN. */
+typedef enum { PW_E4M3 = 0, PW_E5M2 = 1 } pw_f8_format;
+/* 64 ceil(rows / 64) ceil(cols / 128); -1 if either is negative or over 2^30. */
+int64_t pw_f8_scale_bytes(int64_t rows, int64_t cols);
+
+/* x [rows][ldx] in `dtype` to either or both of
+ *   q  [rows][ldq]:  x,            blocks along the columns of x, scale table of (rows, cols);
+ *   qt [cols][ldqt]: x transposed, blocks along the rows of x,    scale table of (cols, rows)
+ * (a null pointer leaves one out; then its scale pointer and stride are not looked at).  block_rows = 1: each row of q (each
+ * row of qt) has scales of its own, as activations and gradients want them: q for the forward and data-gradient product, qt for
+ * the weight gradient, which contracts over the rows.  block_rows = 128: one scale for 128 x 128 elements of x, the same in
+ * both outputs, as weights want it.  e is the smallest integer in [-127, 127] for which no finite element of the block
+ * exceeds the format's largest value times 2^e (-127 for a block of zeros); elements are rounded to nearest, ties to even.
+ * NaN stays NaN; infinities become NaN in e4m3 and stay infinities in e5m2; neither touches the scale of its block.
+ * q, qt: 16-byte aligned, ldq >= cols and ldqt >= rows, both multiples of 16; rows are filled with zeros up to the next multiple
+ * of 16 elements, so that this length can be the K of a product; bytes behind that are left as they were. */
+typedef struct {
+  int32_t dtype;             /* of x: PW_F32 or PW_BF16 */
+  int32_t format;            /* pw_f8_format */
+  int32_t block_rows;        /* 1 or 128 */
+  const void* x;
+  int64_t rows, cols, ldx;   /* rows at most 128 * 65535, columns at most 2^30 */
+  void* q;
+  int64_t ldq;
+  uint8_t* q_scale;
+  void* qt;
+  int64_t ldqt;
+  uint8_t* qt_scale;
+} pw_f8_quantize_args;
+pw_status pw_op_f8_quantize(pw_ctx* ctx, const pw_f8_quantize_args* args);
+
+/* C[M, N] = A[M, K] . B[N, K]^T of two such operands (both contiguous along K), fp32 accumulation, and the epilogues
+ * PW_EPI_STORE .. PW_EPI_GELU_BWD of pw_op_gemm with the same meaning (aux of PW_EPI_GELU_BWD is bf16; a residual and an
+ * accumulating store need out_dtype PW_F32).  K, lda, ldb multiples of 16, ldc a multiple of 8, A, B, C, C2, aux, bias 16-byte
+ * and the scale tables 4-byte aligned.  The table of an operand is the one of (rows, K).  With y = x W of the LM's layers, W
+ * [in][out]: forward A = q(x), B = qt(W); data gradient A = q(dy), B = q(W); weight gradient dW = A = qt(x), B = qt(dy), K = the
+ * rows of x rounded up to 16.  bf16 outputs come from the 8-bit matrix pipe, which drops what lies 2^-13 under the largest of eight
+ * neighbouring products (1e-5 to 3e-5 of the result, in the norm); fp32 outputs come from the bf16 pipe, at half its rate, with
+ * exact products (of values within 2^-126 .. 2^127).  Outputs may overlap aux of PW_EPI_BIAS_RESIDUAL (the same array) and nothing else. */
+typedef struct {
+  int32_t a_format, b_format;   /* pw_f8_format */
+  int64_t M, N, K, lda, ldb, ldc;
+  int32_t epilogue;             /* pw_epilogue */
+  int32_t out_dtype;            /* PW_F32 or PW_BF16: type of C and C2 */
+  int32_t accumulate;           /* 1: C += result (fp32 output, PW_EPI_STORE only) */
+  const void* A;
+  const void* B;
+  const uint8_t* a_scale;
+  const uint8_t* b_scale;
+  const float* bias;            /* [N] or null */
+  const void* aux;              /* [M, ldc] or null */
+  void* C;
+  void* C2;
+} pw_f8_gemm_args;
+pw_status pw_op_f8_gemm(pw_ctx* ctx, const pw_f8_gemm_args* args);
+
+/* ---- dropout ---------------------------------------------------------------------------------------
+ * The mask is a function of its position and is stored nowhere: element (r, c) is kept where 16 bits of Philox4x32-10 with key
+ * `seed` (low word first) and counter (c / 8, r, site, step + *step_dev) are at least round(65536 p) - half-word c % 8 of the four
+ * output words, low halves first.  So p is taken to the nearest 2^-16 (halves to even; 0 keeps everything, 1 drops
+ * everything), kept elements are scaled by exactly 1 / (1 - p) of that value, and neither strides nor types change a mask.
+ * site: which dropout of the model; step: which step; step_dev (device, optional) is added to step when the kernel runs, so
+ * that a captured graph draws anew on every replay if the program advances it.  The backward call takes the same arguments. */
+typedef struct {
+  int32_t dtype;             /* of x and dx: PW_F32 or PW_BF16 */
+  int32_t out_dtype;         /* of y and dy: PW_F32, or PW_BF16 where dtype is */
+  int64_t rows, cols;        /* rows at most 2^31, columns at most 2^24 */
+  int64_t ldx, ldy;          /* rows of x, dx / of y, dy, res are this many elements apart */
+  float p;                   /* 0 .. 1 */
+  uint64_t seed;
+  uint32_t site, step;
+  const uint32_t* step_dev;
+} pw_dropout_args;
+/* y = res + keep (x + bias) / (1 - p).  bias: fp32 [cols] or null; res: fp32 [rows][ldy] or null, with out_dtype PW_F32 only.
+ * y may be the same array as res, or as x where type and stride are the same. */
+pw_status pw_op_dropout_fwd(pw_ctx* ctx, const pw_dropout_args* args, const void* x, const float* bias, const float* res, void* y);
+/* dx = keep dy / (1 - p) (the residual's gradient is dy itself); dbias: null, or fp32 [cols] that receives the column sums of
+ * dx before its rounding (overwritten, or added into when accumulate = 1).  ws: fp32 workspace of
+ * pw_dropout_bwd_ws_floats(rows, cols) floats if dbias is wanted, else null.  dx may be the same array as dy where type and
+ * stride are the same. */
+pw_status pw_op_dropout_bwd(pw_ctx* ctx, const pw_dropout_args* args, const void* dy, void* dx, float* dbias, float* ws, int accumulate);
+int64_t pw_dropout_bwd_ws_floats(int64_t rows, int64_t cols);   /* -1 for impossible sizes */
+
+/* ---- gated linear recurrence -----------------------------------------------------------------------
+ * h_t = a_t h_(t-1) + (1 - a_t) x_t with a_t = sigmoid(f_t), element by element over D channels, y_t = h_t, from h_0: it mixes
+ * positions as attention does, in time linear in their number and with a state of one row.  Sequence b has its steps in rows
+ * b T .. b T + T - 1 of f, x (and y, dy, df, dx); f and x may be columns of one array ([F|X] of one projection).  T = 1 with h0
+ * and h_end (they may be one array) is a decoding step.  State and sums are fp32. */
+typedef struct {
+  int32_t dtype;             /* of f, x, y, dy, df, dx: PW_F32 or PW_BF16 */
+  const void* f;
+  const void* x;
+  int64_t ldf, ldx;
+  int32_t B, T, D;           /* B at most 65535, T at most 2^30, D at most 2^24 */
+  const float* h0;           /* [B, D], or null: zeros */
+  const int32_t* lens;       /* device, [B], or null: T everywhere.  Sequence b has lens[b] steps (clamped to 0 .. T); behind
+                                them y, df and dx are zero, the state stays, and what f, x and dy hold does not matter */
+} pw_scan_args;
+/* y rows ldy apart; h_end: fp32 [B, D] state behind the last step, or null; states: pw_scan_state_floats(B, T, D) floats that the
+ * backward call needs, or null; ws: workspace of pw_scan_ws_floats(B, T, D) floats (8-byte aligned; may be null where that is 0). */
+pw_status pw_op_scan_fwd(pw_ctx* ctx, const pw_scan_args* args, void* y, int64_t ldy, float* h_end, float* states, float* ws);
+/* Gradients from dy (rows lddy apart) and dh_end (fp32 [B, D], or null: zeros): df, dx rows lddf, lddx apart (they may be
+ * columns of one array), dh0 fp32 [B, D] or null (may be the same array as dh_end).  args and states as in the forward call. */
+pw_status pw_op_scan_bwd(pw_ctx* ctx, const pw_scan_args* args, const void* dy, int64_t lddy, const float* dh_end,
+                         const float* states, void* df, int64_t lddf, void* dx, int64_t lddx, float* dh0, float* ws);
+int64_t pw_scan_state_floats(int64_t B, int64_t T, int64_t D);   /* -1 for impossible sizes */
+int64_t pw_scan_ws_floats(int64_t B, int64_t T, int64_t D);
+
 /* ---- measurement aid ----------------------------------------------------------------------------
  * Between pw_profile_begin and pw_profile_end every MFMA GEMM launched on the executor stream (by a train
  * step or by pw_op_gemm) is bracketed by a pair of timing HIP events on that stream.  pw_profile_end

@@ -28,6 +28,7 @@ PW_STREAM, PW_GRAPH, PW_SEQUENTIAL = 0, 1, 2
 PW_PARAMS, PW_GRADS, PW_ADAM_M, PW_ADAM_V = 0, 1, 2, 3
 PW_EPI_STORE, PW_EPI_BIAS, PW_EPI_BIAS_RESIDUAL, PW_EPI_BIAS_GELU, PW_EPI_GELU_BWD, PW_EPI_ADAM, PW_EPI_XENT_STATS, \
     PW_EPI_XENT_GRAD = range(8)
+PW_E4M3, PW_E5M2 = 0, 1
 
 
 class TensorSpec(C.Structure):
@@ -88,6 +89,31 @@ class MhaArgs(C.Structure):
                 ("ldq", C.c_int64), ("ldkv", C.c_int64),
                 ("B", C.c_int32), ("Tq", C.c_int32), ("Tk", C.c_int32), ("H", C.c_int32), ("hd", C.c_int32),
                 ("causal", C.c_int32)]
+
+
+class F8QuantizeArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("format", C.c_int32), ("block_rows", C.c_int32), ("x", C.c_void_p),
+                ("rows", C.c_int64), ("cols", C.c_int64), ("ldx", C.c_int64),
+                ("q", C.c_void_p), ("ldq", C.c_int64), ("q_scale", C.c_void_p),
+                ("qt", C.c_void_p), ("ldqt", C.c_int64), ("qt_scale", C.c_void_p)]
+
+
+class F8GemmArgs(C.Structure):
+    _fields_ = [("a_format", C.c_int32), ("b_format", C.c_int32)] + \
+               [(n, C.c_int64) for n in ("M", "N", "K", "lda", "ldb", "ldc")] + \
+               [(n, C.c_int32) for n in ("epilogue", "out_dtype", "accumulate")] + \
+               [(n, C.c_void_p) for n in ("A", "B", "a_scale", "b_scale", "bias", "aux", "C", "C2")]
+
+
+class DropoutArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("out_dtype", C.c_int32)] + \
+               [(n, C.c_int64) for n in ("rows", "cols", "ldx", "ldy")] + \
+               [("p", C.c_float), ("seed", C.c_uint64), ("site", C.c_uint32), ("step", C.c_uint32), ("step_dev", C.c_void_p)]
+
+
+class ScanArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("f", C.c_void_p), ("x", C.c_void_p), ("ldf", C.c_int64), ("ldx", C.c_int64),
+                ("B", C.c_int32), ("T", C.c_int32), ("D", C.c_int32), ("h0", C.c_void_p), ("lens", C.c_void_p)]
 
 
 class PwError(RuntimeError):
@@ -184,6 +210,17 @@ _SIGS = {
     "pw_op_xent_from_stats": (C.c_int, [C.c_void_p] * 6 + [C.c_int] * 2),
     "pw_op_colsum": (C.c_int, [C.c_void_p, C.c_int] + [C.c_void_p] * 3 + [C.c_int64] * 2 + [C.c_int]),
     "pw_colsum_ws_floats": (C.c_int64, [C.c_int64, C.c_int64]),
+    "pw_f8_scale_bytes": (C.c_int64, [C.c_int64] * 2),
+    "pw_op_f8_quantize": (C.c_int, [C.c_void_p, C.POINTER(F8QuantizeArgs)]),
+    "pw_op_f8_gemm": (C.c_int, [C.c_void_p, C.POINTER(F8GemmArgs)]),
+    "pw_op_dropout_fwd": (C.c_int, [C.c_void_p, C.POINTER(DropoutArgs)] + [C.c_void_p] * 4),
+    "pw_op_dropout_bwd": (C.c_int, [C.c_void_p, C.POINTER(DropoutArgs)] + [C.c_void_p] * 4 + [C.c_int]),
+    "pw_dropout_bwd_ws_floats": (C.c_int64, [C.c_int64] * 2),
+    "pw_op_scan_fwd": (C.c_int, [C.c_void_p, C.POINTER(ScanArgs), C.c_void_p, C.c_int64] + [C.c_void_p] * 3),
+    "pw_op_scan_bwd": (C.c_int, [C.c_void_p, C.POINTER(ScanArgs), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                 C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "pw_scan_state_floats": (C.c_int64, [C.c_int64] * 3),
+    "pw_scan_ws_floats": (C.c_int64, [C.c_int64] * 3),
     "pw_op_sgd": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_float]),
     "pw_op_adam": (C.c_int, [C.c_void_p] + [C.c_void_p] * 5 + [C.c_int64] + [C.c_float] * 4 + [C.c_int]),
 }
@@ -434,6 +471,25 @@ class Context:
                 lddkv: int, o_lo: int = 0):
         self._check(lib().pw_op_mha_bwd(self._h, C.byref(args), o, o_lo or None, dout, lse, delta, dq, lddq, dk, dv, lddkv))
 
+    def f8_quantize(self, args: "F8QuantizeArgs"):
+        self._check(lib().pw_op_f8_quantize(self._h, C.byref(args)))
+
+    def f8_gemm(self, args: "F8GemmArgs"):
+        self._check(lib().pw_op_f8_gemm(self._h, C.byref(args)))
+
+    def dropout_fwd(self, args: "DropoutArgs", x: int, bias: int | None, res: int | None, y: int):
+        self._check(lib().pw_op_dropout_fwd(self._h, C.byref(args), x, bias, res, y))
+
+    def dropout_bwd(self, args: "DropoutArgs", dy: int, dx: int, dbias: int | None = None, ws: int | None = None, accumulate: int = 0):
+        self._check(lib().pw_op_dropout_bwd(self._h, C.byref(args), dy, dx, dbias, ws, accumulate))
+
+    def scan_fwd(self, args: "ScanArgs", y: int, ldy: int, h_end: int | None, states: int | None, ws: int | None):
+        self._check(lib().pw_op_scan_fwd(self._h, C.byref(args), y, ldy, h_end, states, ws))
+
+    def scan_bwd(self, args: "ScanArgs", dy: int, lddy: int, dh_end: int | None, states: int, df: int, lddf: int, dx: int, lddx: int,
+                 dh0: int | None, ws: int | None):
+        self._check(lib().pw_op_scan_bwd(self._h, C.byref(args), dy, lddy, dh_end, states, df, lddf, dx, lddx, dh0, ws))
+
     def gemm_group(self, kws: list):
         arr = (GemmArgs * len(kws))()
         keep = []
@@ -444,6 +500,22 @@ class Context:
     def gemm_pair(self, kw0: dict, kw1: dict):
         a0, a1 = _gemm_args(kw0), _gemm_args(kw1)
         self._check(lib().pw_op_gemm_pair(self._h, C.byref(a0), C.byref(a1)))
+
+
+def f8_scale_bytes(rows: int, cols: int) -> int:
+    return lib().pw_f8_scale_bytes(rows, cols)
+
+
+def dropout_bwd_ws_floats(rows: int, cols: int) -> int:
+    return lib().pw_dropout_bwd_ws_floats(rows, cols)
+
+
+def scan_state_floats(B: int, T: int, D: int) -> int:
+    return lib().pw_scan_state_floats(B, T, D)
+
+
+def scan_ws_floats(B: int, T: int, D: int) -> int:
+    return lib().pw_scan_ws_floats(B, T, D)
 
 
 def _gemm_args(kw: dict, a: "GemmArgs | None" = None) -> "GemmArgs":

@@ -124,6 +124,67 @@ hipError_t launch_embedding_bwd(hipStream_t s, const int32_t* tokens, const floa
 hipError_t launch_softmax_xent(hipStream_t s, int dtype, void* z, const int32_t* tokens, float* loss, float* row_loss,
                                int B, int T, int V);
 
+// out[c] (=|+=) sum over p < parts of ws[p * stride + c], in a fixed order (norm.hip).
+hipError_t launch_reduce_parts(hipStream_t s, const float* ws, float* out, int parts, int64_t stride, int64_t cols, int accumulate);
+
+// f8_quantize.hip, gemm_f8.hip: operands in 8-bit floating point; see pw.h for the layouts.
+enum F8Format { kE4M3 = 0, kE5M2 = 1 };
+struct F8QuantizeArgs {
+  int dtype, format, block_rows;
+  const void* x;
+  int64_t rows, cols, ldx;
+  void* q;
+  int64_t ldq;
+  uint8_t* q_scale;
+  void* qt;
+  int64_t ldqt;
+  uint8_t* qt_scale;
+};
+int64_t f8_scale_bytes(int64_t rows, int64_t cols);
+hipError_t launch_f8_quantize(hipStream_t s, const F8QuantizeArgs& a);
+struct GemmF8Args {
+  int a_format, b_format;
+  int64_t M, N, K, lda, ldb, ldc;
+  int epilogue, out_dtype, accumulate;
+  const void* A;
+  const void* B;
+  const uint8_t* a_scale;
+  const uint8_t* b_scale;
+  const float* bias;
+  const void* aux;
+  void* C;
+  void* C2;
+};
+hipError_t launch_gemm_f8(hipStream_t s, const GemmF8Args& a);
+
+// dropout.hip
+struct DropoutArgs {
+  int dtype, out_dtype;
+  int64_t rows, cols, ldx, ldy;
+  float p;
+  uint64_t seed;
+  uint32_t site, step;
+  const uint32_t* step_dev;
+};
+int64_t dropout_bwd_ws_floats(int64_t rows, int64_t cols);
+hipError_t launch_dropout_fwd(hipStream_t s, const DropoutArgs& a, const void* x, const float* bias, const float* res, void* y);
+hipError_t launch_dropout_bwd(hipStream_t s, const DropoutArgs& a, const void* dy, void* dx, float* dbias, float* ws, int accumulate);
+
+// scan.hip
+struct ScanArgs {
+  int dtype;
+  const void *f, *x;
+  int64_t ldf, ldx;
+  int B, T, D;
+  const float* h0;
+  const int32_t* lens;
+};
+int64_t scan_state_floats(int64_t B, int64_t T, int64_t D);
+int64_t scan_ws_floats(int64_t B, int64_t T, int64_t D);
+hipError_t launch_scan_fwd(hipStream_t s, const ScanArgs& a, void* y, int64_t ldy, float* h_end, float* states, float* ws);
+hipError_t launch_scan_bwd(hipStream_t s, const ScanArgs& a, const void* dy, int64_t lddy, const float* dh_end, const float* states,
+                           void* df, int64_t lddf, void* dx, int64_t lddx, float* dh0, float* ws);
+
 // attention.hip
 // Multi-head attention of Tq queries over Tk keys per (batch, head), scale 1/sqrt(hd).  q, k, v point at element
 // (batch 0, row 0, feature 0) of arrays in `dtype`; rows are ldq (q) and ldkv (k and v) elements apart, batch b

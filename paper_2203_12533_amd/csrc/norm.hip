@@ -473,9 +473,9 @@ __global__ __launch_bounds__(kRpCols * kRpGroups) void reduce_parts_multi_kernel
     out[c] = accumulate ? out[c] + t : t;
   }
 }
-static inline void launch_reduce_parts(hipStream_t s, const float* ws, float* out, int parts, int64_t stride, int64_t cols,
-                                       int accumulate) {
+hipError_t launch_reduce_parts(hipStream_t s, const float* ws, float* out, int parts, int64_t stride, int64_t cols, int accumulate) {
   reduce_parts_kernel<<<(unsigned)((cols + kRpCols - 1) / kRpCols), kRpCols * kRpGroups, 0, s>>>(ws, out, parts, stride, cols, accumulate);
+  return hipGetLastError();
 }
 
 hipError_t launch_layernorm_bwd(hipStream_t s, int dtype, const void* dy, const float* x, const float* g,
@@ -619,8 +619,7 @@ hipError_t launch_colsum(hipStream_t s, int dtype, const void* in, float* out, f
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  launch_reduce_parts(s, ws, out, rows > 0 ? slabs : 0, cols, cols, accumulate);
-  return hipGetLastError();
+  return launch_reduce_parts(s, ws, out, rows > 0 ? slabs : 0, cols, cols, accumulate);
 }
 
 }  // namespace pw

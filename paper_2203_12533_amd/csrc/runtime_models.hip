@@ -303,6 +303,61 @@ pw_status pw_op_adam(pw_ctx* c, float* w, float* m, float* v, const float* g, vo
   PW_OP(c, launch_adam(c->exec, w, m, v, g, w_bf16, n, lr, beta1, beta2, eps, t, nullptr));
 }
 
+// The context's GPU is current while a launcher runs and what was current before is current again afterwards.
+namespace {
+struct OnDevice {
+  int before = -1;
+  bool switched = false;
+  explicit OnDevice(int device) { switched = hipGetDevice(&before) == hipSuccess && before != device && hipSetDevice(device) == hipSuccess; }
+  ~OnDevice() { if (switched) (void)hipSetDevice(before); }
+};
+}  // namespace
+#define PW_OP_ON_DEVICE(c, expr)          \
+  do {                                    \
+    if (!(c)) return PW_ERR_INVALID;      \
+    OnDevice on_((c)->device);            \
+    PW_OP(c, expr);                       \
+  } while (0)
+
+int64_t pw_f8_scale_bytes(int64_t rows, int64_t cols) { return f8_scale_bytes(rows, cols); }
+pw_status pw_op_f8_quantize(pw_ctx* c, const pw_f8_quantize_args* a) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_f8_quantize(c->exec, F8QuantizeArgs{a->dtype, a->format, a->block_rows, a->x, a->rows, a->cols, a->ldx, a->q, a->ldq,
+                                                               a->q_scale, a->qt, a->ldqt, a->qt_scale}));
+}
+pw_status pw_op_f8_gemm(pw_ctx* c, const pw_f8_gemm_args* a) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_gemm_f8(c->exec, GemmF8Args{a->a_format, a->b_format, a->M, a->N, a->K, a->lda, a->ldb, a->ldc, a->epilogue,
+                                                       a->out_dtype, a->accumulate, a->A, a->B, a->a_scale, a->b_scale, a->bias, a->aux,
+                                                       a->C, a->C2}));
+}
+static DropoutArgs dropout_args_of(const pw_dropout_args* a) {
+  return DropoutArgs{a->dtype, a->out_dtype, a->rows, a->cols, a->ldx, a->ldy, a->p, a->seed, a->site, a->step, a->step_dev};
+}
+pw_status pw_op_dropout_fwd(pw_ctx* c, const pw_dropout_args* a, const void* x, const float* bias, const float* res, void* y) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_dropout_fwd(c->exec, dropout_args_of(a), x, bias, res, y));
+}
+pw_status pw_op_dropout_bwd(pw_ctx* c, const pw_dropout_args* a, const void* dy, void* dx, float* dbias, float* ws, int accumulate) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_dropout_bwd(c->exec, dropout_args_of(a), dy, dx, dbias, ws, accumulate));
+}
+int64_t pw_dropout_bwd_ws_floats(int64_t rows, int64_t cols) { return dropout_bwd_ws_floats(rows, cols); }
+static ScanArgs scan_args_of(const pw_scan_args* a) {
+  return ScanArgs{a->dtype, a->f, a->x, a->ldf, a->ldx, a->B, a->T, a->D, a->h0, a->lens};
+}
+pw_status pw_op_scan_fwd(pw_ctx* c, const pw_scan_args* a, void* y, int64_t ldy, float* h_end, float* states, float* ws) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_scan_fwd(c->exec, scan_args_of(a), y, ldy, h_end, states, ws));
+}
+pw_status pw_op_scan_bwd(pw_ctx* c, const pw_scan_args* a, const void* dy, int64_t lddy, const float* dh_end, const float* states, void* df,
+                         int64_t lddf, void* dx, int64_t lddx, float* dh0, float* ws) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_scan_bwd(c->exec, scan_args_of(a), dy, lddy, dh_end, states, df, lddf, dx, lddx, dh0, ws));
+}
+int64_t pw_scan_state_floats(int64_t B, int64_t T, int64_t D) { return scan_state_floats(B, T, D); }
+int64_t pw_scan_ws_floats(int64_t B, int64_t T, int64_t D) { return scan_ws_floats(B, T, D); }
+
 pw_status pw_profile_begin(pw_ctx* c) {
   if (!c) return PW_ERR_INVALID;
   gemm_profile_begin();

@@ -1,0 +1,150 @@
+"""Plain 64-bit references (numpy, CPU) of the 8-bit operands, the dropout mask and the gated recurrence, written from their
+definitions; the CPU suite checks them against published values and finite differences, the GPU tests use them."""
+import math
+
+import numpy as np
+
+
+# ---- 8-bit floating point ----
+TOP = {"e4m3": 448.0, "e5m2": 57344.0}
+HALF_STEP = {"e4m3": 2.0 ** -4, "e5m2": 2.0 ** -3, "bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+def decode_table(fmt):
+    mant, bias = (3, 7) if fmt == "e4m3" else (2, 15)
+    out = np.empty(256)
+    for i in range(256):
+        e, f = (i & 127) >> mant, i & ((1 << mant) - 1)
+        v = math.ldexp(f, 1 - bias - mant) if e == 0 else math.ldexp((1 << mant) + f, e - bias - mant)
+        if fmt == "e4m3" and i & 127 == 127:
+            v = math.nan
+        if fmt == "e5m2" and e == 31:
+            v = math.nan if f else math.inf
+        out[i] = -v if i & 128 else v
+    return out
+
+
+def scale_index(rows, blocks):
+    r, b = np.arange(rows)[:, None], np.arange(blocks)[None, :]
+    return b * (-(-rows // 64) * 64) + r // 64 * 64 + r % 16 * 4 + r % 64 // 16
+
+
+def scale_table(e):
+    """Exponents [rows, blocks] -> bytes in the library's layout."""
+    t = np.zeros(-(-e.shape[0] // 64) * 64 * e.shape[1], np.uint8)
+    t[scale_index(*e.shape)] = e + 127
+    return t
+
+
+def nearest_code(y, fmt):
+    """Byte of the nearest value, ties to the even code, for |y| within the format's range (or not finite)."""
+    v = decode_table(fmt)[:128]
+    n = int(np.isfinite(v).sum())
+    grid = v[:n]
+    a = np.abs(y)
+    at = np.clip(np.searchsorted(grid, a), 1, n - 1)
+    lo, hi = a - grid[at - 1], grid[at] - a
+    code = np.where((lo < hi) | ((lo == hi) & (at % 2 == 1)), at - 1, at)
+    if fmt == "e5m2":
+        code = np.where(np.isinf(y), 124, code)
+        code = np.where(np.isnan(y), 126, code)
+    else:
+        code = np.where(np.isfinite(y), code, 127)
+    return (code + 128 * np.signbit(y)).astype(np.uint8)
+
+
+def quantize(x, fmt, block_rows=1):
+    """(bytes [rows, columns up to a multiple of 16], exponents [rows, blocks]) of x in blocks of 128 columns."""
+    x = np.asarray(x, np.float64)
+    rows, cols = x.shape
+    nb = -(-cols // 128)
+    q, e = np.zeros((rows, -(-cols // 16) * 16), np.uint8), np.zeros((rows, nb), np.int64)
+    for r0 in range(0, rows, block_rows):
+        for b in range(nb):
+            part = x[r0:r0 + block_rows, 128 * b:128 * b + 128]
+            fin = np.abs(part[np.isfinite(part)])
+            top = fin.max() if fin.size else 0.0
+            k = -127 if top == 0 else max(-127, math.frexp(top / TOP[fmt])[1] - 1)
+            while top > TOP[fmt] * 2.0 ** k:
+                k += 1
+            while k > -127 and top <= TOP[fmt] * 2.0 ** (k - 1):
+                k -= 1
+            e[r0:r0 + block_rows, b] = k
+            q[r0:r0 + block_rows, 128 * b:128 * b + part.shape[1]] = nearest_code(part * 2.0 ** -k, fmt)
+    return q, e
+
+
+def values(q, e, fmt):
+    return decode_table(fmt)[q] * (2.0 ** np.repeat(e, 128, 1))[:, :q.shape[1]]
+
+
+def gelu(u):
+    return 0.5 * u * (1 + np.tanh(math.sqrt(2 / math.pi) * (u + 0.044715 * u ** 3)))
+
+
+def gelu_grad(u):
+    c = math.sqrt(2 / math.pi)
+    t = np.tanh(c * (u + 0.044715 * u ** 3))
+    return 0.5 * (1 + t) + 0.5 * u * (1 - t * t) * c * (1 + 3 * 0.044715 * u * u)
+
+
+# ---- dropout ----
+def philox(counter, key):
+    """Philox4x32-10 of four arrays of 32-bit words under a key of two."""
+    c = [np.asarray(v, np.uint32) for v in counter]
+    k = [int(key[0]), int(key[1])]
+    for _ in range(10):
+        p0, p1 = c[0].astype(np.uint64) * np.uint64(0xD2511F53), c[2].astype(np.uint64) * np.uint64(0xCD9E8D57)
+        h0, l0, h1, l1 = (p0 >> np.uint64(32)), p0 & np.uint64(0xFFFFFFFF), (p1 >> np.uint64(32)), p1 & np.uint64(0xFFFFFFFF)
+        c = [h1.astype(np.uint32) ^ c[1] ^ np.uint32(k[0]), l1.astype(np.uint32), h0.astype(np.uint32) ^ c[3] ^ np.uint32(k[1]),
+             l0.astype(np.uint32)]
+        k = [(k[0] + 0x9E3779B9) % (1 << 32), (k[1] + 0xBB67AE85) % (1 << 32)]
+    return c
+
+
+def dropout_threshold(p):
+    return int(np.rint(np.float32(p) * np.float32(65536.0)))
+
+
+def dropout_keep(rows, cols, p, seed, site, step):
+    g = -(-cols // 8)
+    shape = (rows, g)
+    w = philox([np.broadcast_to(np.arange(g), shape), np.broadcast_to(np.arange(rows)[:, None], shape), np.full(shape, site),
+                np.full(shape, step % (1 << 32))], (seed % (1 << 32), seed >> 32))
+    halves = np.stack([h for v in w for h in (v & np.uint32(0xFFFF), v >> np.uint32(16))], -1).reshape(rows, -1)[:, :cols]
+    t = dropout_threshold(p)
+    return halves >= t, (65536.0 / (65536 - t) if t < 65536 else 0.0)
+
+
+# ---- gated recurrence ----
+def _sigmoid(f):
+    return np.where(f >= 0, 1 / (1 + np.exp(-np.abs(f))), np.exp(-np.abs(f)) / (1 + np.exp(-np.abs(f))))
+
+
+def scan_fwd(f, x, h0, lens=None):
+    """f, x [B, T, D]; -> y [B, T, D], h_end [B, D]."""
+    B, T, D = f.shape
+    lens = np.full(B, T) if lens is None else np.clip(lens, 0, T)
+    y, h = np.zeros((B, T, D)), np.array(h0, np.float64)
+    for t in range(T):
+        on = t < lens
+        h[on] = _sigmoid(f[on, t]) * h[on] + _sigmoid(-f[on, t]) * x[on, t]
+        y[on, t] = h[on]
+    return y, h
+
+
+def scan_bwd(f, x, h0, dy, dh_end, lens=None):
+    """-> df, dx [B, T, D], dh0 [B, D]."""
+    B, T, D = f.shape
+    lens = np.full(B, T) if lens is None else np.clip(lens, 0, T)
+    y, _ = scan_fwd(f, x, h0, lens)
+    df, dx, r = np.zeros((B, T, D)), np.zeros((B, T, D)), np.array(dh_end, np.float64)
+    for t in reversed(range(T)):
+        on = t < lens
+        a, z = _sigmoid(f[on, t]), _sigmoid(-f[on, t])
+        before = y[on, t - 1] if t else np.asarray(h0)[on]
+        g = dy[on, t] + r[on]
+        dx[on, t] = g * z
+        df[on, t] = g * (before - x[on, t]) * a * z
+        r[on] = a * g
+    return df, dx, r
