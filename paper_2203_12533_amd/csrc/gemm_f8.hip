@@ -33,6 +33,74 @@ struct GemmF8Params {
   EpiParams epi;
 };
 
+typedef __attribute__((address_space(3))) void* lds_ptr;
+constexpr int kBK = 128;                  // k per tile: the length that shares a scale
+constexpr int64_t kMaxLd = 1 << 23;       // rows of a tile are within 32 bits of byte offset
+
+__device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};
+
+// Bytes from global memory straight into LDS at lds_off + 16 (4) * lane.
+__device__ __forceinline__ void dma16(const uint8_t* g, uint32_t lds_off) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(lds_off) : "memory", "m0");
+}
+__device__ __forceinline__ void dma16_s(const uint8_t* base, uint32_t off, uint32_t lds_off) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds_off) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(const uint8_t* g, uint32_t lds_off) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(g), "s"(lds_off) : "memory", "m0");
+}
+
+// WM x WN waves to a tile of WM FM x WN FN blocks of 16 x 16; WK such groups split k between them (WK > 1: of one wave each).
+template <int WM_, int WN_, int FM_, int FN_, int WK_>
+struct Tile {
+  static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, WK = WK_, G = WM * WN;
+  static constexpr int BM = 16 * WM * FM, BN = 16 * WN * FN, kThreads = 64 * G * WK;
+  static constexpr int kOperands = (BM + BN) * kBK, kStage = kOperands + BM + BN;   // bytes; the scales lie behind the operands
+  static constexpr int kLdP = BN + 4;
+  static constexpr size_t kRing = (size_t)WK * 2 * kStage;
+  static constexpr int kRowsAtOnce = BM < 64 ? BM : 64;                             // of partial sums in LDS, where waves share a tile
+  static constexpr size_t kParts = (size_t)(G > 1 ? kRowsAtOnce : WK * BM) * kLdP * 4;
+  static constexpr size_t kSmem = (kRing > kParts ? kRing : kParts) + 1023 & ~(size_t)1023;
+  static_assert(WK == 1 || G == 1, "groups of one wave only");
+};
+// What gemm_finish_tile sees of it.
+template <class S> struct Finish {
+  static constexpr int BM = S::G > 1 ? S::kRowsAtOnce : S::BM, BN = S::BN, WK = S::WK, kThreads = S::kThreads, kLdP = S::kLdP;
+};
+
+// One operand of a group's tile: R rows of 128 bytes, fetched by G waves in pieces of 1 KiB (8 rows); chunk c (16 bytes) of row
+// r lies at position c ^ ((r >> 1) & 7) of the row, so that the 16 rows of a fragment read hit all banks.
+template <int R, int G>
+struct Operand {
+  static constexpr int kPer = R / 8 / G;
+  const uint8_t* base;
+  uint32_t off[kPer];
+  __device__ __forceinline__ static int k_of(int instr, int lane) { return ((lane & 7) ^ (((instr * 8 + (lane >> 3)) >> 1) & 7)) * 16; }
+  __device__ __forceinline__ void init(const uint8_t* p, int64_t ld, int64_t row0, int64_t rows, int64_t first, int gw, int lane) {
+    base = p + row0 * ld + first * kBK;
+    const int last = (int)(rows - row0 < R ? rows - row0 : R) - 1;     // rows past the end are fetched from the last one
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int instr = gw * kPer + j, r = instr * 8 + (lane >> 3);
+      off[j] = (uint32_t)((r < last ? r : last) * (int)ld + k_of(instr, lane));
+    }
+  }
+  __device__ __forceinline__ void issue_one(int j, uint32_t lds_off, int gw) const { dma16_s(base, off[j], lds_off + (gw * kPer + j) * 1024); }
+  // A k tile of which `left` bytes exist (a multiple of 16).
+  __device__ __forceinline__ void issue(int64_t left, uint32_t lds_off, int gw, int lane) const {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      if (left >= kBK) {
+        issue_one(j, lds_off, gw);
+      } else {
+        const uint8_t* g = base + off[j];
+        if (k_of(gw * kPer + j, lane) >= left) g = reinterpret_cast<const uint8_t*>(kZeros);
+        dma16(g, lds_off + (gw * kPer + j) * 1024);
+      }
+    }
+  }
+};
+
 // Bytes 4 d .. 4 d + 3 of a fragment as bf16 numbers, times 2^(byte - 127).
 template <int FMT> __device__ __forceinline__ bf16x4 widen(int d, int scale_byte) {
   const float k = __uint_as_float((uint32_t)scale_byte << 23);
@@ -52,7 +120,7 @@ template <int FMT> __device__ __forceinline__ bf16x8 widen8(const i32x8& f, int 
 }
 
 template <int FA, int FB, bool EXACT>
-__global__ __launch_bounds__(256) void gemm_f8_kernel(GemmF8Params p) {
+__global__ __launch_bounds__(256) void gemm_f8_plain_kernel(GemmF8Params p) {
   int tm, tn;
   tile_of_block(blockIdx.x, p.tiles_m * p.tiles_n, p.tiles_m, p.tiles_n, tm, tn);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, L = lane & 15, g = lane >> 4;
@@ -105,7 +173,225 @@ __global__ __launch_bounds__(256) void gemm_f8_kernel(GemmF8Params p) {
       }
 }
 
+// 32 bytes of a lane's row: the chunks lane / 16 and 4 + lane / 16.
+__device__ __forceinline__ i32x8 read_fragment(uint32_t at0, uint32_t at1, uint32_t off) {
+  typedef __attribute__((address_space(3))) const i32x4* p;
+  const i32x4 a = *(p)(uintptr_t)(at0 + off), b = *(p)(uintptr_t)(at1 + off);
+  return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+__device__ __forceinline__ int read_scales(uint32_t at) {
+  typedef __attribute__((address_space(3))) const int* p;
+  return *(p)(uintptr_t)at;
+}
+// D[n][m] += B A^T of one block of k; byte IA of sa and IB of sb are the scales (the index has to be a constant).
+template <int FA, int FB> __device__ __forceinline__ f32x4 mfma(const i32x8& b, const i32x8& a, f32x4 c, int ib, int sb, int ia, int sa) {
+#define PW_F8_CASE(IB, IA) if (ib == IB && ia == IA) return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, FB, FA, IB, sb, IA, sa);
+  PW_F8_CASE(0, 0) PW_F8_CASE(0, 1) PW_F8_CASE(0, 2) PW_F8_CASE(0, 3) PW_F8_CASE(1, 0) PW_F8_CASE(1, 1) PW_F8_CASE(1, 2) PW_F8_CASE(1, 3)
+  PW_F8_CASE(2, 0) PW_F8_CASE(2, 1) PW_F8_CASE(2, 2) PW_F8_CASE(2, 3) PW_F8_CASE(3, 0) PW_F8_CASE(3, 1) PW_F8_CASE(3, 2)
+#undef PW_F8_CASE
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, FB, FA, 3, sb, 3, sa);
+}
+
+template <class S, int FA, int FB, bool EXACT>
+__global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_kernel(GemmF8Params p) {
+  constexpr int FM = S::FM, FN = S::FN, G = S::G, WN = S::WN;
+  using OpA = Operand<S::BM, G>;
+  using OpB = Operand<S::BN, G>;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  int tm, tn;
+  tile_of_block(blockIdx.x, p.tiles_m * p.tiles_n, p.tiles_m, p.tiles_n, tm, tn);
+  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int grp = wave / G, gw = wave % G, wm = gw / WN, wn = gw % WN, L = lane & 15, quarter = lane >> 4;
+
+  f32x4 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const int total = (int)((p.K + kBK - 1) / kBK), per = (total + S::WK - 1) / S::WK;
+  const int first = grp * per, n = total - first < per ? (total - first < 0 ? 0 : total - first) : per;
+  OpA oa;
+  OpB ob;
+  oa.init(p.A, p.lda, m0, p.M, first, gw, lane);
+  ob.init(p.B, p.ldb, n0, p.N, first, gw, lane);
+  const uint32_t ring = (uint32_t)(uintptr_t)(lds_ptr)smem + grp * (2 * S::kStage);
+  // Scales of the tile: BM / 4 words of A's table, then BN / 4 of B's, a word to a lane; groups of 64 rows that do not exist
+  // come from the last one.
+  constexpr int kWords = (S::BM + S::BN) / 4, kScaleWaves = (kWords + 63) / 64;
+  static_assert(kScaleWaves <= G, "a wave fetches 64 words at most");
+  const int64_t Ra = (p.M + 63) & ~63LL, Rb = (p.N + 63) & ~63LL;
+  const int word = gw * 64 + lane;
+  const bool of_a = word < S::BM / 4, scales = word < kWords;
+  const uint8_t* sp;
+  int64_t sp_step;
+  {
+    const int w = of_a ? word : word - S::BM / 4;
+    const int64_t R = of_a ? Ra : Rb, row = (of_a ? m0 : n0) + (w >> 4) * 64;
+    sp_step = R;
+    sp = (of_a ? p.sa : p.sb) + first * R + (row < R - 64 ? row : R - 64) + (w & 15) * 4;
+  }
+  auto issue_scales = [&](uint32_t st) {
+    if (gw < kScaleWaves) {
+      if (scales) dma4(sp, st + S::kOperands + gw * 256);
+      sp += sp_step;
+    }
+  };
+  auto issue = [&](int t) {
+    const int64_t left = p.K - (int64_t)(first + t) * kBK;
+    const uint32_t st = ring + (t & 1) * S::kStage;
+    oa.issue(left, st, gw, lane);
+    ob.issue(left, st + S::BM * kBK, gw, lane);
+    oa.base += kBK;
+    ob.base += kBK;
+    issue_scales(st);
+  };
+  // Addresses of this lane's fragments: block j of an operand is 16 j rows of 128 bytes further on, which leaves the swizzle
+  // of the row as it is.
+  const uint32_t row_a = ring + (wm * FM * 16 + L) * kBK, row_b = ring + S::BM * kBK + (wn * FN * 16 + L) * kBK;
+  const uint32_t c0 = (quarter ^ (L >> 1)) << 4, c1 = ((quarter + 4) ^ (L >> 1)) << 4;
+  const uint32_t a0 = row_a + c0, a1 = row_a + c1, b0 = row_b + c0, b1 = row_b + c1;
+  constexpr int GA = (FM + 3) / 4, GB = (FN + 3) / 4;       // words of four scales
+  const uint32_t s_a = ring + S::kOperands + wm * FM * 16 + L * 4, s_b = ring + S::kOperands + S::BM + wn * FN * 16 + L * 4;
+  auto landed_and_met = [&] {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    if (G > 1) __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  if (n > 0) issue(0);
+  landed_and_met();
+  for (int t = 0; t < n; ++t) {
+    const uint32_t st = (t & 1) * S::kStage;
+    if (t + 1 < n) issue(t + 1);
+    int sa[GA], sb[GB];
+    i32x8 fb[FN];
+#pragma unroll
+    for (int g = 0; g < GA; ++g) sa[g] = read_scales(s_a + st + g * 64);
+#pragma unroll
+    for (int g = 0; g < GB; ++g) sb[g] = read_scales(s_b + st + g * 64);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) fb[j] = read_fragment(b0, b1, st + j * 16 * kBK);
+    if constexpr (EXACT) {
+      bf16x8 wb[FN][4];
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) wb[j][s] = widen8<FB>(fb[j], s, (sb[j / 4] >> (8 * (j % 4))) & 255);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const i32x8 fa = read_fragment(a0, a1, st + i * 16 * kBK);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const bf16x8 wa = widen8<FA>(fa, s, (sa[i / 4] >> (8 * (i % 4))) & 255);
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][s], wa, acc[i][j], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const i32x8 fa = read_fragment(a0, a1, st + i * 16 * kBK);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = mfma<FA, FB>(fb[j], fa, acc[i][j], j % 4, sb[j / 4], i % 4, sa[i / 4]);
+      }
+    }
+    landed_and_met();
+  }
+
+  __syncthreads();
+  float* const parts = reinterpret_cast<float*>(smem);
+  auto finish = [&](int64_t m) {
+    switch (epi_extra_kind(p.epi)) {            // uniform over the launch
+      case kExtraAuxBf16: gemm_finish_tile<Finish<S>, kExtraAuxBf16>(parts, p, m, n0); break;
+      case kExtraAuxF32: gemm_finish_tile<Finish<S>, kExtraAuxF32>(parts, p, m, n0); break;
+      case kExtraOldC: gemm_finish_tile<Finish<S>, kExtraOldC>(parts, p, m, n0); break;
+      default: gemm_finish_tile<Finish<S>, kExtraNone>(parts, p, m, n0); break;
+    }
+  };
+  if constexpr (G == 1) {
+    float* mine = parts + (grp * S::BM + L) * S::kLdP + 4 * quarter;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) *reinterpret_cast<f32x4*>(mine + 16 * i * S::kLdP + 16 * j) = acc[i][j];
+    finish(m0);
+  } else {
+    constexpr int kAt = S::kRowsAtOnce / 16;     // blocks of rows that are in LDS at a time
+#pragma unroll
+    for (int c = 0; c < S::BM / S::kRowsAtOnce; ++c) {
+#pragma unroll
+      for (int i = 0; i < kAt; ++i) {
+        constexpr int kPerWave = FM;
+        const int blk = c * kAt + i;
+        if (blk / kPerWave == wm) {
+          float* mine = parts + (16 * i + L) * S::kLdP + wn * FN * 16 + 4 * quarter;
+#pragma unroll
+          for (int j = 0; j < FN; ++j) *reinterpret_cast<f32x4*>(mine + 16 * j) = acc[blk % kPerWave][j];
+        }
+      }
+      if (m0 + c * S::kRowsAtOnce < p.M) finish(m0 + c * S::kRowsAtOnce);
+      __syncthreads();
+    }
+  }
+}
+
+using Big = Tile<2, 4, 8, 4, 1>;       // 256 x 256
+using Mid = Tile<2, 2, 4, 4, 1>;       // 128 x 128, two workgroups per compute unit
+using Split = Tile<1, 1, 4, 4, 4>;     // 64 x 64, k over four waves
+
+template <class S, int FA, int FB, bool EXACT>
+hipError_t prepare() {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_f8_tile_kernel<S, FA, FB, EXACT>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)S::kSmem);
+}
+template <int FA, int FB>
+hipError_t prepare_formats() {
+  hipError_t e = prepare<Big, FA, FB, false>();
+  if (e == hipSuccess) e = prepare<Mid, FA, FB, false>();
+  if (e == hipSuccess) e = prepare<Mid, FA, FB, true>();
+  if (e == hipSuccess) e = prepare<Split, FA, FB, false>();
+  if (e == hipSuccess) e = prepare<Split, FA, FB, true>();
+  return e;
+}
+template <class S, int FA, int FB, bool EXACT>
+hipError_t launch(hipStream_t s, GemmF8Params p) {
+  const int64_t tm = (p.M + S::BM - 1) / S::BM, tn = (p.N + S::BN - 1) / S::BN;
+  if (tm * tn > (1LL << 26)) return hipErrorInvalidValue;
+  p.tiles_m = (int)tm;
+  p.tiles_n = (int)tn;
+  gemm_f8_tile_kernel<S, FA, FB, EXACT><<<(int)(tm * tn), S::kThreads, S::kSmem, s>>>(p);
+  return hipGetLastError();
+}
+template <int FA, int FB>
+hipError_t launch_plain(hipStream_t s, GemmF8Params p, bool exact) {
+  const int64_t tm = (p.M + 63) / 64, tn = (p.N + 63) / 64;
+  if (tm * tn > (1LL << 26)) return hipErrorInvalidValue;
+  p.tiles_m = (int)tm;
+  p.tiles_n = (int)tn;
+  if (exact) gemm_f8_plain_kernel<FA, FB, true><<<(int)(tm * tn), 256, 0, s>>>(p);
+  else gemm_f8_plain_kernel<FA, FB, false><<<(int)(tm * tn), 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+template <int FA, int FB>
+hipError_t choose(hipStream_t s, const GemmF8Params& p, bool exact) {
+  if (p.lda > kMaxLd || p.ldb > kMaxLd) return launch_plain<FA, FB>(s, p, exact);
+  auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
+  if (tiles(128, 128) <= 128) return exact ? launch<Split, FA, FB, true>(s, p) : launch<Split, FA, FB, false>(s, p);
+  if (exact) return launch<Mid, FA, FB, true>(s, p);
+  if (tiles(256, 256) >= 150) return launch<Big, FA, FB, false>(s, p);
+  return launch<Mid, FA, FB, false>(s, p);
+}
+
 }  // namespace
+
+hipError_t gemm_f8_init() {
+  hipError_t e = prepare_formats<0, 0>();
+  if (e == hipSuccess) e = prepare_formats<0, 1>();
+  if (e == hipSuccess) e = prepare_formats<1, 0>();
+  if (e == hipSuccess) e = prepare_formats<1, 1>();
+  return e;
+}
 
 hipError_t launch_gemm_f8(hipStream_t s, const GemmF8Args& a) {
   const int64_t most = 1LL << 30;
@@ -126,21 +412,9 @@ hipError_t launch_gemm_f8(hipStream_t s, const GemmF8Args& a) {
   p.M = a.M; p.N = a.N; p.K = a.K; p.lda = a.lda; p.ldb = a.ldb;
   p.epi.mode = a.epilogue; p.epi.out_bf16 = a.out_dtype == kBF16; p.epi.accumulate = a.accumulate;
   p.epi.bias = a.bias; p.epi.aux = a.aux; p.epi.C = a.C; p.epi.C2 = a.C2; p.epi.ldc = a.ldc;
-  const int64_t tm = (a.M + 63) / 64, tn = (a.N + 63) / 64;
-  if (tm * tn > (1LL << 26)) return hipErrorInvalidValue;
-  p.tiles_m = (int)tm;
-  p.tiles_n = (int)tn;
-  const int grid = (int)(tm * tn);
-  auto go = [&](auto fa, auto fb) {
-    constexpr int A = decltype(fa)::value, B = decltype(fb)::value;
-    if (a.out_dtype == kF32) gemm_f8_kernel<A, B, true><<<grid, 256, 0, s>>>(p);
-    else gemm_f8_kernel<A, B, false><<<grid, 256, 0, s>>>(p);
-  };
-  using e4m3 = std::integral_constant<int, 0>;
-  using e5m2 = std::integral_constant<int, 1>;
-  if (a.a_format == kE4M3) a.b_format == kE4M3 ? go(e4m3{}, e4m3{}) : go(e4m3{}, e5m2{});
-  else a.b_format == kE4M3 ? go(e5m2{}, e4m3{}) : go(e5m2{}, e5m2{});
-  return hipGetLastError();
+  const bool exact = a.out_dtype == kF32;
+  if (a.a_format == kE4M3) return a.b_format == kE4M3 ? choose<0, 0>(s, p, exact) : choose<0, 1>(s, p, exact);
+  return a.b_format == kE4M3 ? choose<1, 0>(s, p, exact) : choose<1, 1>(s, p, exact);
 }
 
 }  // namespace pw

@@ -156,6 +156,8 @@ struct GemmF8Args {
   void* C2;
 };
 hipError_t launch_gemm_f8(hipStream_t s, const GemmF8Args& a);
+// One-time set-up of kernel attributes (dynamic LDS); call once before any capture.
+hipError_t gemm_f8_init();
 
 // dropout.hip
 struct DropoutArgs {

@@ -57,21 +57,17 @@ def quantize(x, fmt, block_rows=1):
     """(bytes [rows, columns up to a multiple of 16], exponents [rows, blocks]) of x in blocks of 128 columns."""
     x = np.asarray(x, np.float64)
     rows, cols = x.shape
-    nb = -(-cols // 128)
-    q, e = np.zeros((rows, -(-cols // 16) * 16), np.uint8), np.zeros((rows, nb), np.int64)
-    for r0 in range(0, rows, block_rows):
-        for b in range(nb):
-            part = x[r0:r0 + block_rows, 128 * b:128 * b + 128]
-            fin = np.abs(part[np.isfinite(part)])
-            top = fin.max() if fin.size else 0.0
-            k = -127 if top == 0 else max(-127, math.frexp(top / TOP[fmt])[1] - 1)
-            while top > TOP[fmt] * 2.0 ** k:
-                k += 1
-            while k > -127 and top <= TOP[fmt] * 2.0 ** (k - 1):
-                k -= 1
-            e[r0:r0 + block_rows, b] = k
-            q[r0:r0 + block_rows, 128 * b:128 * b + part.shape[1]] = nearest_code(part * 2.0 ** -k, fmt)
-    return q, e
+    nb, R = -(-cols // 128), -(-rows // block_rows) * block_rows
+    full = np.zeros((R, nb * 128))
+    full[:rows, :cols] = x
+    mag = np.where(np.isfinite(full), np.abs(full), 0.0).reshape(-1, block_rows, nb, 128)
+    top = mag.max((1, 3))
+    e = np.maximum(np.frexp(np.where(top == 0, 0.0, top / TOP[fmt]))[1].astype(np.int64) - 1, -127)     # at most one too small or large
+    e = np.where(top > TOP[fmt] * 2.0 ** e, e + 1, e)
+    e = np.where((e > -127) & (top <= TOP[fmt] * 2.0 ** (e - 1.0)), e - 1, e)
+    e = np.where(top == 0, -127, e).repeat(block_rows, 0)[:rows]
+    scaled = full[:rows] * 2.0 ** -np.repeat(e, 128, 1).astype(np.float64)
+    return nearest_code(scaled[:, :-(-cols // 16) * 16], fmt), e
 
 
 def values(q, e, fmt):

@@ -250,6 +250,22 @@ def test_f8_product_epilogues(ctx, M, N, K, epilogue, bf16, accumulate):
     product(ctx, M, N, K, epilogue=epilogue, bf16=bf16, accumulate=accumulate, seed=M, block=128)
 
 
+@pytest.mark.parametrize("M,N,K,kw", [
+    (1500, 1420, 400, {"bf16": True}), (1500, 1420, 400, {"fa": "e5m2", "epilogue": pwb.PW_EPI_BIAS_RESIDUAL}),
+    (1408, 1536, 272, {"fb": "e5m2"}), (3100, 3900, 272, {"bf16": True, "epilogue": pwb.PW_EPI_BIAS}),
+    (3100, 3900, 144, {"bf16": True, "epilogue": pwb.PW_EPI_GELU_BWD, "fa": "e5m2"}),
+    (2560, 4096, 384, {"bf16": True, "epilogue": pwb.PW_EPI_BIAS_GELU, "block": 128}), (2560, 4096, 128, {"bf16": True}),
+    (2570, 4099, 272, {"epilogue": pwb.PW_EPI_BIAS}), (40000, 70, 144, {"bf16": True}), (70, 40000, 144, {"accumulate": 1})])
+def test_f8_product_many_tiles(ctx, M, N, K, kw):
+    product(ctx, M, N, K, seed=2, **kw)
+
+
+def test_f8_product_of_rows_far_apart(ctx):
+    product(ctx, 3, 40, 144, lda=(1 << 23) + 16, bf16=True)
+    product(ctx, 40, 3, 144, ldb=(1 << 23) + 16)
+    product(ctx, 70, 5, 400, lda=1 << 23, epilogue=pwb.PW_EPI_BIAS)
+
+
 def test_f8_product_strides_missing_bias_and_empty_sums(ctx):
     product(ctx, 70, 90, 144, lda=208, ldb=176, ldc=136, epilogue=pwb.PW_EPI_BIAS, bf16=True)
     product(ctx, 33, 40, 128, epilogue=pwb.PW_EPI_BIAS, bias=False)
