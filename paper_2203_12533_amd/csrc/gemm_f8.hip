@@ -51,11 +51,12 @@ __device__ __forceinline__ void dma4(const uint8_t* g, uint32_t lds_off) {
 }
 
 // WM x WN waves to a tile of WM FM x WN FN blocks of 16 x 16; WK such groups split k between them (WK > 1: of one wave each).
-template <int WM_, int WN_, int FM_, int FN_, int WK_>
+template <int WM_, int WN_, int FM_, int FN_, int WK_, bool PIPELINED_ = false>
 struct Tile {
+  static constexpr bool kPipelined = PIPELINED_;
   static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, WK = WK_, G = WM * WN;
   static constexpr int BM = 16 * WM * FM, BN = 16 * WN * FN, kThreads = 64 * G * WK;
-  static constexpr int kOperands = (BM + BN) * kBK, kStage = kOperands + BM + BN;   // bytes; the scales lie behind the operands
+  static constexpr int kOperands = (BM + BN) * kBK, kStage = kOperands + (BM + BN + 255) / 256 * 256;   // bytes; the scales lie behind the operands
   static constexpr int kLdP = BN + 4;
   static constexpr size_t kRing = (size_t)WK * 2 * kStage;
   static constexpr int kRowsAtOnce = BM < 64 ? BM : 64;                             // of partial sums in LDS, where waves share a tile
@@ -86,17 +87,12 @@ struct Operand {
     }
   }
   __device__ __forceinline__ void issue_one(int j, uint32_t lds_off, int gw) const { dma16_s(base, off[j], lds_off + (gw * kPer + j) * 1024); }
-  // A k tile of which `left` bytes exist (a multiple of 16).
+  // The next k tile, of which `left` bytes exist (a multiple of 16; whole, partial or none): the rest comes from zeros.
   __device__ __forceinline__ void issue(int64_t left, uint32_t lds_off, int gw, int lane) const {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      if (left >= kBK) {
-        issue_one(j, lds_off, gw);
-      } else {
-        const uint8_t* g = base + off[j];
-        if (k_of(gw * kPer + j, lane) >= left) g = reinterpret_cast<const uint8_t*>(kZeros);
-        dma16(g, lds_off + (gw * kPer + j) * 1024);
-      }
+      const uint8_t* const g = base + off[j];
+      dma16(k_of(gw * kPer + j, lane) < left ? g : reinterpret_cast<const uint8_t*>(kZeros), lds_off + (gw * kPer + j) * 1024);
     }
   }
 };
@@ -217,26 +213,19 @@ __global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_
   oa.init(p.A, p.lda, m0, p.M, first, gw, lane);
   ob.init(p.B, p.ldb, n0, p.N, first, gw, lane);
   const uint32_t ring = (uint32_t)(uintptr_t)(lds_ptr)smem + grp * (2 * S::kStage);
-  // Scales of the tile: BM / 4 words of A's table, then BN / 4 of B's, a word to a lane; groups of 64 rows that do not exist
-  // come from the last one.
-  constexpr int kWords = (S::BM + S::BN) / 4, kScaleWaves = (kWords + 63) / 64;
-  static_assert(kScaleWaves <= G, "a wave fetches 64 words at most");
+  // Scales of the tile: BM / 4 words of A's table, then BN / 4 of B's.  Every wave fetches 64 of them, the same ones as another
+  // where there are fewer (a branch here would let the compiler move MFMAs past it); groups of 64 rows that do not exist come
+  // from the last one.
+  constexpr int kWords = (S::BM + S::BN) / 4, kSets = (kWords + 63) / 64;
+  static_assert(kSets <= G && (kWords % 64 == 0 || kSets == 1), "a wave fetches 64 words");
   const int64_t Ra = (p.M + 63) & ~63LL, Rb = (p.N + 63) & ~63LL;
-  const int word = gw * 64 + lane;
-  const bool of_a = word < S::BM / 4, scales = word < kWords;
-  const uint8_t* sp;
-  int64_t sp_step;
-  {
-    const int w = of_a ? word : word - S::BM / 4;
-    const int64_t R = of_a ? Ra : Rb, row = (of_a ? m0 : n0) + (w >> 4) * 64;
-    sp_step = R;
-    sp = (of_a ? p.sa : p.sb) + first * R + (row < R - 64 ? row : R - 64) + (w & 15) * 4;
-  }
-  auto issue_scales = [&](uint32_t st) {
-    if (gw < kScaleWaves) {
-      if (scales) dma4(sp, st + S::kOperands + gw * 256);
-      sp += sp_step;
-    }
+  const int word = (gw % kSets * 64 + lane) % kWords, w = word < S::BM / 4 ? word : word - S::BM / 4;
+  const bool of_a = word < S::BM / 4;
+  const int64_t sp_step = of_a ? Ra : Rb, sp_row = (of_a ? m0 : n0) + (w >> 4) * 64;
+  const uint8_t* const sp = (of_a ? p.sa : p.sb) + (sp_row < sp_step - 64 ? sp_row : sp_step - 64) + (w & 15) * 4;
+  auto issue_scales = [&](int t, uint32_t st) {
+    const int kb = first + t < total ? first + t : total - 1;
+    dma4(sp + kb * sp_step, st + S::kOperands + gw % kSets * 256);
   };
   auto issue = [&](int t) {
     const int64_t left = p.K - (int64_t)(first + t) * kBK;
@@ -245,7 +234,7 @@ __global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_
     ob.issue(left, st + S::BM * kBK, gw, lane);
     oa.base += kBK;
     ob.base += kBK;
-    issue_scales(st);
+    issue_scales(t, st);
   };
   // Addresses of this lane's fragments: block j of an operand is 16 j rows of 128 bytes further on, which leaves the swizzle
   // of the row as it is.
@@ -259,44 +248,132 @@ __global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_
     if (G > 1) __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  if (n > 0) issue(0);
-  landed_and_met();
-  for (int t = 0; t < n; ++t) {
-    const uint32_t st = (t & 1) * S::kStage;
-    if (t + 1 < n) issue(t + 1);
-    int sa[GA], sb[GB];
-    i32x8 fb[FN];
+  if constexpr (S::kPipelined && !EXACT) {
+    // MFMAs run across k tiles without a pause.  A unit is one block of rows against all columns of the wave; the fragments of the
+    // next block are read while it runs.  All of a tile has been asked for one unit before its end: there the waves meet, the
+    // next tile is there, and the stage of this one is free for the one after next, whose direct loads go out between the
+    // MFMAs of the last unit; the next tile's columns take the place of this one's as those are used for the last time.
+    static_assert(FM % 2 == 0 && GA + GB <= FN, "two fragments of rows in turn; a slot for each word of scales");
+    constexpr int kPer = OpA::kPer + OpB::kPer;
+    i32x8 fa[2], fb[FN];
+    int sa[GA], sb[GB], nsa[GA], nsb[GB];
+    auto read_a = [&](uint32_t st, int i) { fa[i & 1] = read_fragment(a0 + st, a1 + st, i * 16 * kBK); };
+    auto read_b = [&](uint32_t st, int j) { fb[j] = read_fragment(b0 + st, b1 + st, j * 16 * kBK); };
+    auto read_scale = [&](uint32_t st, int g) {
+      if (g < GA) nsa[g] = read_scales(s_a + st + g * 64);
+      else nsb[g - GA] = read_scales(s_b + st + (g - GA) * 64);
+    };
+    auto take_scales = [&] {
 #pragma unroll
-    for (int g = 0; g < GA; ++g) sa[g] = read_scales(s_a + st + g * 64);
+      for (int g = 0; g < GA; ++g) sa[g] = nsa[g];
 #pragma unroll
-    for (int g = 0; g < GB; ++g) sb[g] = read_scales(s_b + st + g * 64);
-#pragma unroll
-    for (int j = 0; j < FN; ++j) fb[j] = read_fragment(b0, b1, st + j * 16 * kBK);
-    if constexpr (EXACT) {
-      bf16x8 wb[FN][4];
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int s = 0; s < 4; ++s) wb[j][s] = widen8<FB>(fb[j], s, (sb[j / 4] >> (8 * (j % 4))) & 255);
+      for (int g = 0; g < GB; ++g) sb[g] = nsb[g];
+    };
+    auto issue_one = [&](int t, int m) {       // of the whole tile t
+      const uint32_t st = ring + (t & 1) * S::kStage;
+      if (m < OpA::kPer) oa.issue_one(m, st, gw);
+      else ob.issue_one(m - OpA::kPer, st + S::BM * kBK, gw);
+      if (m == kPer - 1) {
+        oa.base += kBK;
+        ob.base += kBK;
+        issue_scales(t, st);
+      }
+    };
+    // STREAM: tile t + 2 is a whole one; MORE: tile t + 1 exists (t + 2, where it does not, is made of zeros nobody reads).  No
+    // branches inside: the compiler would move MFMAs past them.
+    auto tile = [&](int t, auto streaming, auto follows) {
+      constexpr bool STREAM = decltype(streaming)::value, more = decltype(follows)::value;
+      const uint32_t st = (t & 1) * S::kStage, next = S::kStage - st;
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        const i32x8 fa = read_fragment(a0, a1, st + i * 16 * kBK);
+        if (i == FM - 1 && more) {
+          landed_and_met();
+          if (!STREAM) issue(t + 2);
+        }
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const bf16x8 wa = widen8<FA>(fa, s, (sa[i / 4] >> (8 * (i % 4))) & 255);
+        for (int jj = 0; jj < FN; ++jj) {
+          // back and forth: consecutive MFMAs share an operand; the last unit and the next tile's first in one order
+          const int j = (i & 1) || i == 0 ? jj : FN - 1 - jj;
+          __builtin_amdgcn_sched_barrier(0);
+          // behind the first MFMA of a tile, so that its wait does not cover what is asked for here
+          if (i < FM - 1 && jj == (i == 0 ? 1 : 0)) read_a(st, i + 1);
+          if (i == FM - 1 && more) {
+            if (jj < GA + GB) read_scale(next, jj);
+            if (jj == 0) read_a(next, 0);
+            if (STREAM) {
 #pragma unroll
-          for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][s], wa, acc[i][j], 0, 0, 0);
+              for (int m = jj * kPer / FN; m < (jj + 1) * kPer / FN; ++m) issue_one(t + 2, m);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          acc[i][j] = mfma<FA, FB>(fb[j], fa[i & 1], acc[i][j], j % 4, sb[j / 4], i % 4, sa[i / 4]);
+          if (i == FM - 1 && more) {           // the column block's last use
+            __builtin_amdgcn_sched_barrier(0);
+            read_b(next, j);
+          }
         }
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const i32x8 fa = read_fragment(a0, a1, st + i * 16 * kBK);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mfma<FA, FB>(fb[j], fa, acc[i][j], j % 4, sb[j / 4], i % 4, sa[i / 4]);
-      }
-    }
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) take_scales();
+    };
+    if (n > 0) issue(0);
     landed_and_met();
+    if (n > 1) issue(1);
+    if (n > 0) {
+#pragma unroll
+      for (int g = 0; g < GA + GB; ++g) read_scale(0, g);
+      take_scales();
+      read_a(0, 0);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) read_b(0, j);
+    }
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    int t = 0;
+    for (; t + 3 < n; ++t) tile(t, yes, yes);  // the last tile may be a partial one
+    for (; t + 1 < n; ++t) tile(t, no, yes);
+    if (t < n) tile(t, no, no);
+    landed_and_met();
+  } else {
+    if (n > 0) issue(0);
+    landed_and_met();
+    for (int t = 0; t < n; ++t) {
+      const uint32_t st = (t & 1) * S::kStage;
+      if (t + 1 < n) issue(t + 1);
+      int sa[GA], sb[GB];
+      i32x8 fb[FN];
+#pragma unroll
+      for (int g = 0; g < GA; ++g) sa[g] = read_scales(s_a + st + g * 64);
+#pragma unroll
+      for (int g = 0; g < GB; ++g) sb[g] = read_scales(s_b + st + g * 64);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[j] = read_fragment(b0, b1, st + j * 16 * kBK);
+      if constexpr (EXACT) {
+        bf16x8 wb[FN][4];
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int s = 0; s < 4; ++s) wb[j][s] = widen8<FB>(fb[j], s, (sb[j / 4] >> (8 * (j % 4))) & 255);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+          const i32x8 fa = read_fragment(a0, a1, st + i * 16 * kBK);
+#pragma unroll
+          for (int s = 0; s < 4; ++s) {
+            const bf16x8 wa = widen8<FA>(fa, s, (sa[i / 4] >> (8 * (i % 4))) & 255);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][s], wa, acc[i][j], 0, 0, 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+          const i32x8 fa = read_fragment(a0, a1, st + i * 16 * kBK);
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j] = mfma<FA, FB>(fb[j], fa, acc[i][j], j % 4, sb[j / 4], i % 4, sa[i / 4]);
+        }
+      }
+      landed_and_met();
+    }
   }
 
   __syncthreads();
@@ -309,6 +386,10 @@ __global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_
       default: gemm_finish_tile<Finish<S>, kExtraNone>(parts, p, m, n0); break;
     }
   };
+  if (S::kPipelined && m0 + S::BM <= p.M && n0 + S::BN <= p.N) {
+    gemm_epilogue_staged<(FM + 1) / 2, (FN + 3) / 4 * 2>(reinterpret_cast<bf16*>(smem), acc, p, m0 + wm * FM * 16, n0 + wn * FN * 16, wave, lane);
+    return;
+  }
   if constexpr (G == 1) {
     float* mine = parts + (grp * S::BM + L) * S::kLdP + 4 * quarter;
 #pragma unroll
@@ -336,7 +417,7 @@ __global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_
   }
 }
 
-using Big = Tile<2, 4, 8, 4, 1>;       // 256 x 256
+using Big = Tile<2, 4, 8, 4, 1, true>;       // 256 x 256
 using Mid = Tile<2, 2, 4, 4, 1>;       // 128 x 128, two workgroups per compute unit
 using Split = Tile<1, 1, 4, 4, 4>;     // 64 x 64, k over four waves
 
