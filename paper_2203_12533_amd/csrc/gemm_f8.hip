@@ -115,58 +115,86 @@ template <int FMT> __device__ __forceinline__ bf16x8 widen8(const i32x8& f, int 
   return bf16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
-template <int FA, int FB, bool EXACT>
-__global__ __launch_bounds__(256) void gemm_f8_plain_kernel(GemmF8Params p) {
-  int tm, tn;
-  tile_of_block(blockIdx.x, p.tiles_m * p.tiles_n, p.tiles_m, p.tiles_n, tm, tn);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, L = lane & 15, g = lane >> 4;
-  const int64_t m0 = (int64_t)tm * 64 + (wave >> 1) * 32, n0 = (int64_t)tn * 64 + (wave & 1) * 32;
+// Few rows, and rows too far apart for 32-bit offsets.  What bounds a product of few rows is reading B once, so nothing is
+// staged: a block owns 16 columns and 16 FM rows, its waves take every fourth k block, operands go from memory straight into
+// fragments (a lane has 32 consecutive bytes of its row, four lanes a line), kAhead blocks at a time, and the waves' sums meet
+// in LDS in wave order.
+constexpr int kAhead = 4, kDirectWaves = 4;
+template <int FM, int FA, int FB, bool EXACT>
+__global__ __launch_bounds__(64 * kDirectWaves) void gemm_f8_direct_kernel(GemmF8Params p) {
+  __shared__ __attribute__((aligned(16))) float part[kDirectWaves][FM][16][16 + 4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, L = lane & 15, g = lane >> 4;
+  const int64_t m0 = (int64_t)(blockIdx.x / p.tiles_n) * (16 * FM), n0 = (int64_t)(blockIdx.x % p.tiles_n) * 16;
   const int64_t Ra = (p.M + 63) & ~63LL, Rb = (p.N + 63) & ~63LL;
-  f32x4 acc[2][2] = {};
-  for (int64_t k0 = 0, kb = 0; k0 < p.K; k0 += 128, ++kb) {
-    i32x8 fa[2], fb[2];
-    int sa[2], sb[2];
-    auto load = [&](const uint8_t* base, int64_t ld, int64_t row, int64_t rows, i32x8& f) {
-      if (row >= rows) row = rows - 1;
+  auto in = [](int64_t r, int64_t rows) { return r < rows ? r : rows - 1; };
+  auto scale_of = [](const uint8_t* t, int64_t r) { return t + (r & ~63LL) + (r & 15) * 4 + ((r & 63) >> 4); };
+  const int64_t rb = in(n0 + L, p.N);
+  const uint8_t* const pb = p.B + rb * p.ldb + 32 * g;
+  const uint8_t* const qb = scale_of(p.sb, rb);
+  const uint8_t *pa[FM], *qa[FM];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int64_t k = k0 + 16 * (g + 4 * h);
-        i32x4 v = {};
-        if (k < p.K) v = *reinterpret_cast<const i32x4*>(base + row * ld + k);
+  for (int i = 0; i < FM; ++i) {
+    const int64_t ra = in(m0 + 16 * i + L, p.M);
+    pa[i] = p.A + ra * p.lda + 32 * g;
+    qa[i] = scale_of(p.sa, ra);
+  }
+  f32x4 acc[FM] = {};
+  const int total = (int)((p.K + kBK - 1) / kBK);
+  auto load = [&](const uint8_t* q, int kb) {
+    i32x8 f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[4 * h + e] = v[e];
+    for (int h = 0; h < 2; ++h) {
+      const int64_t k = (int64_t)kb * kBK;
+      i32x4 v = {};
+      if (k + 32 * g + 16 * h < p.K) v = *reinterpret_cast<const i32x4*>(q + k + 16 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[4 * h + e] = v[e];
+    }
+    return f;
+  };
+  auto several = [&](int kb, auto count) {
+    constexpr int U = decltype(count)::value;
+    i32x8 fb[U], fa[U][FM];
+    int sb[U], sa[U][FM];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = kb + u * kDirectWaves;
+      fb[u] = load(pb, k);
+      sb[u] = qb[k * Rb];
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        fa[u][i] = load(pa[i], k);
+        sa[u][i] = qa[i][k * Ra];
       }
-    };
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t ra = m0 + 16 * i + L, rb = n0 + 16 * i + L;
-      load(p.A, p.lda, ra, p.M, fa[i]);
-      load(p.B, p.ldb, rb, p.N, fb[i]);
-      sa[i] = p.sa[kb * Ra + (ra & ~63LL) + (ra & 15) * 4 + ((ra & 63) >> 4)];
-      sb[i] = p.sb[kb * Rb + (rb & ~63LL) + (rb & 15) * 4 + ((rb & 63) >> 4)];
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int i = 0; i < FM; ++i) {
         if constexpr (EXACT) {
 #pragma unroll
           for (int s = 0; s < 4; ++s)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FB>(fb[j], s, sb[j]), widen8<FA>(fa[i], s, sa[i]), acc[i][j], 0, 0, 0);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FB>(fb[u], s, sb[u]), widen8<FA>(fa[u][i], s, sa[u][i]), acc[i], 0, 0, 0);
         } else {
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i], acc[i][j], FB, FA, 0, sb[j], 0, sa[i]);
+          acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u], fa[u][i], acc[i], FB, FA, 0, sb[u], 0, sa[u][i]);
         }
       }
+  };
+  int kb = wave;
+  for (; kb + (kAhead - 1) * kDirectWaves < total; kb += kAhead * kDirectWaves) several(kb, std::integral_constant<int, kAhead>{});
+  for (; kb < total; kb += kDirectWaves) several(kb, std::integral_constant<int, 1>{});
+#pragma unroll
+  for (int i = 0; i < FM; ++i) *reinterpret_cast<f32x4*>(&part[wave][i][L][4 * g]) = acc[i];
+  __syncthreads();
+  const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    float v = part[0][i][r][c];
+#pragma unroll
+    for (int w = 1; w < kDirectWaves; ++w) v += part[w][i][r][c];
+    const int64_t m = m0 + 16 * i + r, n = n0 + c;
+    if (m < p.M && n < p.N) epilogue1<true>(p.epi, m, n, v);
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t m = m0 + 16 * i + L, n = n0 + 16 * j + 4 * g + r;
-        if (m < p.M && n < p.N) epilogue1<true>(p.epi, m, n, acc[i][j][r]);
-      }
 }
 
 // 32 bytes of a lane's row: the chunks lane / 16 and 4 + lane / 16.
@@ -444,20 +472,21 @@ hipError_t launch(hipStream_t s, GemmF8Params p) {
   gemm_f8_tile_kernel<S, FA, FB, EXACT><<<(int)(tm * tn), S::kThreads, S::kSmem, s>>>(p);
   return hipGetLastError();
 }
-template <int FA, int FB>
-hipError_t launch_plain(hipStream_t s, GemmF8Params p, bool exact) {
-  const int64_t tm = (p.M + 63) / 64, tn = (p.N + 63) / 64;
-  if (tm * tn > (1LL << 26)) return hipErrorInvalidValue;
+template <int FM, int FA, int FB>
+hipError_t launch_direct(hipStream_t s, GemmF8Params p, bool exact) {
+  const int64_t tm = (p.M + 16 * FM - 1) / (16 * FM), tn = (p.N + 15) / 16;
+  if (tm * tn > (1LL << 30)) return hipErrorInvalidValue;
   p.tiles_m = (int)tm;
   p.tiles_n = (int)tn;
-  if (exact) gemm_f8_plain_kernel<FA, FB, true><<<(int)(tm * tn), 256, 0, s>>>(p);
-  else gemm_f8_plain_kernel<FA, FB, false><<<(int)(tm * tn), 256, 0, s>>>(p);
+  if (exact) gemm_f8_direct_kernel<FM, FA, FB, true><<<(int)(tm * tn), 64 * kDirectWaves, 0, s>>>(p);
+  else gemm_f8_direct_kernel<FM, FA, FB, false><<<(int)(tm * tn), 64 * kDirectWaves, 0, s>>>(p);
   return hipGetLastError();
 }
 template <int FA, int FB>
 hipError_t choose(hipStream_t s, const GemmF8Params& p, bool exact) {
-  if (p.lda > kMaxLd || p.ldb > kMaxLd) return launch_plain<FA, FB>(s, p, exact);
   auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
+  if (p.M <= 16) return launch_direct<1, FA, FB>(s, p, exact);
+  if (p.M <= 32 || p.lda > kMaxLd || p.ldb > kMaxLd) return launch_direct<2, FA, FB>(s, p, exact);
   if (tiles(128, 128) <= 128) return exact ? launch<Split, FA, FB, true>(s, p) : launch<Split, FA, FB, false>(s, p);
   if (exact) return launch<Mid, FA, FB, true>(s, p);
   if (tiles(256, 256) >= 150) return launch<Big, FA, FB, false>(s, p);
