@@ -51,17 +51,19 @@ __device__ __forceinline__ void dma4(const uint8_t* g, uint32_t lds_off) {
 }
 
 // WM x WN waves to a tile of WM FM x WN FN blocks of 16 x 16; WK such groups split k between them (WK > 1: of one wave each).
-template <int WM_, int WN_, int FM_, int FN_, int WK_, bool PIPELINED_ = false>
+template <int WM_, int WN_, int FM_, int FN_, int WK_, int NS_ = 2>
 struct Tile {
-  static constexpr bool kPipelined = PIPELINED_;
+  static constexpr int NS = NS_;                                                    // stages of LDS per group
   static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, WK = WK_, G = WM * WN;
   static constexpr int BM = 16 * WM * FM, BN = 16 * WN * FN, kThreads = 64 * G * WK;
-  static constexpr int kOperands = (BM + BN) * kBK, kStage = kOperands + (BM + BN + 255) / 256 * 256;   // bytes; the scales lie behind the operands
+  static constexpr int kScalesA = BM < 64 ? 64 : BM, kScales = kScalesA + BN;       // bytes: whole groups of 64 rows
+  static constexpr int kOperands = (BM + BN) * kBK, kStage = kOperands + (kScales + 255) / 256 * 256;   // the scales lie behind the operands
   static constexpr int kLdP = BN + 4;
-  static constexpr size_t kRing = (size_t)WK * 2 * kStage;
+  static constexpr size_t kRing = (size_t)WK * NS * kStage;
   static constexpr int kRowsAtOnce = BM < 64 ? BM : 64;                             // of partial sums in LDS, where waves share a tile
   static constexpr size_t kParts = (size_t)(G > 1 ? kRowsAtOnce : WK * BM) * kLdP * 4;
   static constexpr size_t kSmem = (kRing > kParts ? kRing : kParts) + 1023 & ~(size_t)1023;
+  static constexpr int kWavesPerSimd = WK == 1 ? 2 : 1;
   static_assert(WK == 1 || G == 1, "groups of one wave only");
 };
 // What gemm_finish_tile sees of it.
@@ -116,29 +118,24 @@ template <int FMT> __device__ __forceinline__ bf16x8 widen8(const i32x8& f, int 
 }
 
 // Few rows, and rows too far apart for 32-bit offsets.  What bounds a product of few rows is reading B once, so nothing is
-// staged: a block owns 16 columns and 16 FM rows, its waves take every fourth k block, operands go from memory straight into
+// staged: a block owns 16 columns and 16 rows, its waves take every W-th k block, operands go from memory straight into
 // fragments (a lane has 32 consecutive bytes of its row, four lanes a line), kAhead blocks at a time, and the waves' sums meet
-// in LDS in wave order.
-constexpr int kAhead = 4, kDirectWaves = 4;
-template <int FM, int FA, int FB, bool EXACT>
-__global__ __launch_bounds__(64 * kDirectWaves) void gemm_f8_direct_kernel(GemmF8Params p) {
-  __shared__ __attribute__((aligned(16))) float part[kDirectWaves][FM][16][16 + 4];
+// in LDS in wave order.  1 x 8192 x 2048: 5.4 us a pass, of which the launch is about 4.
+constexpr int kAhead = 4;
+template <int W, int FA, int FB, bool EXACT>
+__global__ __launch_bounds__(64 * W) void gemm_f8_direct_kernel(GemmF8Params p) {
+  __shared__ __attribute__((aligned(16))) float part[W][16][16 + 4];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, L = lane & 15, g = lane >> 4;
-  const int64_t m0 = (int64_t)(blockIdx.x / p.tiles_n) * (16 * FM), n0 = (int64_t)(blockIdx.x % p.tiles_n) * 16;
+  const int64_t m0 = (int64_t)(blockIdx.x / p.tiles_n) * 16, n0 = (int64_t)(blockIdx.x % p.tiles_n) * 16;
   const int64_t Ra = (p.M + 63) & ~63LL, Rb = (p.N + 63) & ~63LL;
   auto in = [](int64_t r, int64_t rows) { return r < rows ? r : rows - 1; };
   auto scale_of = [](const uint8_t* t, int64_t r) { return t + (r & ~63LL) + (r & 15) * 4 + ((r & 63) >> 4); };
-  const int64_t rb = in(n0 + L, p.N);
+  const int64_t ra = in(m0 + L, p.M), rb = in(n0 + L, p.N);
+  const uint8_t* const pa = p.A + ra * p.lda + 32 * g;
   const uint8_t* const pb = p.B + rb * p.ldb + 32 * g;
+  const uint8_t* const qa = scale_of(p.sa, ra);
   const uint8_t* const qb = scale_of(p.sb, rb);
-  const uint8_t *pa[FM], *qa[FM];
-#pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const int64_t ra = in(m0 + 16 * i + L, p.M);
-    pa[i] = p.A + ra * p.lda + 32 * g;
-    qa[i] = scale_of(p.sa, ra);
-  }
-  f32x4 acc[FM] = {};
+  f32x4 acc = {};
   const int total = (int)((p.K + kBK - 1) / kBK);
   auto load = [&](const uint8_t* q, int kb) {
     i32x8 f;
@@ -154,46 +151,38 @@ __global__ __launch_bounds__(64 * kDirectWaves) void gemm_f8_direct_kernel(GemmF
   };
   auto several = [&](int kb, auto count) {
     constexpr int U = decltype(count)::value;
-    i32x8 fb[U], fa[U][FM];
-    int sb[U], sa[U][FM];
+    i32x8 fa[U], fb[U];
+    int sa[U], sb[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int k = kb + u * kDirectWaves;
+      const int k = kb + u * W;
       fb[u] = load(pb, k);
       sb[u] = qb[k * Rb];
-#pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        fa[u][i] = load(pa[i], k);
-        sa[u][i] = qa[i][k * Ra];
-      }
+      fa[u] = load(pa, k);
+      sa[u] = qa[k * Ra];
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      if constexpr (EXACT) {
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        if constexpr (EXACT) {
-#pragma unroll
-          for (int s = 0; s < 4; ++s)
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FB>(fb[u], s, sb[u]), widen8<FA>(fa[u][i], s, sa[u][i]), acc[i], 0, 0, 0);
-        } else {
-          acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u], fa[u][i], acc[i], FB, FA, 0, sb[u], 0, sa[u][i]);
-        }
+        for (int s = 0; s < 4; ++s)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FB>(fb[u], s, sb[u]), widen8<FA>(fa[u], s, sa[u]), acc, 0, 0, 0);
+      } else {
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u], fa[u], acc, FB, FA, 0, sb[u], 0, sa[u]);
       }
+    }
   };
   int kb = wave;
-  for (; kb + (kAhead - 1) * kDirectWaves < total; kb += kAhead * kDirectWaves) several(kb, std::integral_constant<int, kAhead>{});
-  for (; kb < total; kb += kDirectWaves) several(kb, std::integral_constant<int, 1>{});
-#pragma unroll
-  for (int i = 0; i < FM; ++i) *reinterpret_cast<f32x4*>(&part[wave][i][L][4 * g]) = acc[i];
+  for (; kb + (kAhead - 1) * W < total; kb += kAhead * W) several(kb, std::integral_constant<int, kAhead>{});
+  for (; kb < total; kb += W) several(kb, std::integral_constant<int, 1>{});
+  *reinterpret_cast<f32x4*>(&part[wave][L][4 * g]) = acc;
   __syncthreads();
   const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
+  if (r < 16 && m0 + r < p.M && n0 + c < p.N) {
+    float v = part[0][r][c];
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    float v = part[0][i][r][c];
-#pragma unroll
-    for (int w = 1; w < kDirectWaves; ++w) v += part[w][i][r][c];
-    const int64_t m = m0 + 16 * i + r, n = n0 + c;
-    if (m < p.M && n < p.N) epilogue1<true>(p.epi, m, n, v);
+    for (int w = 1; w < W; ++w) v += part[w][r][c];
+    epilogue1<true>(p.epi, m0 + r, n0 + c, v);
   }
 }
 
@@ -217,7 +206,7 @@ template <int FA, int FB> __device__ __forceinline__ f32x4 mfma(const i32x8& b, 
 }
 
 template <class S, int FA, int FB, bool EXACT>
-__global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_kernel(GemmF8Params p) {
+__global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_kernel(GemmF8Params p) {
   constexpr int FM = S::FM, FN = S::FN, G = S::G, WN = S::WN;
   using OpA = Operand<S::BM, G>;
   using OpB = Operand<S::BN, G>;
@@ -240,24 +229,24 @@ __global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_
   OpB ob;
   oa.init(p.A, p.lda, m0, p.M, first, gw, lane);
   ob.init(p.B, p.ldb, n0, p.N, first, gw, lane);
-  const uint32_t ring = (uint32_t)(uintptr_t)(lds_ptr)smem + grp * (2 * S::kStage);
-  // Scales of the tile: BM / 4 words of A's table, then BN / 4 of B's.  Every wave fetches 64 of them, the same ones as another
+  const uint32_t ring = (uint32_t)(uintptr_t)(lds_ptr)smem + grp * (S::NS * S::kStage);
+  // Scales of the tile: kScalesA / 4 words of A's table, then BN / 4 of B's.  Every wave fetches 64 of them, the same ones as another
   // where there are fewer (a branch here would let the compiler move MFMAs past it); groups of 64 rows that do not exist come
   // from the last one.
-  constexpr int kWords = (S::BM + S::BN) / 4, kSets = (kWords + 63) / 64;
+  constexpr int kWords = S::kScales / 4, kSets = (kWords + 63) / 64;
   static_assert(kSets <= G && (kWords % 64 == 0 || kSets == 1), "a wave fetches 64 words");
   const int64_t Ra = (p.M + 63) & ~63LL, Rb = (p.N + 63) & ~63LL;
-  const int word = (gw % kSets * 64 + lane) % kWords, w = word < S::BM / 4 ? word : word - S::BM / 4;
-  const bool of_a = word < S::BM / 4;
-  const int64_t sp_step = of_a ? Ra : Rb, sp_row = (of_a ? m0 : n0) + (w >> 4) * 64;
+  const int word = (gw % kSets * 64 + lane) % kWords, w = word < S::kScalesA / 4 ? word : word - S::kScalesA / 4;
+  const bool of_a = word < S::kScalesA / 4;
+  const int64_t sp_step = of_a ? Ra : Rb, sp_row = (of_a ? m0 & ~63LL : n0) + (w >> 4) * 64;
   const uint8_t* const sp = (of_a ? p.sa : p.sb) + (sp_row < sp_step - 64 ? sp_row : sp_step - 64) + (w & 15) * 4;
   auto issue_scales = [&](int t, uint32_t st) {
     const int kb = first + t < total ? first + t : total - 1;
     dma4(sp + kb * sp_step, st + S::kOperands + gw % kSets * 256);
   };
-  auto issue = [&](int t) {
+  auto issue = [&](int t, uint32_t at) {       // k tile t into the stage at `at`; zeros where it does not exist
     const int64_t left = p.K - (int64_t)(first + t) * kBK;
-    const uint32_t st = ring + (t & 1) * S::kStage;
+    const uint32_t st = ring + at;
     oa.issue(left, st, gw, lane);
     ob.issue(left, st + S::BM * kBK, gw, lane);
     oa.base += kBK;
@@ -270,70 +259,99 @@ __global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_
   const uint32_t c0 = (quarter ^ (L >> 1)) << 4, c1 = ((quarter + 4) ^ (L >> 1)) << 4;
   const uint32_t a0 = row_a + c0, a1 = row_a + c1, b0 = row_b + c0, b1 = row_b + c1;
   constexpr int GA = (FM + 3) / 4, GB = (FN + 3) / 4;       // words of four scales
-  const uint32_t s_a = ring + S::kOperands + wm * FM * 16 + L * 4, s_b = ring + S::kOperands + S::BM + wn * FN * 16 + L * 4;
-  auto landed_and_met = [&] {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  const int rows_at = (S::BM < 64 ? (int)(m0 & 63) : 0) + wm * FM * 16, cols_at = wn * FN * 16;   // of this wave, in the words' groups
+  const uint32_t s_a = ring + S::kOperands + (rows_at & ~63) + L * 4, s_b = ring + S::kOperands + S::kScalesA + (cols_at & ~63) + L * 4;
+  // A wave of fewer than 64 rows (columns) begins with a later byte of its word.
+  auto word_a = [&](int v) { return FM % 4 ? v >> ((rows_at & 63) / 2) : v; };
+  auto word_b = [&](int v) { return FN % 4 ? v >> ((cols_at & 63) / 2) : v; };
+  constexpr int kPer = OpA::kPer + OpB::kPer, kLoads = kPer + 1;    // direct loads of a wave per k tile
+  // All but the direct loads of the `later` tiles asked for last are there, and this wave's LDS reads are done ...
+  auto landed = [&](auto later) { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(later)::value * kLoads) : "memory"); };
+  auto meet = [&] {                            // ... and those of the group's other waves
     if (G > 1) __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  if constexpr (S::kPipelined && !EXACT) {
-    // MFMAs run across k tiles without a pause.  A unit is one block of rows against all columns of the wave; the fragments of the
-    // next block are read while it runs.  All of a tile has been asked for one unit before its end: there the waves meet, the
-    // next tile is there, and the stage of this one is free for the one after next, whose direct loads go out between the
-    // MFMAs of the last unit; the next tile's columns take the place of this one's as those are used for the last time.
-    static_assert(FM % 2 == 0 && GA + GB <= FN, "two fragments of rows in turn; a slot for each word of scales");
-    constexpr int kPer = OpA::kPer + OpB::kPer;
-    i32x8 fa[2], fb[FN];
-    int sa[GA], sb[GB], nsa[GA], nsb[GB];
-    auto read_a = [&](uint32_t st, int i) { fa[i & 1] = read_fragment(a0 + st, a1 + st, i * 16 * kBK); };
-    auto read_b = [&](uint32_t st, int j) { fb[j] = read_fragment(b0 + st, b1 + st, j * 16 * kBK); };
-    auto read_scale = [&](uint32_t st, int g) {
-      if (g < GA) nsa[g] = read_scales(s_a + st + g * 64);
-      else nsb[g - GA] = read_scales(s_b + st + (g - GA) * 64);
-    };
-    auto take_scales = [&] {
+  i32x8 fa[2], fb[FN];
+  int sa[GA], sb[GB], nsa[GA], nsb[GB];
+  auto read_a = [&](uint32_t st, int i) { fa[i & 1] = read_fragment(a0 + st, a1 + st, i * 16 * kBK); };
+  auto read_b = [&](uint32_t st, int j) { fb[j] = read_fragment(b0 + st, b1 + st, j * 16 * kBK); };
+  auto read_scale = [&](uint32_t st, int g) {
+    if (g < GA) nsa[g] = read_scales(s_a + st + g * 64);
+    else nsb[g - GA] = read_scales(s_b + st + (g - GA) * 64);
+  };
+  auto take_scales = [&] {
 #pragma unroll
-      for (int g = 0; g < GA; ++g) sa[g] = nsa[g];
+    for (int g = 0; g < GA; ++g) sa[g] = word_a(nsa[g]);
 #pragma unroll
-      for (int g = 0; g < GB; ++g) sb[g] = nsb[g];
-    };
-    auto issue_one = [&](int t, int m) {       // of the whole tile t
-      const uint32_t st = ring + (t & 1) * S::kStage;
-      if (m < OpA::kPer) oa.issue_one(m, st, gw);
-      else ob.issue_one(m - OpA::kPer, st + S::BM * kBK, gw);
-      if (m == kPer - 1) {
-        oa.base += kBK;
-        ob.base += kBK;
-        issue_scales(t, st);
+    for (int g = 0; g < GB; ++g) sb[g] = word_b(nsb[g]);
+  };
+  auto issue_one = [&](int t, int m, uint32_t at) {       // of the whole tile t
+    const uint32_t st = ring + at;
+    if (m < OpA::kPer) oa.issue_one(m, st, gw);
+    else ob.issue_one(m - OpA::kPer, st + S::BM * kBK, gw);
+    if (m == kPer - 1) {
+      oa.base += kBK;
+      ob.base += kBK;
+      issue_scales(t, st);
+    }
+  };
+  bf16x8 wa[EXACT ? 2 : 1][4], wb[EXACT ? FN : 1][4];
+  auto byte_of = [](const int* w, int i) { return (w[i / 4] >> (8 * (i % 4))) & 255; };
+  // MFMAs run across k tiles without a pause.  A unit is one block of rows against all columns of the wave.
+  //  8-bit pipe: the next block's fragments are read while a unit runs.  All of a tile has been asked for one unit before its
+  //    end; the next tile's columns take the place of this one's as those are used for the last time.
+  //  bf16 pipe: the next block is widened while a unit runs and the one after it read; the columns are widened between the MFMAs
+  //    of the first unit, and their bytes' registers are free from there on.  All of a tile has been asked for two units before
+  //    its end.
+  // There (kTurn) the waves meet, the next tile is there, and the stage of this one is free for tile t + NS, whose direct loads
+  // go out between the MFMAs that are left.
+  // STREAM: tile t + NS is a whole one; MORE: tile t + 1 exists (t + NS, where it does not, is made of zeros nobody reads).  No
+  // branches inside: the compiler would move MFMAs past them.
+  constexpr int kTurn = EXACT ? FM - 2 : FM - 1, kSlots = (FM - kTurn) * FN;
+  static_assert(FM % 2 == 0 && GA + GB <= FN && (!EXACT || 4 % FN == 0), "two fragments of rows in turn; a slot for each word of scales");
+  auto tile = [&](int t, uint32_t st, uint32_t next, auto streaming, auto follows) {
+    constexpr bool STREAM = decltype(streaming)::value, more = decltype(follows)::value;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      if (i == kTurn && more) {
+        landed(std::integral_constant<int, S::NS - 2>{});
+        meet();
+        if (!STREAM) issue(t + S::NS, st);
       }
-    };
-    // STREAM: tile t + 2 is a whole one; MORE: tile t + 1 exists (t + 2, where it does not, is made of zeros nobody reads).  No
-    // branches inside: the compiler would move MFMAs past them.
-    auto tile = [&](int t, auto streaming, auto follows) {
-      constexpr bool STREAM = decltype(streaming)::value, more = decltype(follows)::value;
-      const uint32_t st = (t & 1) * S::kStage, next = S::kStage - st;
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        if (i == FM - 1 && more) {
-          landed_and_met();
-          if (!STREAM) issue(t + 2);
-        }
-#pragma unroll
-        for (int jj = 0; jj < FN; ++jj) {
-          // back and forth: consecutive MFMAs share an operand; the last unit and the next tile's first in one order
-          const int j = (i & 1) || i == 0 ? jj : FN - 1 - jj;
-          __builtin_amdgcn_sched_barrier(0);
-          // behind the first MFMA of a tile, so that its wait does not cover what is asked for here
+      for (int jj = 0; jj < FN; ++jj) {
+        // back and forth: consecutive MFMAs share an operand; the last unit and the next tile's first in one order
+        const int j = (i & 1) || i == 0 ? jj : FN - 1 - jj, slot = (i - kTurn) * FN + jj;
+        __builtin_amdgcn_sched_barrier(0);
+        if (EXACT) {
+          if (i < FM - 2 && jj == 0) read_a(st, i + 2);
+        } else {                               // behind the first MFMA of a tile, so that its wait does not cover this
           if (i < FM - 1 && jj == (i == 0 ? 1 : 0)) read_a(st, i + 1);
-          if (i == FM - 1 && more) {
-            if (jj < GA + GB) read_scale(next, jj);
-            if (jj == 0) read_a(next, 0);
-            if (STREAM) {
+        }
+        if (slot >= 0 && more) {
+          if (slot < GA + GB) read_scale(next, slot);
+          if (slot == 0) read_a(next, 0);
+          if (EXACT && slot == FN) read_a(next, 1);
+          if (EXACT && (slot & 1)) read_b(next, slot >> 1);
+          if (STREAM) {
 #pragma unroll
-              for (int m = jj * kPer / FN; m < (jj + 1) * kPer / FN; ++m) issue_one(t + 2, m);
-            }
+            for (int m = slot * kPer / kSlots; m < (slot + 1) * kPer / kSlots; ++m) issue_one(t + S::NS, m, st);
           }
-          __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (EXACT) {
+          if (i == 0) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) wb[j][s] = widen8<FB>(fb[j], s, byte_of(sb, j));
+          }
+          if (i + 1 < FM || more) {
+            const int k = i + 1 < FM ? byte_of(sa, i + 1) : word_a(nsa[0]) & 255;
+#pragma unroll
+            for (int s = jj * 4 / FN; s < (jj + 1) * 4 / FN; ++s) wa[(i + 1) & 1][s] = widen8<FA>(fa[(i + 1) & 1], s, k);
+          }
+#pragma unroll
+          for (int s = 0; s < 4; ++s) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][s], wa[i & 1][s], acc[i][j], 0, 0, 0);
+        } else {
           acc[i][j] = mfma<FA, FB>(fb[j], fa[i & 1], acc[i][j], j % 4, sb[j / 4], i % 4, sa[i / 4]);
           if (i == FM - 1 && more) {           // the column block's last use
             __builtin_amdgcn_sched_barrier(0);
@@ -341,67 +359,41 @@ __global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_
           }
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if (more) take_scales();
-    };
-    if (n > 0) issue(0);
-    landed_and_met();
-    if (n > 1) issue(1);
-    if (n > 0) {
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) take_scales();
+  };
+  if (n > 0) {
 #pragma unroll
-      for (int g = 0; g < GA + GB; ++g) read_scale(0, g);
-      take_scales();
-      read_a(0, 0);
+    for (int i = 0; i < S::NS; ++i) issue(i, i * S::kStage);
+    landed(std::integral_constant<int, S::NS - 1>{});
+    meet();
 #pragma unroll
-      for (int j = 0; j < FN; ++j) read_b(0, j);
+    for (int g = 0; g < GA + GB; ++g) read_scale(0, g);
+    take_scales();
+    read_a(0, 0);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) read_b(0, j);
+    if constexpr (EXACT) {
+      read_a(0, 1);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) wa[0][s] = widen8<FA>(fa[0], s, byte_of(sa, 0));
     }
     constexpr std::true_type yes;
     constexpr std::false_type no;
     int t = 0;
-    for (; t + 3 < n; ++t) tile(t, yes, yes);  // the last tile may be a partial one
-    for (; t + 1 < n; ++t) tile(t, no, yes);
-    if (t < n) tile(t, no, no);
-    landed_and_met();
-  } else {
-    if (n > 0) issue(0);
-    landed_and_met();
-    for (int t = 0; t < n; ++t) {
-      const uint32_t st = (t & 1) * S::kStage;
-      if (t + 1 < n) issue(t + 1);
-      int sa[GA], sb[GB];
-      i32x8 fb[FN];
-#pragma unroll
-      for (int g = 0; g < GA; ++g) sa[g] = read_scales(s_a + st + g * 64);
-#pragma unroll
-      for (int g = 0; g < GB; ++g) sb[g] = read_scales(s_b + st + g * 64);
-#pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = read_fragment(b0, b1, st + j * 16 * kBK);
-      if constexpr (EXACT) {
-        bf16x8 wb[FN][4];
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-          for (int s = 0; s < 4; ++s) wb[j][s] = widen8<FB>(fb[j], s, (sb[j / 4] >> (8 * (j % 4))) & 255);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          const i32x8 fa = read_fragment(a0, a1, st + i * 16 * kBK);
-#pragma unroll
-          for (int s = 0; s < 4; ++s) {
-            const bf16x8 wa = widen8<FA>(fa, s, (sa[i / 4] >> (8 * (i % 4))) & 255);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][s], wa, acc[i][j], 0, 0, 0);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          const i32x8 fa = read_fragment(a0, a1, st + i * 16 * kBK);
-#pragma unroll
-          for (int j = 0; j < FN; ++j) acc[i][j] = mfma<FA, FB>(fb[j], fa, acc[i][j], j % 4, sb[j / 4], i % 4, sa[i / 4]);
-        }
-      }
-      landed_and_met();
+    uint32_t st = 0;
+    auto after = [](uint32_t at) { return at == (S::NS - 1) * S::kStage ? 0u : at + S::kStage; };
+    for (; t + S::NS + 1 < n; ++t) {           // the last tile may be a partial one
+      tile(t, st, after(st), yes, yes);
+      st = after(st);
     }
+    for (; t + 1 < n; ++t) {
+      tile(t, st, after(st), no, yes);
+      st = after(st);
+    }
+    tile(t, st, 0, no, no);
+    landed(std::integral_constant<int, 0>{});  // nothing is on its way into LDS any more
   }
 
   __syncthreads();
@@ -414,9 +406,11 @@ __global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_
       default: gemm_finish_tile<Finish<S>, kExtraNone>(parts, p, m, n0); break;
     }
   };
-  if (S::kPipelined && m0 + S::BM <= p.M && n0 + S::BN <= p.N) {
-    gemm_epilogue_staged<(FM + 1) / 2, (FN + 3) / 4 * 2>(reinterpret_cast<bf16*>(smem), acc, p, m0 + wm * FM * 16, n0 + wn * FN * 16, wave, lane);
-    return;
+  if constexpr (G > 1 && FN % 4 == 0) {
+    if (m0 + S::BM <= p.M && n0 + S::BN <= p.N) {
+      gemm_epilogue_staged<FM / 2, FN / 2>(reinterpret_cast<bf16*>(smem), acc, p, m0 + wm * FM * 16, n0 + wn * FN * 16, wave, lane);
+      return;
+    }
   }
   if constexpr (G == 1) {
     float* mine = parts + (grp * S::BM + L) * S::kLdP + 4 * quarter;
@@ -445,23 +439,32 @@ __global__ __launch_bounds__(S::kThreads, S::WK == 1 ? 2 : 1) void gemm_f8_tile_
   }
 }
 
-using Big = Tile<2, 4, 8, 4, 1, true>;       // 256 x 256
-using Mid = Tile<2, 2, 4, 4, 1>;       // 128 x 128, two workgroups per compute unit
-using Split = Tile<1, 1, 4, 4, 4>;     // 64 x 64, k over four waves
+using Big = Tile<2, 4, 8, 4, 1>;        // 256 x 256
+using Mid = Tile<2, 2, 4, 4, 1>;        // 128 x 128, two workgroups to a compute unit
+using MidOne = Tile<2, 2, 4, 4, 1, 4>;  // the same with four stages, one workgroup to a unit
+using Half = Tile<2, 2, 4, 2, 1, 3>;    // 128 x 64
+using Split = Tile<1, 1, 4, 4, 4>;      // 64 x 64, k over four waves
+using Few = Tile<1, 1, 2, 4, 4, 3>;     // 32 x 64, likewise
 
 template <class S, int FA, int FB, bool EXACT>
 hipError_t prepare() {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_f8_tile_kernel<S, FA, FB, EXACT>), hipFuncAttributeMaxDynamicSharedMemorySize,
                              (int)S::kSmem);
 }
+template <int FA, int FB, class S, class... Rest>
+hipError_t prepare_both() {
+  hipError_t e = prepare<S, FA, FB, false>();
+  if (e == hipSuccess) e = prepare<S, FA, FB, true>();
+  if constexpr (sizeof...(Rest) > 0) {
+    if (e == hipSuccess) e = prepare_both<FA, FB, Rest...>();
+  }
+  return e;
+}
 template <int FA, int FB>
 hipError_t prepare_formats() {
   hipError_t e = prepare<Big, FA, FB, false>();
-  if (e == hipSuccess) e = prepare<Mid, FA, FB, false>();
-  if (e == hipSuccess) e = prepare<Mid, FA, FB, true>();
-  if (e == hipSuccess) e = prepare<Split, FA, FB, false>();
-  if (e == hipSuccess) e = prepare<Split, FA, FB, true>();
-  return e;
+  if (e == hipSuccess) e = prepare<MidOne, FA, FB, false>();
+  return e == hipSuccess ? prepare_both<FA, FB, Mid, Half, Split, Few>() : e;
 }
 template <class S, int FA, int FB, bool EXACT>
 hipError_t launch(hipStream_t s, GemmF8Params p) {
@@ -472,25 +475,39 @@ hipError_t launch(hipStream_t s, GemmF8Params p) {
   gemm_f8_tile_kernel<S, FA, FB, EXACT><<<(int)(tm * tn), S::kThreads, S::kSmem, s>>>(p);
   return hipGetLastError();
 }
-template <int FM, int FA, int FB>
+template <int W, int FA, int FB>
 hipError_t launch_direct(hipStream_t s, GemmF8Params p, bool exact) {
-  const int64_t tm = (p.M + 16 * FM - 1) / (16 * FM), tn = (p.N + 15) / 16;
+  const int64_t tm = (p.M + 15) / 16, tn = (p.N + 15) / 16;
   if (tm * tn > (1LL << 30)) return hipErrorInvalidValue;
   p.tiles_m = (int)tm;
   p.tiles_n = (int)tn;
-  if (exact) gemm_f8_direct_kernel<FM, FA, FB, true><<<(int)(tm * tn), 64 * kDirectWaves, 0, s>>>(p);
-  else gemm_f8_direct_kernel<FM, FA, FB, false><<<(int)(tm * tn), 64 * kDirectWaves, 0, s>>>(p);
+  if (exact) gemm_f8_direct_kernel<W, FA, FB, true><<<(int)(tm * tn), 64 * W, 0, s>>>(p);
+  else gemm_f8_direct_kernel<W, FA, FB, false><<<(int)(tm * tn), 64 * W, 0, s>>>(p);
   return hipGetLastError();
 }
+// Which shape: the largest whose tiles give every compute unit one, as a launch of up to one round takes as long as one tile.
+// us (rows x columns x k, bf16 out unless it says fp32):
+//   direct    1 x 8192 x 2048 5.4 (Few 5.8), 1 x 32768 x 2048 13.4 (15.3), 1 x 8192 x 8192 14.1 (13.2), 4 x 8192 x 2048 6.0 (5.7), 16 x 2048 x 2048
+//             4.9 (5.7), 32 x 2048 x 2048 4.7 (5.7), 16 x 8192 x 2048 6.8 (5.9); eight waves from k = 4096 on: 1 x 2048 x 8192 7.9 (four: 8.6)
+//   Few       256 x 2048 x 2048 6.1 (Split 7.1), 64 x 2048 x 8192 11.4 (16.0), fp32 7.6 (9.5); 512 x 2048 x 2048, two rounds, 10.5 (7.4)
+//   Split     512 x 2048 x 2048 7.4 (Half 9.7), 1024 x 1024 x 1024 6.0 (7.2), fp32 7.7 (9.9); 1024 x 2048 x 2048 13.6 (10.3)
+//   Half      1024 x 2048 x 2048 10.3 (Mid 14.8, MidOne 13.5), fp32 16.8 (20.5)
+//   MidOne    1024 x 4096 x 2048 14.8 (Mid 15.8, Half 15.5), 2048 x 2048 x 8192 37.8 (44.4, 43.5); fp32 66.2 (66.1, 72.7): left to Mid
+//   Mid       1500 x 4096 x 2048 19.7 (MidOne 27.2, Half 23.4, Big 31.0), fp32 32.1 (40.8, 35.3)
+//   Big       a round from 144 tiles on, 2304 x 4096 x 2048 30.1 (Mid 31.1), 2816 x 3840 x 8192 89 (96); beyond one where few of the last
+//             are idle: 384 tiles, 6144 x 4096 x 2048, 60.3 (58.2), 320 59.8 (53.4), 272 60.5 (50.1), 512, k = 512, 30.9 (33.7)
 template <int FA, int FB>
 hipError_t choose(hipStream_t s, const GemmF8Params& p, bool exact) {
   auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
-  if (p.M <= 16) return launch_direct<1, FA, FB>(s, p, exact);
-  if (p.M <= 32 || p.lda > kMaxLd || p.ldb > kMaxLd) return launch_direct<2, FA, FB>(s, p, exact);
-  if (tiles(128, 128) <= 128) return exact ? launch<Split, FA, FB, true>(s, p) : launch<Split, FA, FB, false>(s, p);
+  if (p.M < 4 || tiles(16, 16) <= 256 || p.lda > kMaxLd || p.ldb > kMaxLd)
+    return p.K >= 4096 ? launch_direct<8, FA, FB>(s, p, exact) : launch_direct<4, FA, FB>(s, p, exact);
+  if (tiles(Few::BM, Few::BN) <= 256) return exact ? launch<Few, FA, FB, true>(s, p) : launch<Few, FA, FB, false>(s, p);
+  if (tiles(Split::BM, Split::BN) <= 256) return exact ? launch<Split, FA, FB, true>(s, p) : launch<Split, FA, FB, false>(s, p);
+  if (tiles(Half::BM, Half::BN) <= 256) return exact ? launch<Half, FA, FB, true>(s, p) : launch<Half, FA, FB, false>(s, p);
   if (exact) return launch<Mid, FA, FB, true>(s, p);
-  if (tiles(256, 256) >= 150) return launch<Big, FA, FB, false>(s, p);
-  return launch<Mid, FA, FB, false>(s, p);
+  const int64_t big = tiles(Big::BM, Big::BN), slots = (big + 255) / 256 * 256;
+  if (big <= 256 ? big >= 144 : 100 * big > 78 * slots) return launch<Big, FA, FB, false>(s, p);
+  return tiles(Mid::BM, Mid::BN) <= 256 ? launch<MidOne, FA, FB, false>(s, p) : launch<Mid, FA, FB, false>(s, p);
 }
 
 }  // namespace

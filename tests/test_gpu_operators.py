@@ -260,6 +260,19 @@ def test_f8_product_many_tiles(ctx, M, N, K, kw):
     product(ctx, M, N, K, seed=2, **kw)
 
 
+@pytest.mark.parametrize("bf16,fa,fb", [(True, "e4m3", "e4m3"), (True, "e5m2", "e4m3"), (False, "e4m3", "e5m2")])
+@pytest.mark.parametrize("K", [16, 128, 240, 400, 1040])
+@pytest.mark.parametrize("M,N", [(3, 5000), (260, 300), (500, 1300), (1300, 1100), (1700, 1900), (2100, 2600)])
+def test_f8_product_every_tile_and_depth(ctx, M, N, K, bf16, fa, fb):
+    """A size for each tile, none of them whole, with one to nine k tiles, the last of them partial or not."""
+    product(ctx, M, N, K, fa, fb, bf16=bf16, epilogue=pwb.PW_EPI_BIAS, seed=K, block=128)
+
+
+@pytest.mark.parametrize("K", [16, 256, 272, 528])
+def test_f8_product_largest_tile_and_depth(ctx, K):
+    product(ctx, 3000, 3100, K, bf16=True, seed=K)
+
+
 def test_f8_product_of_rows_far_apart(ctx):
     product(ctx, 3, 40, 144, lda=(1 << 23) + 16, bf16=True)
     product(ctx, 40, 3, 144, ldb=(1 << 23) + 16)
