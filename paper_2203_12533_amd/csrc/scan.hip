@@ -7,18 +7,18 @@
 //   g_t = dy_t + r_(t+1),  dx_t = g_t (1 - a_t),  df_t = g_t (h_(t-1) - x_t) a_t (1 - a_t),  dh_0 = r_1.
 //
 // A step is the map h -> a h + v, and maps compose: (P, S) after (p, s) is (P p, P s + S).  A thread takes 8 consecutive
-// steps of its channels into registers and composes them, the waves of a block hand their maps over through LDS, and every
-// thread then runs its steps again from the state in front of them: inputs are read once, nothing but outputs is written.
-// A block of up to 16 waves has 64 channels (two to a lane, so that a row is 128 or 256 bytes) and a tile of 16 steps per
-// wave; it walks down its tiles with the state in registers.  The forward pass keeps the state in front of each tile
-// (fp32, one value per channel and tile); the backward pass starts every tile from it and walks upwards.
+// steps of its four channels into registers and composes them, the quarters of a wave exchange their maps, the waves of a block
+// hand theirs over through LDS, and every thread then runs its steps again from the state in front of them: inputs are
+// read once, nothing but outputs is written.  A block of up to 8 waves has 64 channels (16 lanes of four, so that a row is
+// 128 or 256 bytes) and a tile of 32 steps per wave; it walks down its tiles with the state in registers, the next tile on its
+// way.  The forward pass keeps the state in front of each tile (fp32, one value per channel and tile); the backward pass
+// starts every tile from it and walks upwards.
 //
 // Few channels leave compute units idle.  The sequence is then cut into segments of whole tiles: a first launch composes
 // each segment into one map, the second composes the maps in front of its segment (behind it, backward) and goes on as above.
 //
 // Steps behind the end of a sequence (lens) are the identity map with outputs of zero; their inputs are not read.
 // Sums, states and gates are fp32; y, df and dx are rounded once.  All orders are fixed: the same bits on every run.
-#include <initializer_list>
 #include <type_traits>
 
 #include "common.hpp"
@@ -29,15 +29,24 @@ namespace pw {
 namespace {
 
 constexpr int kSteps = 8;          // consecutive steps of a thread
-constexpr int kMostWaves = 16;
-constexpr int kLanes = 32;         // lanes side by side along the channels; the wave's other half has the next 8 steps
+constexpr int kVec = 2;            // channels of a thread
+constexpr int kLanes = 16;         // lanes side by side along the channels; a wave's parts follow one another in time
+constexpr int kParts = kWave / kLanes, kLevels = 2;
+static_assert(1 << kLevels == kParts, "parts meet in pairs");
+constexpr int kWaveSteps = kSteps * kParts;
+constexpr int kMostWaves = 8;
+constexpr int kChannels = kVec * kLanes;
+constexpr int64_t kMostLd = 1 << 21;     // a tile's rows are within 32 bits of offset
+// Blocks next to each other in memory share a cache line where a row of theirs is 64 bytes: they start on the same XCD then (ids
+// go round the eight of them).
+constexpr bool kSwap = kChannels < 64;
 
 int waves_of(int T) {
-  const int w = (T + 2 * kSteps - 1) / (2 * kSteps);
+  const int w = (int)(((int64_t)T + kWaveSteps - 1) / kWaveSteps);
   return w < 1 ? 1 : (w > kMostWaves ? kMostWaves : w);
 }
-int tile_of(int T) { return waves_of(T) * 2 * kSteps; }
-int tiles_of(int T) { return (T + tile_of(T) - 1) / tile_of(T); }
+int tile_of(int T) { return waves_of(T) * kWaveSteps; }
+int tiles_of(int T) { return (int)(((int64_t)T + tile_of(T) - 1) / tile_of(T)); }
 
 struct Params {
   const void *f, *x, *dy;
@@ -48,53 +57,49 @@ struct Params {
   float2* maps;                          // [B][segments][D]
   const int32_t* lens;
   int T, D, tiles, segments, seg_tiles;
+  int dma;                               // bf16 rows start on four bytes
 };
 
-// Two or one adjacent channels.
-template <class T, int VEC> struct Raw;
-template <> struct Raw<bf16, 2> { typedef bf16x2 type; };
-template <> struct Raw<bf16, 1> { typedef bf16 type; };
-template <> struct Raw<float, 2> { typedef float type __attribute__((ext_vector_type(2))); };
-template <> struct Raw<float, 1> { typedef float type; };
-template <class T, int VEC> __device__ __forceinline__ float lane_of(const typename Raw<T, VEC>::type& r, int j) {
-  if constexpr (VEC == 2) return (float)r[j];
-  else return (float)r;
-}
-template <class T, int VEC> __device__ __forceinline__ void put(T* p, const float* v) {
-  typename Raw<T, VEC>::type r;
-  if constexpr (VEC == 2) {
-    r[0] = (T)v[0];
-    r[1] = (T)v[1];
-  } else {
-    r = (T)v[0];
-  }
-  *reinterpret_cast<typename Raw<T, VEC>::type*>(p) = r;
-}
-
+// Four adjacent channels, wherever they start.
+template <class T> struct Raw;
+template <> struct Raw<bf16> { typedef __bf16 type __attribute__((ext_vector_type(kVec), aligned(2))); };
+template <> struct Raw<float> { typedef float type __attribute__((ext_vector_type(kVec), aligned(4))); };
 // a = sigmoid(f) and z = 1 - a, each to full relative precision.
 __device__ __forceinline__ void gate(float f, float& a, float& z) {
-  const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * __builtin_fabsf(f));
-  const float big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
-  a = f >= 0.f ? big : small;
-  z = f >= 0.f ? small : big;
-  if (f != f) a = z = f;
+  const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * f);
+  a = __builtin_amdgcn_rcpf(1.f + e);
+  z = e > 1.f ? 1.f - a : e * a;               // e may be infinite, or NaN with f
+}
+// The same in one register: the smaller of the two, negative where that is a.  The other one is 1 minus it, to half a unit.
+__device__ __forceinline__ float packed_gate(float f) {
+  const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * f), a = __builtin_amdgcn_rcpf(1.f + e);
+  return e > 1.f ? -a : e * a;
+}
+__device__ __forceinline__ void unpack_gate(float g, float& a, float& z) {
+  const float other = 1.f - __builtin_fabsf(g);
+  const bool of_a = (int)__float_as_uint(g) < 0;                  // -0 is an a of zero
+  a = of_a ? -g : other;
+  z = of_a ? other : g;
 }
 
 struct Where {
   int64_t b;
-  int c, sub, wave, half, li, nw, len;
-  bool on;                               // the lane has channels
+  int c, n, sub, wave, part, li, nw, len;        // n: channels of the lane that exist
+  bool whole;                                    // every lane of the block has all of its channels
 };
-template <int VEC> __device__ __forceinline__ Where where(const Params& p) {
+__device__ __forceinline__ Where where(const Params& p) {
   Where w;
   w.b = blockIdx.y;
   w.wave = threadIdx.x >> 6;
-  w.half = (threadIdx.x >> 5) & 1;
-  w.li = threadIdx.x & (kLanes - 1);
-  w.sub = 2 * w.wave + w.half;
+  w.part = (threadIdx.x / kLanes) % kParts;
+  w.li = threadIdx.x % kLanes;
+  w.sub = kParts * w.wave + w.part;
   w.nw = blockDim.x >> 6;
-  w.c = (blockIdx.x * kLanes + w.li) * VEC;
-  w.on = w.c < p.D;
+  int g = blockIdx.x;
+  if (kSwap && g < (int)(gridDim.x & ~15u)) g = (g & ~15) | ((g & 7) << 1) | ((g >> 3) & 1);
+  w.c = (g * kLanes + w.li) * kVec;
+  w.n = p.D - w.c < 0 ? 0 : (p.D - w.c < kVec ? p.D - w.c : kVec);
+  w.whole = (g + 1) * kChannels <= p.D;
   w.len = p.T;
   if (p.lens) {
     const int l = p.lens[w.b];
@@ -103,315 +108,462 @@ template <int VEC> __device__ __forceinline__ Where where(const Params& p) {
   return w;
 }
 
-// The eight steps from t0 on of an array's channels.  Steps that do not exist come out as zeros: what is fetched in their
-// place is the sequence's last row (or its first place in memory, where it has no step) and is not looked at.
-template <class T, int VEC>
-__device__ __forceinline__ void fetch(const void* base, int64_t ld, const Where& w, const Params& p, int t0,
-                                      typename Raw<T, VEC>::type (&r)[kSteps]) {
-  typedef typename Raw<T, VEC>::type raw;
-  const T* const q = reinterpret_cast<const T*>(base) + w.b * p.T * ld + (w.on ? w.c : 0);
-  const int end = t0 - w.sub * kSteps + w.nw * 2 * kSteps;      // of the block's tile
-  if (end <= w.len) {
+// One array seen by a thread: its eight steps of a tile are rows of `ld` elements behind a wave-uniform base, at an offset
+// that stays the same from tile to tile (32 bits hold it: kMostLd).
+template <class T>
+struct Column {
+  const char* base;                              // row 0 of the sequence
+  int64_t row;                                   // bytes
+  uint32_t off;
+  __device__ __forceinline__ Column(const void* p, int64_t ld, const Where& w, int T_)
+      : base(reinterpret_cast<const char*>(p) + w.b * T_ * ld * (int64_t)sizeof(T)), row(ld * (int64_t)sizeof(T)),
+        off((uint32_t)(w.sub * kSteps) * (uint32_t)row + (uint32_t)w.c * (uint32_t)sizeof(T)) {}
+  __device__ __forceinline__ const char* at(int tile0, int i) const { return base + (tile0 + i) * row + off; }
+};
+// The steps of the tile that begins at step tile0.  WHOLE: all steps and channels exist; else those that do not come out as zeros
+// (fetched in their place is the sequence's last row, or its first place in memory where it has no step).
+template <class T, bool WHOLE>
+__device__ __forceinline__ void fetch(const Column<T>& q, const Where& w, int tile0, typename Raw<T>::type (&r)[kSteps]) {
+  typedef typename Raw<T>::type raw;
+  if constexpr (WHOLE) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) r[i] = *reinterpret_cast<const raw*>(q + (t0 + i) * ld);
+    for (int i = 0; i < kSteps; ++i) r[i] = *reinterpret_cast<const raw*>(q.at(tile0, i));
   } else {
     const int top = w.len > 0 ? w.len - 1 : 0;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      const raw v = *reinterpret_cast<const raw*>(q + (t0 + i < top ? t0 + i : top) * ld);
-      r[i] = t0 + i < w.len ? v : raw{};
+      const int t = tile0 + w.sub * kSteps + i;
+      const T* const g = reinterpret_cast<const T*>(q.base + (t < top ? t : top) * q.row) + w.c;
+      r[i] = raw{};
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        if (j < w.n) {
+          const T v = g[j];
+          r[i][j] = t < w.len ? v : (T)0.f;
+        }
     }
   }
 }
-
-// Maps of the waves of a block, one array per composed quantity.
-template <int VEC> struct Maps { float p[VEC], s[VEC]; };
-
-template <int VEC>
-__device__ __forceinline__ Maps<VEC> other_half(const Maps<VEC>& m) {
-  Maps<VEC> o;
+template <class T, bool WHOLE>
+__device__ __forceinline__ void put(const Column<T>& q, const Where& w, int tile0, int T_, int i, const float* v) {
+  if constexpr (WHOLE) {
+    typename Raw<T>::type r;
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) {
-    o.p[j] = __shfl_xor(m.p[j], 32, 64);
-    o.s[j] = __shfl_xor(m.s[j], 32, 64);
+    for (int j = 0; j < kVec; ++j) r[j] = (T)v[j];
+    *reinterpret_cast<typename Raw<T>::type*>(const_cast<char*>(q.at(tile0, i))) = r;
+  } else if (tile0 + w.sub * kSteps + i < T_) {
+    T* const g = reinterpret_cast<T*>(const_cast<char*>(q.at(tile0, i)));
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (j < w.n) g[j] = (T)v[j];
+  }
+}
+
+// Maps of a stretch of steps: of the state walking down (DIRS & 1) and of r walking up (DIRS & 2); both have the same product.
+enum { kDown = 1, kUp = 2 };
+template <int DIRS> struct Map { float p[kVec], s[DIRS == 3 ? 2 : 1][kVec]; };
+template <int DIRS, int D> constexpr int sum_of() { return DIRS == 3 && D == kUp ? 1 : 0; }
+
+template <int DIRS> __device__ __forceinline__ Map<DIRS> exchanged(const Map<DIRS>& m, int lanes) {
+  Map<DIRS> o;
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) {
+    o.p[j] = __shfl_xor(m.p[j], lanes, kWave);
+#pragma unroll
+    for (int d = 0; d < (DIRS == 3 ? 2 : 1); ++d) o.s[d][j] = __shfl_xor(m.s[d][j], lanes, kWave);
   }
   return o;
 }
-
-// carry: the state in front of the block's tile (FORWARD) or handed in from behind it; replaced by the one on the other
-// side.  in: what reaches this thread's eight steps.  mine: the map of those.  slot: LDS of this tile, [waves][lanes].
-template <int VEC, bool FORWARD>
-__device__ __forceinline__ void compose(Maps<VEC>* slot, const Where& w, const Maps<VEC>& mine, float (&carry)[VEC], float (&in)[VEC]) {
-  const Maps<VEC> other = other_half(mine);
-  const bool first = FORWARD ? w.half == 0 : w.half == 1;      // the half that the state reaches first
-  Maps<VEC> both;
+template <int DIRS, int D> __device__ __forceinline__ void apply(const Map<DIRS>& m, float (&h)[kVec]) {
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) {
-    both.p[j] = mine.p[j] * other.p[j];
-    both.s[j] = first ? __builtin_fmaf(other.p[j], mine.s[j], other.s[j]) : __builtin_fmaf(mine.p[j], other.s[j], mine.s[j]);
-  }
-  if (w.half == 0) slot[w.wave * kLanes + w.li] = both;
-  __syncthreads();
-  float h[VEC], at[VEC];
+  for (int j = 0; j < kVec; ++j) h[j] = __builtin_fmaf(m.p[j], h[j], m.s[sum_of<DIRS, D>()][j]);
+}
+// The map of two neighbouring stretches, `mine` the earlier one or not.
+template <int DIRS> __device__ __forceinline__ Map<DIRS> joined(const Map<DIRS>& mine, const Map<DIRS>& other, bool earlier) {
+  Map<DIRS> r;
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) at[j] = h[j] = carry[j];
-  for (int i = 0; i < w.nw; ++i) {
-    const int k = FORWARD ? i : w.nw - 1 - i;
-    const Maps<VEC> m = slot[k * kLanes + w.li];
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      if (k == w.wave) at[j] = h[j];
-      h[j] = __builtin_fmaf(m.p[j], h[j], m.s[j]);
+  for (int j = 0; j < kVec; ++j) {
+    r.p[j] = mine.p[j] * other.p[j];
+    auto after = [&](float first, float p, float s) { return __builtin_fmaf(p, first, s); };
+    if (DIRS & kDown) {
+      constexpr int d = sum_of<DIRS, kDown>();
+      r.s[d][j] = earlier ? after(mine.s[d][j], other.p[j], other.s[d][j]) : after(other.s[d][j], mine.p[j], mine.s[d][j]);
+    }
+    if (DIRS & kUp) {
+      constexpr int d = sum_of<DIRS, kUp>();
+      r.s[d][j] = earlier ? after(other.s[d][j], mine.p[j], mine.s[d][j]) : after(mine.s[d][j], other.p[j], other.s[d][j]);
     }
   }
+  return r;
+}
+
+// down: the state in front of the block's tile, up: the r handed in from behind it; each is replaced by the one on the other
+// side.  in_down, in_up: what reaches this thread's steps, whose map is `mine`.  slot: LDS of this tile, [waves][lanes].
+template <int DIRS>
+__device__ __forceinline__ void compose(Map<DIRS>* slot, const Where& w, const Map<DIRS>& mine, float (&down)[kVec], float (&in_down)[kVec],
+                                        float (&up)[kVec], float (&in_up)[kVec]) {
+  Map<DIRS> others[kLevels], all = mine;
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) {
-    carry[j] = h[j];
-    in[j] = first ? at[j] : __builtin_fmaf(other.p[j], at[j], other.s[j]);
+  for (int l = 0; l < kLevels; ++l) {
+    others[l] = exchanged(all, kLanes << l);
+    all = joined(all, others[l], ((w.part >> l) & 1) == 0);
+  }
+  if (w.part == 0) slot[w.wave * kLanes + w.li] = all;
+  // What the waves exchange is in LDS: loads and stores of other data stay on their way.
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  const int wave = __builtin_amdgcn_readfirstlane(w.wave);
+  const Map<DIRS>* const at = slot + w.li;
+  if (DIRS & kDown) {
+    for (int k = 0; k < wave; ++k) apply<DIRS, kDown>(at[k * kLanes], down);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) in_down[j] = down[j];
+    for (int k = wave; k < w.nw; ++k) apply<DIRS, kDown>(at[k * kLanes], down);
+#pragma unroll
+    for (int l = kLevels - 1; l >= 0; --l)
+      if ((w.part >> l) & 1) apply<DIRS, kDown>(others[l], in_down);
+  }
+  if (DIRS & kUp) {
+    for (int k = w.nw - 1; k > wave; --k) apply<DIRS, kUp>(at[k * kLanes], up);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) in_up[j] = up[j];
+    for (int k = wave; k >= 0; --k) apply<DIRS, kUp>(at[k * kLanes], up);
+#pragma unroll
+    for (int l = kLevels - 1; l >= 0; --l)
+      if (!((w.part >> l) & 1)) apply<DIRS, kUp>(others[l], in_up);
   }
 }
 
-// What reaches segment `seg`: the maps of the slots 0 .. seg (FORWARD) or segments - 1 .. seg, the first of which is a
-// constant.  Each wave composes a stretch of them, then the waves meet as they do in a tile.
-template <int VEC, bool FORWARD>
-__device__ __forceinline__ void segment_carry(Maps<VEC>* slot, const Where& w, const Params& p, int seg, float (&carry)[VEC]) {
-  const int n = FORWARD ? seg + 1 : p.segments - seg, per = (n + 2 * w.nw - 1) / (2 * w.nw);
-  Maps<VEC> m;
+// What reaches segment `seg`: the maps of the slots 0 .. seg (down) or segments - 1 .. seg (up), the first of which is a
+// constant.  Each part of a wave composes a stretch of them, then they meet as they do in a tile.
+template <int D>
+__device__ __forceinline__ void segment_carry(Map<D>* slot, const Where& w, const Params& p, int seg, float (&carry)[kVec]) {
+  const int subs = kParts * w.nw, n = D == kDown ? seg + 1 : p.segments - seg, per = (n + subs - 1) / subs;
+  Map<D> m;
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) {
+  for (int j = 0; j < kVec; ++j) {
     m.p[j] = 1.f;
-    m.s[j] = 0.f;
+    m.s[0][j] = 0.f;
     carry[j] = 0.f;
   }
   for (int i = 0; i < per; ++i) {
-    const int k = FORWARD ? w.sub * per + i : n - 1 - ((2 * w.nw - 1 - w.sub) * per + i);
-    const bool there = FORWARD ? k < n : k >= 0;
-    if (w.on && there) {
-      const float2* q = p.maps + (w.b * p.segments + (FORWARD ? k : seg + k)) * p.D + w.c;
+    const int k = D == kDown ? w.sub * per + i : n - 1 - ((subs - 1 - w.sub) * per + i);
+    if (D == kDown ? k < n : k >= 0) {
+      const float2* q = p.maps + (w.b * p.segments + (D == kDown ? k : seg + k)) * p.D + w.c;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float2 v = q[j];
-        m.s[j] = __builtin_fmaf(v.x, m.s[j], v.y);
-        m.p[j] *= v.x;
+      for (int j = 0; j < kVec; ++j) {
+        if (j < w.n) {
+          const float2 v = q[j];
+          m.s[0][j] = __builtin_fmaf(v.x, m.s[0][j], v.y);
+          m.p[j] *= v.x;
+        }
       }
     }
   }
-  float in[VEC];
-  compose<VEC, FORWARD>(slot, w, m, carry, in);
+  float in[kVec], none[kVec] = {}, none2[kVec];
+  if constexpr (D == kDown) compose<D>(slot, w, m, carry, in, none, none2);
+  else compose<D>(slot, w, m, none, none2, carry, in);
 }
 
-template <class T, int VEC>
-__device__ __forceinline__ void gates(const typename Raw<T, VEC>::type (&rf)[kSteps], const Where& w, int t0, float (&a)[kSteps][VEC],
-                                      float (&z)[kSteps][VEC]) {
+// The next tile of N bf16 arrays on its way into LDS, without registers: a wave fetches the steps its own threads will take,
+// 256 bytes at a time, and a lane finds its two channels of step i of array n at [n][i][lane].
+template <int N> struct Ahead {
+  typedef __attribute__((address_space(3))) void* lds_ptr;
+  uint32_t (*mine)[kSteps][kWave];               // this wave's part
+  uint32_t at;                                   // its offset in LDS
+  __device__ __forceinline__ Ahead(uint32_t (*lds)[N][kSteps][kWave], const Where& w) {
+    mine = lds[w.wave];
+    at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)mine);
+  }
+  __device__ __forceinline__ void ask(int n, const Column<bf16>& q, int tile0) const {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(q.off), "s"(q.base + (tile0 + i) * q.row),
+                   "s"(at + (n * kSteps + i) * (kWave * 4)) : "memory", "m0");
+  }
+  __device__ __forceinline__ void take(int n, Raw<bf16>::type (&r)[kSteps]) const {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) r[i] = __builtin_bit_cast(bf16x2, mine[n][i][threadIdx.x & 63]);
+  }
+  // Between take() of one tile and ask() for the next: what was read is in registers.
+  __device__ __forceinline__ static void taken() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+  // In front of the tile's stores, behind which this would wait for those.
+  __device__ __forceinline__ static void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+};
+template <class T, bool WHOLE>
+__device__ __forceinline__ void gates(const typename Raw<T>::type (&rf)[kSteps], const Where& w, int tile0, float (&a)[kSteps][kVec],
+                                      float (&z)[kSteps][kVec]) {
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      gate(lane_of<T, VEC>(rf[i], j), a[i][j], z[i][j]);
-      if (t0 + i >= w.len) {
+    for (int j = 0; j < kVec; ++j) {
+      gate((float)rf[i][j], a[i][j], z[i][j]);
+      if (!WHOLE && tile0 + w.sub * kSteps + i >= w.len) {
         a[i][j] = 1.f;
         z[i][j] = 0.f;
       }
     }
 }
+template <class T, bool WHOLE>
+__device__ __forceinline__ void packed_gates(const typename Raw<T>::type (&rf)[kSteps], const Where& w, int tile0, float (&g)[kSteps][kVec]) {
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      g[i][j] = packed_gate((float)rf[i][j]);
+      if (!WHOLE && tile0 + w.sub * kSteps + i >= w.len) g[i][j] = 0.f;      // a = 1
+    }
+}
+// One value per channel of a [B, .., D] array of floats.
+__device__ __forceinline__ void get_row(const float* p, const Where& w, float (&v)[kVec]) {
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) v[j] = j < w.n ? p[w.c + j] : 0.f;
+}
+__device__ __forceinline__ void put_row(float* p, const Where& w, const float (&v)[kVec]) {
+#pragma unroll
+  for (int j = 0; j < kVec; ++j)
+    if (j < w.n) p[w.c + j] = v[j];
+}
 
 // SUMMARY: only the map of the block's segment, into slot seg + 1.
-template <class T, int VEC, bool SUMMARY>
-__global__ __launch_bounds__(64 * kMostWaves) void scan_fwd_kernel(Params p) {
-  __shared__ __attribute__((aligned(16))) Maps<VEC> slots[2][kMostWaves * kLanes];
-  const Where w = where<VEC>(p);
-  const int seg = blockIdx.z, tile = w.nw * 2 * kSteps;
+template <class T, bool SUMMARY>
+__global__ __launch_bounds__(64 * kMostWaves, 4) void scan_fwd_kernel(Params p) {
+  constexpr bool DMA = sizeof(T) == 2;
+  __shared__ __attribute__((aligned(16))) Map<kDown> slots[2][kMostWaves * kLanes];
+  __shared__ __attribute__((aligned(16))) uint32_t next[DMA ? kMostWaves : 1][2][kSteps][kWave];
+  typedef typename Raw<T>::type raw;
+  const Where w = where(p);
+  const int seg = blockIdx.z, tile = w.nw * kWaveSteps;
   const int first = seg * p.seg_tiles, last = first + p.seg_tiles < p.tiles ? first + p.seg_tiles : p.tiles;
-  float h[VEC] = {}, in[VEC], prod[VEC];
+  float h[kVec] = {}, prod[kVec], up[kVec] = {}, in_up[kVec];
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) prod[j] = 1.f;
-  if (SUMMARY || p.segments == 1) {
-    if (p.h0 && seg == 0 && w.on) {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) h[j] = p.h0[w.b * p.D + w.c + j];
+  for (int j = 0; j < kVec; ++j) prod[j] = 1.f;
+  float2* const maps = p.maps + w.b * p.segments * p.D + w.c;
+  const Column<T> qf(p.f, p.ldf, w, p.T), qx(p.x, p.ldx, w, p.T), qy(p.y, p.ldy, w, p.T);
+  const Ahead<2> ahead(next, w);
+  auto all_of = [&](int k) { return w.whole && (k + 1) * tile <= w.len; };      // wave-uniform
+  auto ask = [&](int k) {
+    if constexpr (DMA) {
+      if (p.dma && all_of(k)) {
+        ahead.ask(0, qf, k * tile);
+        ahead.ask(1, qx, k * tile);
+      }
     }
-    if (SUMMARY && seg == 0 && w.on && w.sub == 0) {
+  };
+  if (first < last) ask(first);          // a sequence of no steps hands its state through
+  if (SUMMARY || p.segments == 1) {
+    if (p.h0 && seg == 0) get_row(p.h0 + w.b * p.D, w, h);
+    if (SUMMARY && seg == 0 && w.sub == 0) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) p.maps[w.b * p.segments * p.D + w.c + j] = make_float2(0.f, h[j]);
+      for (int j = 0; j < kVec; ++j)
+        if (j < w.n) maps[j] = make_float2(0.f, h[j]);
     }
   } else {
-    segment_carry<VEC, true>(slots[1], w, p, seg, h);
+    segment_carry<kDown>(slots[1], w, p, seg, h);
   }
-  int t0 = first * tile + w.sub * kSteps, parity = 0;
-  typename Raw<T, VEC>::type rf[kSteps], rx[kSteps];
-  if (first < last) {                    // a sequence of no steps hands its state through
-    fetch<T, VEC>(p.f, p.ldf, w, p, t0, rf);
-    fetch<T, VEC>(p.x, p.ldx, w, p, t0, rx);
-  }
-  for (int k = first; k < last; ++k, t0 += tile, parity ^= 1) {
-    float a[kSteps][VEC], v[kSteps][VEC];
-    gates<T, VEC>(rf, w, t0, a, v);
-    Maps<VEC> m;
+  if (DMA) ahead.landed();
+  auto step = [&](int k, auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    Map<kDown>* const slot = slots[(k - first) & 1];
+    raw rf[kSteps], rx[kSteps];
+    if (DMA && WHOLE && p.dma) {
+      if constexpr (DMA) {
+        ahead.take(0, rf);
+        ahead.take(1, rx);
+        ahead.taken();
+      }
+    } else {
+      fetch<T, WHOLE>(qf, w, k * tile, rf);
+      fetch<T, WHOLE>(qx, w, k * tile, rx);
+    }
+    if (k + 1 < last) ask(k + 1);
+    float a[kSteps][kVec], v[kSteps][kVec], in[kVec];
+    gates<T, WHOLE>(rf, w, k * tile, a, v);
+    Map<kDown> m;
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
+    for (int j = 0; j < kVec; ++j) {
       m.p[j] = 1.f;
-      m.s[j] = 0.f;
+      m.s[0][j] = 0.f;
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        v[i][j] *= lane_of<T, VEC>(rx[i], j);
-        m.s[j] = __builtin_fmaf(a[i][j], m.s[j], v[i][j]);
+        v[i][j] *= (float)rx[i][j];
+        m.s[0][j] = __builtin_fmaf(a[i][j], m.s[0][j], v[i][j]);
         m.p[j] *= a[i][j];
       }
     }
-    if (k + 1 < last) {
-      fetch<T, VEC>(p.f, p.ldf, w, p, t0 + tile, rf);
-      fetch<T, VEC>(p.x, p.ldx, w, p, t0 + tile, rx);
-    }
-    if (!SUMMARY && p.states && w.on && w.sub == 0) {
+    float before[kVec];
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) p.states[(w.b * p.tiles + k) * p.D + w.c + j] = h[j];
-    }
-    compose<VEC, true>(slots[parity], w, m, h, in);
+    for (int j = 0; j < kVec; ++j) before[j] = h[j];
+    compose<kDown>(slot, w, m, h, in, up, in_up);
+    if (DMA) ahead.landed();
+    if (!SUMMARY && p.states && w.sub == 0) put_row(p.states + (w.b * p.tiles + k) * p.D, w, before);
     if constexpr (SUMMARY) {
-      // the product over the tile: composed once more with a state of one and sums of zero
-      Maps<VEC>* slot = slots[parity];
       for (int i = 0; i < w.nw; ++i)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) prod[j] *= slot[i * kLanes + w.li].p[j];
-    } else if (w.on) {
-      T* const y = reinterpret_cast<T*>(p.y) + (w.b * p.T + t0) * p.ldy + w.c;
+        for (int j = 0; j < kVec; ++j) prod[j] *= slot[i * kLanes + w.li].p[j];
+    } else {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        float o[VEC];
+        float o[kVec];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
+        for (int j = 0; j < kVec; ++j) {
           in[j] = __builtin_fmaf(a[i][j], in[j], v[i][j]);
-          o[j] = t0 + i < w.len ? in[j] : 0.f;
+          o[j] = WHOLE || k * tile + w.sub * kSteps + i < w.len ? in[j] : 0.f;
         }
-        if (t0 + i < p.T) put<T, VEC>(y + i * p.ldy, o);
+        put<T, WHOLE>(qy, w, k * tile, p.T, i, o);
       }
     }
+  };
+  for (int k = first; k < last; ++k) {
+    if (all_of(k)) step(k, std::true_type{});
+    else step(k, std::false_type{});
   }
-  if (w.on && w.sub == 0) {
+  if (w.sub == 0) {
+    if constexpr (SUMMARY) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      if (SUMMARY) p.maps[(w.b * p.segments + seg + 1) * p.D + w.c + j] = make_float2(seg == 0 ? 0.f : prod[j], h[j]);
-      else if (p.h_end && seg == p.segments - 1) p.h_end[w.b * p.D + w.c + j] = h[j];
+      for (int j = 0; j < kVec; ++j)
+        if (j < w.n) maps[(int64_t)(seg + 1) * p.D + j] = make_float2(seg == 0 ? 0.f : prod[j], h[j]);
+    } else if (p.h_end && seg == p.segments - 1) {
+      put_row(p.h_end + w.b * p.D, w, h);
     }
   }
 }
 
 // SUMMARY: the map of r over the block's segment seg + 1, into slot seg (the last slot holds dh_end).
-template <class T, int VEC, bool SUMMARY>
-__global__ __launch_bounds__(64 * kMostWaves) void scan_bwd_kernel(Params p) {
-  __shared__ __attribute__((aligned(16))) Maps<VEC> slots[2][2][kMostWaves * kLanes];   // [parity][backward, forward]
-  const Where w = where<VEC>(p);
-  const int seg = SUMMARY ? blockIdx.z + 1 : blockIdx.z, tile = w.nw * 2 * kSteps;
+template <class T, bool SUMMARY>
+__global__ __launch_bounds__(64 * kMostWaves, 4) void scan_bwd_kernel(Params p) {
+  constexpr bool DMA = sizeof(T) == 2;
+  constexpr int DIRS = SUMMARY ? kUp : kUp | kDown, N = SUMMARY ? 2 : 3;
+  __shared__ __attribute__((aligned(16))) Map<DIRS> slots[2][kMostWaves * kLanes];
+  __shared__ __attribute__((aligned(16))) uint32_t next[DMA ? kMostWaves : 1][N][kSteps][kWave];
+  typedef typename Raw<T>::type raw;
+  const Where w = where(p);
+  const int seg = SUMMARY ? blockIdx.z + 1 : blockIdx.z, tile = w.nw * kWaveSteps;
   const int first = seg * p.seg_tiles, last = first + p.seg_tiles < p.tiles ? first + p.seg_tiles : p.tiles;
   const bool behind = seg == p.segments - 1;
-  float r[VEC] = {}, in[VEC], prod[VEC];
+  float r[kVec] = {}, prod[kVec];
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) prod[j] = 1.f;
-  if (SUMMARY || p.segments == 1) {
-    if (p.dh_end && behind && w.on) {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) r[j] = p.dh_end[w.b * p.D + w.c + j];
+  for (int j = 0; j < kVec; ++j) prod[j] = 1.f;
+  float2* const maps = p.maps + w.b * p.segments * p.D + w.c;
+  const Column<T> qf(p.f, p.ldf, w, p.T), qx(p.x, p.ldx, w, p.T), qd(p.dy, p.ldy, w, p.T), of(p.df, p.lddf, w, p.T), ox(p.dx, p.lddx, w, p.T);
+  const Ahead<N> ahead(next, w);
+  auto all_of = [&](int k) { return w.whole && (k + 1) * tile <= w.len; };      // wave-uniform
+  auto ask = [&](int k) {
+    if constexpr (DMA) {
+      if (p.dma && all_of(k)) {
+        ahead.ask(0, qf, k * tile);
+        ahead.ask(1, qd, k * tile);
+        if constexpr (!SUMMARY) ahead.ask(2, qx, k * tile);
+      }
     }
-    if (SUMMARY && behind && w.on && w.sub == 0) {
+  };
+  if (first < last) ask(last - 1);
+  if (SUMMARY || p.segments == 1) {
+    if (p.dh_end && behind) get_row(p.dh_end + w.b * p.D, w, r);
+    if (SUMMARY && behind && w.sub == 0) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) p.maps[(w.b * p.segments + seg) * p.D + w.c + j] = make_float2(0.f, r[j]);
+      for (int j = 0; j < kVec; ++j)
+        if (j < w.n) maps[(int64_t)seg * p.D + j] = make_float2(0.f, r[j]);
     }
   } else {
-    segment_carry<VEC, false>(slots[1][0], w, p, seg, r);
+    segment_carry<kUp>(reinterpret_cast<Map<kUp>*>(slots[1]), w, p, seg, r);
   }
-  int t0 = (last - 1) * tile + w.sub * kSteps, parity = 0;
-  typename Raw<T, VEC>::type rf[kSteps], rx[kSteps], rd[kSteps];
-  for (int k = last - 1; k >= first; --k, t0 -= tile, parity ^= 1) {
-    fetch<T, VEC>(p.f, p.ldf, w, p, t0, rf);
-    fetch<T, VEC>(p.dy, p.ldy, w, p, t0, rd);
-    float a[kSteps][VEC], z[kSteps][VEC];
-    Maps<VEC> m;
-    if constexpr (SUMMARY) {
-      gates<T, VEC>(rf, w, t0, a, z);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        m.p[j] = 1.f;
-        m.s[j] = 0.f;
-#pragma unroll
-        for (int i = kSteps - 1; i >= 0; --i) {
-          m.s[j] = a[i][j] * (lane_of<T, VEC>(rd[i], j) + m.s[j]);
-          m.p[j] *= a[i][j];
-        }
+  if (DMA) ahead.landed();
+  auto step = [&](int k, auto all) {
+    constexpr bool WHOLE = decltype(all)::value;
+    raw rf[kSteps], rx[kSteps], rd[kSteps];
+    float h[kVec] = {}, g[kSteps][kVec], in[kVec], hin[kVec];
+    if (!SUMMARY) get_row(p.states + (w.b * p.tiles + k) * p.D, w, h);
+    if (DMA && WHOLE && p.dma) {
+      if constexpr (DMA) {
+        ahead.take(0, rf);
+        ahead.take(1, rd);
+        if constexpr (!SUMMARY) ahead.take(2, rx);
+        ahead.taken();
       }
-      compose<VEC, false>(slots[parity][0], w, m, r, in);
-      for (int i = 0; i < w.nw; ++i)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) prod[j] *= slots[parity][0][i * kLanes + w.li].p[j];
     } else {
-      fetch<T, VEC>(p.x, p.ldx, w, p, t0, rx);
-      float h[VEC] = {};
-      if (w.on) {
+      fetch<T, WHOLE>(qf, w, k * tile, rf);
+      fetch<T, WHOLE>(qd, w, k * tile, rd);
+      if (!SUMMARY) fetch<T, WHOLE>(qx, w, k * tile, rx);
+    }
+    if (k > first) ask(k - 1);
+    packed_gates<T, WHOLE>(rf, w, k * tile, g);
+    Map<DIRS> m;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) h[j] = p.states[(w.b * p.tiles + k) * p.D + w.c + j];
+    for (int j = 0; j < kVec; ++j) {
+      m.p[j] = 1.f;
+      float up = 0.f, down = 0.f, a, z;
+#pragma unroll
+      for (int i = kSteps - 1; i >= 0; --i) {
+        unpack_gate(g[i][j], a, z);
+        up = a * ((float)rd[i][j] + up);
+        m.p[j] *= a;
       }
-      gates<T, VEC>(rf, w, t0, a, z);
-      Maps<VEC> mf;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        m.p[j] = 1.f;
-        m.s[j] = mf.s[j] = 0.f;
+      m.s[sum_of<DIRS, kUp>()][j] = up;
+      if constexpr (!SUMMARY) {
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-          mf.s[j] = __builtin_fmaf(a[i][j], mf.s[j], z[i][j] * lane_of<T, VEC>(rx[i], j));
+          unpack_gate(g[i][j], a, z);
+          down = __builtin_fmaf(a, down, z * (float)rx[i][j]);
         }
-#pragma unroll
-        for (int i = kSteps - 1; i >= 0; --i) {
-          m.s[j] = a[i][j] * (lane_of<T, VEC>(rd[i], j) + m.s[j]);
-          m.p[j] *= a[i][j];
-        }
-        mf.p[j] = m.p[j];
-      }
-      float hin[VEC];
-      compose<VEC, false>(slots[parity][0], w, m, r, in);
-      compose<VEC, true>(slots[parity][1], w, mf, h, hin);
-      if (w.on) {
-        float before[kSteps][VEC];
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            const float xi = lane_of<T, VEC>(rx[i], j);
-            before[i][j] = hin[j] - xi;                       // h_(t-1) - x_t
-            hin[j] = __builtin_fmaf(a[i][j], hin[j], z[i][j] * xi);
-          }
-        T* const df = reinterpret_cast<T*>(p.df) + (w.b * p.T + t0) * p.lddf + w.c;
-        T* const dx = reinterpret_cast<T*>(p.dx) + (w.b * p.T + t0) * p.lddx + w.c;
-#pragma unroll
-        for (int i = kSteps - 1; i >= 0; --i) {
-          float of[VEC], ox[VEC];
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            const float g = lane_of<T, VEC>(rd[i], j) + in[j];
-            const bool there = t0 + i < w.len;
-            ox[j] = there ? g * z[i][j] : 0.f;
-            of[j] = there ? ox[j] * a[i][j] * before[i][j] : 0.f;
-            in[j] = a[i][j] * g;
-          }
-          if (t0 + i < p.T) {
-            put<T, VEC>(df + i * p.lddf, of);
-            put<T, VEC>(dx + i * p.lddx, ox);
-          }
-        }
+        m.s[sum_of<DIRS, kDown>()][j] = down;
       }
     }
-  }
-  if (w.on && w.sub == 0) {
+    // Only what is packed stays in registers while the waves meet.
+    __builtin_amdgcn_sched_barrier(0);
+    Map<DIRS>* const slot = slots[(last - 1 - k) & 1];
+    compose<DIRS>(slot, w, m, h, hin, r, in);
+    if (DMA) ahead.landed();
+    if constexpr (SUMMARY) {
+      for (int i = 0; i < w.nw; ++i)
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      if (SUMMARY) p.maps[(w.b * p.segments + seg - 1) * p.D + w.c + j] = make_float2(behind ? 0.f : prod[j], r[j]);
-      else if (p.dh0 && seg == 0) p.dh0[w.b * p.D + w.c + j] = r[j];
+        for (int j = 0; j < kVec; ++j) prod[j] *= slot[i * kLanes + w.li].p[j];
+    } else {
+      float before[kSteps][kVec], a, z;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+          asm volatile("" : "+v"(g[i][j]));                 // unpacked again here, not kept from above
+          unpack_gate(g[i][j], a, z);
+          const float xi = (float)rx[i][j];
+          before[i][j] = hin[j] - xi;                       // h_(t-1) - x_t
+          hin[j] = __builtin_fmaf(a, hin[j], z * xi);
+        }
+#pragma unroll
+      for (int i = kSteps - 1; i >= 0; --i) {
+        float vf[kVec], vx[kVec];
+        const bool there = WHOLE || k * tile + w.sub * kSteps + i < w.len;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+          unpack_gate(g[i][j], a, z);
+          const float gr = (float)rd[i][j] + in[j];
+          vx[j] = there ? gr * z : 0.f;
+          vf[j] = there ? vx[j] * a * before[i][j] : 0.f;
+          in[j] = a * gr;
+        }
+        put<T, WHOLE>(of, w, k * tile, p.T, i, vf);
+        put<T, WHOLE>(ox, w, k * tile, p.T, i, vx);
+      }
+    }
+  };
+  for (int k = last - 1; k >= first; --k) {
+    if (all_of(k)) step(k, std::true_type{});
+    else step(k, std::false_type{});
+  }
+  if (w.sub == 0) {
+    if constexpr (SUMMARY) {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        if (j < w.n) maps[(int64_t)(seg - 1) * p.D + j] = make_float2(behind ? 0.f : prod[j], r[j]);
+    } else if (p.dh0 && seg == 0) {
+      put_row(p.dh0 + w.b * p.D, w, r);
     }
   }
 }
 
 // How many segments: as many as bring the launch to a block per compute unit, and no more than there are tiles.
 int segments_of(int64_t B, int T, int D) {
-  const int64_t blocks = B * ((D + 2 * kLanes - 1) / (2 * kLanes)), tiles = tiles_of(T);
+  const int64_t blocks = B * ((D + kChannels - 1) / kChannels), tiles = tiles_of(T);
   int64_t n = blocks >= 192 ? 1 : (256 + blocks - 1) / blocks;
   if (n > tiles) n = tiles;
   if (n <= 1) return 1;
@@ -419,11 +571,11 @@ int segments_of(int64_t B, int T, int D) {
   return (int)((tiles + per - 1) / per);
 }
 bool dims_ok(int64_t B, int64_t T, int64_t D) {
-  return B >= 0 && T >= 0 && D >= 0 && B <= 65535 && T <= (1 << 30) && D <= (1 << 24);
+  return B >= 0 && T >= 0 && D >= 0 && B <= 65535 && T <= (1 << 30) && D <= kMostLd;
 }
 bool args_ok(const ScanArgs& a) {
   if (a.dtype != kF32 && a.dtype != kBF16) return false;
-  if (!dims_ok(a.B, a.T, a.D) || !a.f || !a.x || a.ldf < a.D || a.ldx < a.D) return false;
+  if (!dims_ok(a.B, a.T, a.D) || !a.f || !a.x || a.ldf < a.D || a.ldx < a.D || a.ldf > kMostLd || a.ldx > kMostLd) return false;
   const uintptr_t el = a.dtype == kBF16 ? 1 : 3;
   return !(((uintptr_t)a.f | (uintptr_t)a.x) & el) && !(((uintptr_t)a.h0 | (uintptr_t)a.lens) & 3);
 }
@@ -438,15 +590,6 @@ Params params_of(const ScanArgs& a, float* ws) {
   p.maps = reinterpret_cast<float2*>(ws);
   return p;
 }
-// Two channels to a lane where every row starts on a pair.
-template <class T> bool pairs(std::initializer_list<const void*> ptrs, std::initializer_list<int64_t> lds, int D) {
-  uintptr_t bits = 0;
-  for (const void* q : ptrs) bits |= (uintptr_t)q;
-  int64_t odd = D;
-  for (int64_t l : lds) odd |= l;
-  return bits % (2 * sizeof(T)) == 0 && (odd & 1) == 0;
-}
-
 }  // namespace
 
 int64_t scan_state_floats(int64_t B, int64_t T, int64_t D) {
@@ -460,51 +603,45 @@ int64_t scan_ws_floats(int64_t B, int64_t T, int64_t D) {
 }
 
 hipError_t launch_scan_fwd(hipStream_t s, const ScanArgs& a, void* y, int64_t ldy, float* h_end, float* states, float* ws) {
-  if (!args_ok(a) || !y || ldy < a.D || ((uintptr_t)y & (a.dtype == kBF16 ? 1 : 3))) return hipErrorInvalidValue;
+  if (!args_ok(a) || !y || ldy < a.D || ldy > kMostLd || ((uintptr_t)y & (a.dtype == kBF16 ? 1 : 3))) return hipErrorInvalidValue;
   if ((((uintptr_t)h_end | (uintptr_t)states) & 3) || ((uintptr_t)ws & 7)) return hipErrorInvalidValue;
   if (a.B == 0 || a.D == 0) return hipSuccess;
   Params p = params_of(a, ws);
   if (p.segments > 1 && !ws) return hipErrorInvalidValue;
   p.y = y; p.ldy = ldy; p.h_end = h_end; p.states = states;
-  const int threads = 64 * waves_of(a.T);
-  auto go = [&](auto t, auto vec) {
+  p.dma = !(((uintptr_t)a.f | (uintptr_t)a.x) & 3) && !((a.ldf | a.ldx) & 1);
+  const dim3 threads(64 * waves_of(a.T)), grid((a.D + kChannels - 1) / kChannels, a.B, p.segments), summaries(grid.x, a.B, p.segments - 1);
+  auto go = [&](auto t) {
     using T = decltype(t);
-    constexpr int V = decltype(vec)::value;
-    const unsigned groups = (unsigned)((a.D + V * kLanes - 1) / (V * kLanes));
-    if (p.segments > 1) scan_fwd_kernel<T, V, true><<<dim3(groups, a.B, p.segments - 1), threads, 0, s>>>(p);
-    scan_fwd_kernel<T, V, false><<<dim3(groups, a.B, p.segments), threads, 0, s>>>(p);
+    if (p.segments > 1) scan_fwd_kernel<T, true><<<summaries, threads, 0, s>>>(p);
+    scan_fwd_kernel<T, false><<<grid, threads, 0, s>>>(p);
   };
-  using one = std::integral_constant<int, 1>;
-  using two = std::integral_constant<int, 2>;
-  if (a.dtype == kBF16) pairs<bf16>({a.f, a.x, y}, {a.ldf, a.ldx, ldy}, a.D) ? go(bf16{}, two{}) : go(bf16{}, one{});
-  else pairs<float>({a.f, a.x, y}, {a.ldf, a.ldx, ldy}, a.D) ? go(float{}, two{}) : go(float{}, one{});
+  if (a.dtype == kBF16) go(bf16{});
+  else go(float{});
   return hipGetLastError();
 }
 
 hipError_t launch_scan_bwd(hipStream_t s, const ScanArgs& a, const void* dy, int64_t lddy, const float* dh_end, const float* states,
                            void* df, int64_t lddf, void* dx, int64_t lddx, float* dh0, float* ws) {
-  if (!args_ok(a) || !dy || !df || !dx || lddy < a.D || lddf < a.D || lddx < a.D) return hipErrorInvalidValue;
+  if (!args_ok(a) || !dy || !df || !dx || lddy < a.D || lddf < a.D || lddx < a.D || lddy > kMostLd || lddf > kMostLd ||
+      lddx > kMostLd)
+    return hipErrorInvalidValue;
   if (((uintptr_t)dy | (uintptr_t)df | (uintptr_t)dx) & (a.dtype == kBF16 ? 1 : 3)) return hipErrorInvalidValue;
   if ((((uintptr_t)dh_end | (uintptr_t)states | (uintptr_t)dh0) & 3) || ((uintptr_t)ws & 7)) return hipErrorInvalidValue;
   if (a.B == 0 || a.D == 0) return hipSuccess;
   Params p = params_of(a, ws);
   if ((!states && a.T > 0) || (p.segments > 1 && !ws)) return hipErrorInvalidValue;
   p.dy = dy; p.ldy = lddy; p.dh_end = dh_end; p.states = const_cast<float*>(states);
+  p.dma = !(((uintptr_t)a.f | (uintptr_t)a.x | (uintptr_t)dy) & 3) && !((a.ldf | a.ldx | lddy) & 1);
   p.df = df; p.lddf = lddf; p.dx = dx; p.lddx = lddx; p.dh0 = dh0;
-  const int threads = 64 * waves_of(a.T);
-  auto go = [&](auto t, auto vec) {
+  const dim3 threads(64 * waves_of(a.T)), grid((a.D + kChannels - 1) / kChannels, a.B, p.segments), summaries(grid.x, a.B, p.segments - 1);
+  auto go = [&](auto t) {
     using T = decltype(t);
-    constexpr int V = decltype(vec)::value;
-    const unsigned groups = (unsigned)((a.D + V * kLanes - 1) / (V * kLanes));
-    if (p.segments > 1) scan_bwd_kernel<T, V, true><<<dim3(groups, a.B, p.segments - 1), threads, 0, s>>>(p);
-    scan_bwd_kernel<T, V, false><<<dim3(groups, a.B, p.segments), threads, 0, s>>>(p);
+    if (p.segments > 1) scan_bwd_kernel<T, true><<<summaries, threads, 0, s>>>(p);
+    scan_bwd_kernel<T, false><<<grid, threads, 0, s>>>(p);
   };
-  using one = std::integral_constant<int, 1>;
-  using two = std::integral_constant<int, 2>;
-  if (a.dtype == kBF16)
-    pairs<bf16>({a.f, a.x, dy, df, dx}, {a.ldf, a.ldx, lddy, lddf, lddx}, a.D) ? go(bf16{}, two{}) : go(bf16{}, one{});
-  else
-    pairs<float>({a.f, a.x, dy, df, dx}, {a.ldf, a.ldx, lddy, lddf, lddx}, a.D) ? go(float{}, two{}) : go(float{}, one{});
+  if (a.dtype == kBF16) go(bf16{});
+  else go(float{});
   return hipGetLastError();
 }
 
