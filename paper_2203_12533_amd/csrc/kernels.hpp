@@ -181,6 +181,7 @@ struct ScanArgs {
   const float* h0;
   const int32_t* lens;
 };
+hipError_t scan_init();   // one-time set-up of kernel attributes (dynamic LDS); call once before any capture
 int64_t scan_state_floats(int64_t B, int64_t T, int64_t D);
 int64_t scan_ws_floats(int64_t B, int64_t T, int64_t D);
 hipError_t launch_scan_fwd(hipStream_t s, const ScanArgs& a, void* y, int64_t ldy, float* h_end, float* states, float* ws);

@@ -20,6 +20,7 @@
 // Steps behind the end of a sequence (lens) are the identity map with outputs of zero; their inputs are not read.
 // Sums, states and gates are fp32; y, df and dx are rounded once.  All orders are fixed: the same bits on every run.
 #include <type_traits>
+#include <utility>
 
 #include "common.hpp"
 #include "kernels.hpp"
@@ -28,10 +29,11 @@ namespace pw {
 
 namespace {
 
-constexpr int kSteps = 8;          // consecutive steps of a thread
+constexpr int kSteps = 16;         // consecutive steps of a thread
+constexpr int kFew = 2;             // steps that a tile of hardly any is cut down to
 constexpr int kVec = 2;            // channels of a thread
-constexpr int kLanes = 16;         // lanes side by side along the channels; a wave's parts follow one another in time
-constexpr int kParts = kWave / kLanes, kLevels = 2;
+constexpr int kLanes = 32;         // lanes side by side along the channels; a wave's parts follow one another in time
+constexpr int kParts = kWave / kLanes, kLevels = 1;
 static_assert(1 << kLevels == kParts, "parts meet in pairs");
 constexpr int kWaveSteps = kSteps * kParts;
 constexpr int kMostWaves = 8;
@@ -57,7 +59,7 @@ struct Params {
   float2* maps;                          // [B][segments][D]
   const int32_t* lens;
   int T, D, tiles, segments, seg_tiles;
-  int dma;                               // bf16 rows start on four bytes
+  int dma;                               // pairs of bf16 channels start on four bytes everywhere
 };
 
 // Four adjacent channels, wherever they start.
@@ -84,8 +86,8 @@ __device__ __forceinline__ void unpack_gate(float g, float& a, float& z) {
 
 struct Where {
   int64_t b;
-  int c, n, sub, wave, part, li, nw, len;        // n: channels of the lane that exist
-  bool whole;                                    // every lane of the block has all of its channels
+  int c, n, shift, sub, wave, part, li, nw, len; // n: channels of the lane that exist; it reads them `shift` further left,
+  bool whole;                                    // where a row ends.  whole: every lane of the block has all of its channels
 };
 __device__ __forceinline__ Where where(const Params& p) {
   Where w;
@@ -100,6 +102,8 @@ __device__ __forceinline__ Where where(const Params& p) {
   w.c = (g * kLanes + w.li) * kVec;
   w.n = p.D - w.c < 0 ? 0 : (p.D - w.c < kVec ? p.D - w.c : kVec);
   w.whole = (g + 1) * kChannels <= p.D;
+  const int last = p.D - kVec > 0 ? p.D - kVec : 0;
+  w.shift = w.c > last ? w.c - last : 0;
   w.len = p.T;
   if (p.lens) {
     const int l = p.lens[w.b];
@@ -108,54 +112,74 @@ __device__ __forceinline__ Where where(const Params& p) {
   return w;
 }
 
-// One array seen by a thread: its eight steps of a tile are rows of `ld` elements behind a wave-uniform base, at an offset
-// that stays the same from tile to tile (32 bits hold it: kMostLd).
+// One array seen by a thread: its steps of a tile are rows of `ld` elements behind a wave-uniform base, at an offset that stays
+// the same from tile to tile (32 bits hold it: kMostLd).  What is read begins with the last channels of a row where the lane's
+// own are not all there.
 template <class T>
 struct Column {
   const char* base;                              // row 0 of the sequence
   int64_t row;                                   // bytes
-  uint32_t off;
-  __device__ __forceinline__ Column(const void* p, int64_t ld, const Where& w, int T_)
+  uint32_t col, off;
+  __device__ __forceinline__ Column(const void* p, int64_t ld, const Where& w, int T_, bool written = false)
       : base(reinterpret_cast<const char*>(p) + w.b * T_ * ld * (int64_t)sizeof(T)), row(ld * (int64_t)sizeof(T)),
-        off((uint32_t)(w.sub * kSteps) * (uint32_t)row + (uint32_t)w.c * (uint32_t)sizeof(T)) {}
+        col((uint32_t)(written ? w.c : w.c - w.shift) * (uint32_t)sizeof(T)), off((uint32_t)(w.sub * kSteps) * (uint32_t)row + col) {}
   __device__ __forceinline__ const char* at(int tile0, int i) const { return base + (tile0 + i) * row + off; }
 };
-// The steps of the tile that begins at step tile0.  WHOLE: all steps and channels exist; else those that do not come out as zeros
-// (fetched in their place is the sequence's last row, or its first place in memory where it has no step).
-template <class T, bool WHOLE>
-__device__ __forceinline__ void fetch(const Column<T>& q, const Where& w, int tile0, typename Raw<T>::type (&r)[kSteps]) {
-  typedef typename Raw<T>::type raw;
-  if constexpr (WHOLE) {
+// Own channels first (in a lane without channels anything will do).  Branches are kept out of the loops over steps: they keep the
+// loads of a tile from being asked for together.
+template <class T> __device__ __forceinline__ void align(const Where& w, typename Raw<T>::type (&r)[kSteps]) {
+  static_assert(kVec == 2, "a shift of one");
+  if (!w.whole) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) r[i] = *reinterpret_cast<const raw*>(q.at(tile0, i));
-  } else {
-    const int top = w.len > 0 ? w.len - 1 : 0;
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int t = tile0 + w.sub * kSteps + i;
-      const T* const g = reinterpret_cast<const T*>(q.base + (t < top ? t : top) * q.row) + w.c;
-      r[i] = raw{};
-#pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        if (j < w.n) {
-          const T v = g[j];
-          r[i][j] = t < w.len ? v : (T)0.f;
-        }
-    }
+    for (int i = 0; i < kSteps; ++i) r[i][0] = w.shift ? r[i][1] : r[i][0];
   }
 }
+// The steps of the tile that begins at step tile0.  WHOLE: all steps exist; else those that do not come out as zeros (fetched in
+// their place is another row of the tile).
 template <class T, bool WHOLE>
-__device__ __forceinline__ void put(const Column<T>& q, const Where& w, int tile0, int T_, int i, const float* v) {
+__device__ __forceinline__ void fetch(const Column<T>& q, const Where& w, const Params& p, int tile0, typename Raw<T>::type (&r)[kSteps]) {
+  typedef typename Raw<T>::type raw;
+  const int end = w.len - tile0, top = end > 0 ? end - 1 : 0;
+  auto place = [&](int i) {
+    const int t = w.sub * kSteps + i;
+    return WHOLE ? q.at(tile0, i) : q.base + tile0 * q.row + ((uint32_t)(t < top ? t : top) * (uint32_t)q.row + q.col);
+  };
+  auto load = [&](auto count) {
+    if (p.D >= kVec) {
+#pragma unroll
+      for (int i = 0; i < decltype(count)::value; ++i) r[i] = *reinterpret_cast<const raw*>(place(i));
+    } else {
+#pragma unroll
+      for (int i = 0; i < decltype(count)::value; ++i) r[i][0] = *reinterpret_cast<const T*>(place(i));
+    }
+  };
   if constexpr (WHOLE) {
+    load(std::integral_constant<int, kSteps>{});
+    align<T>(w, r);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) r[i] = raw{};
+    if (end > kFew) load(std::integral_constant<int, kSteps>{});
+    else load(std::integral_constant<int, kFew>{});
+    align<T>(w, r);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) r[i][j] = w.sub * kSteps + i < end ? r[i][j] : (T)0.f;
+  }
+}
+// FULL: every lane of the block has all of its channels.
+template <class T, bool WHOLE, bool FULL>
+__device__ __forceinline__ void put(const Column<T>& q, const Where& w, int tile0, int T_, int i, const float* v) {
+  if (!WHOLE && tile0 + w.sub * kSteps + i >= T_) return;
+  T* const g = reinterpret_cast<T*>(const_cast<char*>(q.at(tile0, i)));
+  if (FULL || w.n == kVec) {
     typename Raw<T>::type r;
 #pragma unroll
     for (int j = 0; j < kVec; ++j) r[j] = (T)v[j];
-    *reinterpret_cast<typename Raw<T>::type*>(const_cast<char*>(q.at(tile0, i))) = r;
-  } else if (tile0 + w.sub * kSteps + i < T_) {
-    T* const g = reinterpret_cast<T*>(const_cast<char*>(q.at(tile0, i)));
-#pragma unroll
-    for (int j = 0; j < kVec; ++j)
-      if (j < w.n) g[j] = (T)v[j];
+    *reinterpret_cast<typename Raw<T>::type*>(g) = r;
+  } else if (w.n) {
+    *g = (T)v[0];
   }
 }
 
@@ -268,10 +292,11 @@ __device__ __forceinline__ void segment_carry(Map<D>* slot, const Where& w, cons
 // 256 bytes at a time, and a lane finds its two channels of step i of array n at [n][i][lane].
 template <int N> struct Ahead {
   typedef __attribute__((address_space(3))) void* lds_ptr;
+  static constexpr int kBytes = N * kSteps * kWave * 4;   // of a wave
   uint32_t (*mine)[kSteps][kWave];               // this wave's part
   uint32_t at;                                   // its offset in LDS
-  __device__ __forceinline__ Ahead(uint32_t (*lds)[N][kSteps][kWave], const Where& w) {
-    mine = lds[w.wave];
+  __device__ __forceinline__ Ahead(uint8_t* lds, const Where& w) {
+    mine = reinterpret_cast<uint32_t (*)[kSteps][kWave]>(lds + w.wave * kBytes);
     at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)mine);
   }
   __device__ __forceinline__ void ask(int n, const Column<bf16>& q, int tile0) const {
@@ -280,38 +305,64 @@ template <int N> struct Ahead {
       asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(q.off), "s"(q.base + (tile0 + i) * q.row),
                    "s"(at + (n * kSteps + i) * (kWave * 4)) : "memory", "m0");
   }
-  __device__ __forceinline__ void take(int n, Raw<bf16>::type (&r)[kSteps]) const {
+  __device__ __forceinline__ void take(int n, const Where& w, Raw<bf16>::type (&r)[kSteps]) const {
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) r[i] = __builtin_bit_cast(bf16x2, mine[n][i][threadIdx.x & 63]);
+    align<bf16>(w, r);
   }
   // Between take() of one tile and ask() for the next: what was read is in registers.
   __device__ __forceinline__ static void taken() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
   // In front of the tile's stores, behind which this would wait for those.
   __device__ __forceinline__ static void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 };
+// Gates of the steps of a tile; a = 1 where there is no step.  In a tile of few steps (kFew) no lane computes more.
+template <bool WHOLE, class F> __device__ __forceinline__ void for_steps(const Where& w, int tile0, F&& f) {
+  if (WHOLE || w.len - tile0 > kFew) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) f(i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kFew; ++i) f(i);
+  }
+}
 template <class T, bool WHOLE>
 __device__ __forceinline__ void gates(const typename Raw<T>::type (&rf)[kSteps], const Where& w, int tile0, float (&a)[kSteps][kVec],
                                       float (&z)[kSteps][kVec]) {
+  if (!WHOLE) {
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i)
+    for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      gate((float)rf[i][j], a[i][j], z[i][j]);
-      if (!WHOLE && tile0 + w.sub * kSteps + i >= w.len) {
+      for (int j = 0; j < kVec; ++j) {
         a[i][j] = 1.f;
         z[i][j] = 0.f;
       }
+  }
+  for_steps<WHOLE>(w, tile0, [&](int i) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      float ai, zi;
+      gate((float)rf[i][j], ai, zi);
+      const bool there = WHOLE || tile0 + w.sub * kSteps + i < w.len;
+      a[i][j] = there ? ai : 1.f;
+      z[i][j] = there ? zi : 0.f;
     }
+  });
 }
 template <class T, bool WHOLE>
 __device__ __forceinline__ void packed_gates(const typename Raw<T>::type (&rf)[kSteps], const Where& w, int tile0, float (&g)[kSteps][kVec]) {
+  if (!WHOLE) {
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i)
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) g[i][j] = 0.f;
+  }
+  for_steps<WHOLE>(w, tile0, [&](int i) {
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
-      g[i][j] = packed_gate((float)rf[i][j]);
-      if (!WHOLE && tile0 + w.sub * kSteps + i >= w.len) g[i][j] = 0.f;      // a = 1
+      const float gi = packed_gate((float)rf[i][j]);
+      g[i][j] = WHOLE || tile0 + w.sub * kSteps + i < w.len ? gi : 0.f;
     }
+  });
 }
 // One value per channel of a [B, .., D] array of floats.
 __device__ __forceinline__ void get_row(const float* p, const Where& w, float (&v)[kVec]) {
@@ -326,10 +377,10 @@ __device__ __forceinline__ void put_row(float* p, const Where& w, const float (&
 
 // SUMMARY: only the map of the block's segment, into slot seg + 1.
 template <class T, bool SUMMARY>
-__global__ __launch_bounds__(64 * kMostWaves, 4) void scan_fwd_kernel(Params p) {
+__global__ __launch_bounds__(64 * kMostWaves, 2) void scan_fwd_kernel(Params p) {
   constexpr bool DMA = sizeof(T) == 2;
   __shared__ __attribute__((aligned(16))) Map<kDown> slots[2][kMostWaves * kLanes];
-  __shared__ __attribute__((aligned(16))) uint32_t next[DMA ? kMostWaves : 1][2][kSteps][kWave];
+  extern __shared__ __attribute__((aligned(16))) uint8_t next[];
   typedef typename Raw<T>::type raw;
   const Where w = where(p);
   const int seg = blockIdx.z, tile = w.nw * kWaveSteps;
@@ -338,9 +389,9 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void scan_fwd_kernel(Params p) 
 #pragma unroll
   for (int j = 0; j < kVec; ++j) prod[j] = 1.f;
   float2* const maps = p.maps + w.b * p.segments * p.D + w.c;
-  const Column<T> qf(p.f, p.ldf, w, p.T), qx(p.x, p.ldx, w, p.T), qy(p.y, p.ldy, w, p.T);
+  const Column<T> qf(p.f, p.ldf, w, p.T), qx(p.x, p.ldx, w, p.T), qy(p.y, p.ldy, w, p.T, true);
   const Ahead<2> ahead(next, w);
-  auto all_of = [&](int k) { return w.whole && (k + 1) * tile <= w.len; };      // wave-uniform
+  auto all_of = [&](int k) { return (k + 1) * tile <= w.len; };      // wave-uniform
   auto ask = [&](int k) {
     if constexpr (DMA) {
       if (p.dma && all_of(k)) {
@@ -367,13 +418,13 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void scan_fwd_kernel(Params p) 
     raw rf[kSteps], rx[kSteps];
     if (DMA && WHOLE && p.dma) {
       if constexpr (DMA) {
-        ahead.take(0, rf);
-        ahead.take(1, rx);
+        ahead.take(0, w, rf);
+        ahead.take(1, w, rx);
         ahead.taken();
       }
     } else {
-      fetch<T, WHOLE>(qf, w, k * tile, rf);
-      fetch<T, WHOLE>(qx, w, k * tile, rx);
+      fetch<T, WHOLE>(qf, w, p, k * tile, rf);
+      fetch<T, WHOLE>(qx, w, p, k * tile, rx);
     }
     if (k + 1 < last) ask(k + 1);
     float a[kSteps][kVec], v[kSteps][kVec], in[kVec];
@@ -401,16 +452,20 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void scan_fwd_kernel(Params p) 
 #pragma unroll
         for (int j = 0; j < kVec; ++j) prod[j] *= slot[i * kLanes + w.li].p[j];
     } else {
+      auto emit = [&](auto full) {
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        float o[kVec];
+        for (int i = 0; i < kSteps; ++i) {
+          float o[kVec];
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-          in[j] = __builtin_fmaf(a[i][j], in[j], v[i][j]);
-          o[j] = WHOLE || k * tile + w.sub * kSteps + i < w.len ? in[j] : 0.f;
+          for (int j = 0; j < kVec; ++j) {
+            in[j] = __builtin_fmaf(a[i][j], in[j], v[i][j]);
+            o[j] = WHOLE || k * tile + w.sub * kSteps + i < w.len ? in[j] : 0.f;
+          }
+          put<T, WHOLE, decltype(full)::value>(qy, w, k * tile, p.T, i, o);
         }
-        put<T, WHOLE>(qy, w, k * tile, p.T, i, o);
-      }
+      };
+      if (w.whole) emit(std::true_type{});
+      else emit(std::false_type{});
     }
   };
   for (int k = first; k < last; ++k) {
@@ -430,11 +485,11 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void scan_fwd_kernel(Params p) 
 
 // SUMMARY: the map of r over the block's segment seg + 1, into slot seg (the last slot holds dh_end).
 template <class T, bool SUMMARY>
-__global__ __launch_bounds__(64 * kMostWaves, 4) void scan_bwd_kernel(Params p) {
+__global__ __launch_bounds__(64 * kMostWaves, 2) void scan_bwd_kernel(Params p) {
   constexpr bool DMA = sizeof(T) == 2;
   constexpr int DIRS = SUMMARY ? kUp : kUp | kDown, N = SUMMARY ? 2 : 3;
   __shared__ __attribute__((aligned(16))) Map<DIRS> slots[2][kMostWaves * kLanes];
-  __shared__ __attribute__((aligned(16))) uint32_t next[DMA ? kMostWaves : 1][N][kSteps][kWave];
+  extern __shared__ __attribute__((aligned(16))) uint8_t next[];
   typedef typename Raw<T>::type raw;
   const Where w = where(p);
   const int seg = SUMMARY ? blockIdx.z + 1 : blockIdx.z, tile = w.nw * kWaveSteps;
@@ -444,9 +499,10 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void scan_bwd_kernel(Params p) 
 #pragma unroll
   for (int j = 0; j < kVec; ++j) prod[j] = 1.f;
   float2* const maps = p.maps + w.b * p.segments * p.D + w.c;
-  const Column<T> qf(p.f, p.ldf, w, p.T), qx(p.x, p.ldx, w, p.T), qd(p.dy, p.ldy, w, p.T), of(p.df, p.lddf, w, p.T), ox(p.dx, p.lddx, w, p.T);
+  const Column<T> qf(p.f, p.ldf, w, p.T), qx(p.x, p.ldx, w, p.T), qd(p.dy, p.ldy, w, p.T), of(p.df, p.lddf, w, p.T, true),
+      ox(p.dx, p.lddx, w, p.T, true);
   const Ahead<N> ahead(next, w);
-  auto all_of = [&](int k) { return w.whole && (k + 1) * tile <= w.len; };      // wave-uniform
+  auto all_of = [&](int k) { return (k + 1) * tile <= w.len; };      // wave-uniform
   auto ask = [&](int k) {
     if constexpr (DMA) {
       if (p.dma && all_of(k)) {
@@ -475,15 +531,15 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void scan_bwd_kernel(Params p) 
     if (!SUMMARY) get_row(p.states + (w.b * p.tiles + k) * p.D, w, h);
     if (DMA && WHOLE && p.dma) {
       if constexpr (DMA) {
-        ahead.take(0, rf);
-        ahead.take(1, rd);
-        if constexpr (!SUMMARY) ahead.take(2, rx);
+        ahead.take(0, w, rf);
+        ahead.take(1, w, rd);
+        if constexpr (!SUMMARY) ahead.take(2, w, rx);
         ahead.taken();
       }
     } else {
-      fetch<T, WHOLE>(qf, w, k * tile, rf);
-      fetch<T, WHOLE>(qd, w, k * tile, rd);
-      if (!SUMMARY) fetch<T, WHOLE>(qx, w, k * tile, rx);
+      fetch<T, WHOLE>(qf, w, p, k * tile, rf);
+      fetch<T, WHOLE>(qd, w, p, k * tile, rd);
+      if (!SUMMARY) fetch<T, WHOLE>(qx, w, p, k * tile, rx);
     }
     if (k > first) ask(k - 1);
     packed_gates<T, WHOLE>(rf, w, k * tile, g);
@@ -529,21 +585,25 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void scan_bwd_kernel(Params p) 
           before[i][j] = hin[j] - xi;                       // h_(t-1) - x_t
           hin[j] = __builtin_fmaf(a, hin[j], z * xi);
         }
+      auto emit = [&](auto full) {
 #pragma unroll
-      for (int i = kSteps - 1; i >= 0; --i) {
-        float vf[kVec], vx[kVec];
-        const bool there = WHOLE || k * tile + w.sub * kSteps + i < w.len;
+        for (int i = kSteps - 1; i >= 0; --i) {
+          float vf[kVec], vx[kVec];
+          const bool there = WHOLE || k * tile + w.sub * kSteps + i < w.len;
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-          unpack_gate(g[i][j], a, z);
-          const float gr = (float)rd[i][j] + in[j];
-          vx[j] = there ? gr * z : 0.f;
-          vf[j] = there ? vx[j] * a * before[i][j] : 0.f;
-          in[j] = a * gr;
+          for (int j = 0; j < kVec; ++j) {
+            unpack_gate(g[i][j], a, z);
+            const float gr = (float)rd[i][j] + in[j];
+            vx[j] = there ? gr * z : 0.f;
+            vf[j] = there ? vx[j] * a * before[i][j] : 0.f;
+            in[j] = a * gr;
+          }
+          put<T, WHOLE, decltype(full)::value>(of, w, k * tile, p.T, i, vf);
+          put<T, WHOLE, decltype(full)::value>(ox, w, k * tile, p.T, i, vx);
         }
-        put<T, WHOLE>(of, w, k * tile, p.T, i, vf);
-        put<T, WHOLE>(ox, w, k * tile, p.T, i, vx);
-      }
+      };
+      if (w.whole) emit(std::true_type{});
+      else emit(std::false_type{});
     }
   };
   for (int k = last - 1; k >= first; --k) {
@@ -592,6 +652,18 @@ Params params_of(const ScanArgs& a, float* ws) {
 }
 }  // namespace
 
+hipError_t scan_init() {
+  const std::pair<const void*, int> k[] = {{reinterpret_cast<const void*>(scan_fwd_kernel<bf16, true>), Ahead<2>::kBytes},
+                                           {reinterpret_cast<const void*>(scan_fwd_kernel<bf16, false>), Ahead<2>::kBytes},
+                                           {reinterpret_cast<const void*>(scan_bwd_kernel<bf16, true>), Ahead<2>::kBytes},
+                                           {reinterpret_cast<const void*>(scan_bwd_kernel<bf16, false>), Ahead<3>::kBytes}};
+  for (const auto& f : k) {
+    const hipError_t e = hipFuncSetAttribute(f.first, hipFuncAttributeMaxDynamicSharedMemorySize, kMostWaves * f.second);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 int64_t scan_state_floats(int64_t B, int64_t T, int64_t D) {
   return dims_ok(B, T, D) ? (T == 0 ? 0 : B * tiles_of((int)T) * D) : -1;
 }
@@ -609,12 +681,13 @@ hipError_t launch_scan_fwd(hipStream_t s, const ScanArgs& a, void* y, int64_t ld
   Params p = params_of(a, ws);
   if (p.segments > 1 && !ws) return hipErrorInvalidValue;
   p.y = y; p.ldy = ldy; p.h_end = h_end; p.states = states;
-  p.dma = !(((uintptr_t)a.f | (uintptr_t)a.x) & 3) && !((a.ldf | a.ldx) & 1);
+  p.dma = a.D % 2 == 0 && !(((uintptr_t)a.f | (uintptr_t)a.x) & 3) && !((a.ldf | a.ldx) & 1);
   const dim3 threads(64 * waves_of(a.T)), grid((a.D + kChannels - 1) / kChannels, a.B, p.segments), summaries(grid.x, a.B, p.segments - 1);
   auto go = [&](auto t) {
     using T = decltype(t);
-    if (p.segments > 1) scan_fwd_kernel<T, true><<<summaries, threads, 0, s>>>(p);
-    scan_fwd_kernel<T, false><<<grid, threads, 0, s>>>(p);
+    auto lds = [&](int bytes) { return sizeof(T) == 2 ? (size_t)waves_of(a.T) * bytes : 0; };
+    if (p.segments > 1) scan_fwd_kernel<T, true><<<summaries, threads, lds(Ahead<2>::kBytes), s>>>(p);
+    scan_fwd_kernel<T, false><<<grid, threads, lds(Ahead<2>::kBytes), s>>>(p);
   };
   if (a.dtype == kBF16) go(bf16{});
   else go(float{});
@@ -632,13 +705,14 @@ hipError_t launch_scan_bwd(hipStream_t s, const ScanArgs& a, const void* dy, int
   Params p = params_of(a, ws);
   if ((!states && a.T > 0) || (p.segments > 1 && !ws)) return hipErrorInvalidValue;
   p.dy = dy; p.ldy = lddy; p.dh_end = dh_end; p.states = const_cast<float*>(states);
-  p.dma = !(((uintptr_t)a.f | (uintptr_t)a.x | (uintptr_t)dy) & 3) && !((a.ldf | a.ldx | lddy) & 1);
+  p.dma = a.D % 2 == 0 && !(((uintptr_t)a.f | (uintptr_t)a.x | (uintptr_t)dy) & 3) && !((a.ldf | a.ldx | lddy) & 1);
   p.df = df; p.lddf = lddf; p.dx = dx; p.lddx = lddx; p.dh0 = dh0;
   const dim3 threads(64 * waves_of(a.T)), grid((a.D + kChannels - 1) / kChannels, a.B, p.segments), summaries(grid.x, a.B, p.segments - 1);
   auto go = [&](auto t) {
     using T = decltype(t);
-    if (p.segments > 1) scan_bwd_kernel<T, true><<<summaries, threads, 0, s>>>(p);
-    scan_bwd_kernel<T, false><<<grid, threads, 0, s>>>(p);
+    auto lds = [&](int bytes) { return sizeof(T) == 2 ? (size_t)waves_of(a.T) * bytes : 0; };
+    if (p.segments > 1) scan_bwd_kernel<T, true><<<summaries, threads, lds(Ahead<2>::kBytes), s>>>(p);
+    scan_bwd_kernel<T, false><<<grid, threads, lds(Ahead<3>::kBytes), s>>>(p);
   };
   if (a.dtype == kBF16) go(bf16{});
   else go(float{});
