@@ -551,7 +551,7 @@ int64_t pw_f8_scale_bytes(int64_t rows, int64_t cols);
  * both outputs, as weights want it.  e is the smallest integer in [-127, 127] for which no finite element of the block
  * exceeds the format's largest value times 2^e (-127 for a block of zeros); elements are rounded to nearest, ties to even.
  * NaN stays NaN; infinities become NaN in e4m3 and stay infinities in e5m2; neither touches the scale of its block.
- * q, qt: 16-byte aligned, ldq >= cols and ldqt >= rows, both multiples of 16; rows are filled with zeros up to the next multiple
+ * The scale tables are 4-byte aligned; q, qt 16-byte aligned, ldq >= cols and ldqt >= rows, both multiples of 16; rows are filled with zeros up to the next multiple
  * of 16 elements, so that this length can be the K of a product; bytes behind that are left as they were. */
 typedef struct {
   int32_t dtype;             /* of x: PW_F32 or PW_BF16 */

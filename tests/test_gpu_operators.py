@@ -130,6 +130,13 @@ def test_quantisation_is_exact(ctx, fmt, block, rows, cols, bf16, kw):
     check_quantized(ctx, x, fmt, block, bf16, **kw)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("cols", [2, 7, 8, 9, 121, 122, 123, 124, 125, 126, 127, 128, 129, 135, 255])
+def test_quantisation_of_any_width(ctx, cols, bf16):
+    """Every number of columns left over behind whole groups of eight, at rows that start anywhere; what lies behind a row is NaN."""
+    check_quantized(ctx, rnd(cols, 131, cols) * np.exp(rnd(3, 1, cols)), "e4m3", 1, bf16, ldx=cols + 3, offset=1)
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
 @pytest.mark.parametrize("block", [1, 128])
 def test_quantisation_of_every_kind_of_value(ctx, fmt, block):

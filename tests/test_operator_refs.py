@@ -99,7 +99,7 @@ int main() {
   ACCEPT(Q, q0, rows = 0) ACCEPT(Q, q0, cols = 0)
   REFUSE(Q, q0, dtype = kI32) REFUSE(Q, q0, format = 2) REFUSE(Q, q0, format = -1) REFUSE(Q, q0, block_rows = 64) REFUSE(Q, q0, x = nullptr)
   REFUSE(Q, q0, rows = -1) REFUSE(Q, q0, cols = -1) REFUSE(Q, q0, ldx = 99) REFUSE(Q, q0, ldq = 104) REFUSE(Q, q0, ldq = 96)
-  REFUSE(Q, q0, ldqt = 0) REFUSE(Q, q0, ldqt = 24) REFUSE(Q, q0, q_scale = nullptr) REFUSE(Q, q0, qt_scale = nullptr)
+  REFUSE(Q, q0, ldqt = 0) REFUSE(Q, q0, ldqt = 24) REFUSE(Q, q0, q_scale = S + 2) REFUSE(Q, q0, qt_scale = S + 1) REFUSE(Q, q0, q_scale = nullptr) REFUSE(Q, q0, qt_scale = nullptr)
   REFUSE(Q, q0, q = (char*)P + 8) REFUSE(Q, q0, qt = (char*)P + 4) REFUSE(Q, q0, x = (char*)P + 2) REFUSE(Q, q0, rows = 128LL * 65535 + 1)
   REFUSE(Q, q0, cols = (1LL << 30) + 1)
   { auto a = q0; a.q = a.qt = nullptr; expect("no output", Q, no); }
