@@ -615,7 +615,7 @@ typedef struct {
 pw_status pw_op_dropout_fwd(pw_ctx* ctx, const pw_dropout_args* args, const void* x, const float* bias, const float* res, void* y);
 /* dx = keep dy / (1 - p) (the residual's gradient is dy itself); dbias: null, or fp32 [cols] that receives the column sums of
  * dx before its rounding (overwritten, or added into when accumulate = 1).  ws: fp32 workspace of
- * pw_dropout_bwd_ws_floats(rows, cols) floats if dbias is wanted, else null.  dx may be the same array as dy where type and
+ * pw_dropout_bwd_ws_floats(rows, cols) floats if dbias is wanted (may be null where that is 0), else null.  dx may be the same array as dy where type and
  * stride are the same. */
 pw_status pw_op_dropout_bwd(pw_ctx* ctx, const pw_dropout_args* args, const void* dy, void* dx, float* dbias, float* ws, int accumulate);
 int64_t pw_dropout_bwd_ws_floats(int64_t rows, int64_t cols);   /* -1 for impossible sizes */

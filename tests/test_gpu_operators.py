@@ -342,7 +342,7 @@ def dropout(ctx, rows, cols, bf16, out_bf16, p, res=True, bias=True, seed=(1 << 
     dx, pdx = dev(np.full((rows, cols), 7.0), act(bf16), ldx, fill=7.0, offset=offset)
     db0 = rnd(5, cols).astype(np.float32)
     dbt, pdb = dev(db0)
-    ws = torch.full((pwb.dropout_bwd_ws_floats(rows, cols),), float("nan"), device="cuda")
+    ws = torch.full((max(1, pwb.dropout_bwd_ws_floats(rows, cols)),), float("nan"), device="cuda")
     torch.cuda.synchronize()
     a = pwb.DropoutArgs(dtype=DT[bf16], out_dtype=DT[out_bf16], rows=rows, cols=cols, ldx=ldx, ldy=ldy, p=p, seed=seed, site=site,
                         step=step, step_dev=step_dev.data_ptr() if step_dev is not None else None)
@@ -411,7 +411,7 @@ def test_dropout_step_on_the_device_wraps_and_replays_draw_anew(ctx):
         x = torch.ones(rows, cols, device="cuda")
         y = torch.zeros_like(x)
         dx, db = torch.zeros_like(x), torch.zeros(cols, device="cuda")
-        ws = torch.empty(pwb.dropout_bwd_ws_floats(rows, cols), device="cuda")
+        ws = torch.empty(max(1, pwb.dropout_bwd_ws_floats(rows, cols)), device="cuda")
         a = pwb.DropoutArgs(dtype=pwb.PW_F32, out_dtype=pwb.PW_F32, rows=rows, cols=cols, ldx=cols, ldy=cols, p=0.25, seed=1, site=2, step=0,
                             step_dev=step.data_ptr())
         torch.cuda.synchronize()
