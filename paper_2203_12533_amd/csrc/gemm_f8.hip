@@ -119,7 +119,7 @@ template <int FMT> __device__ __forceinline__ bf16x8 widen8(const i32x8& f, int 
 
 // Few rows, and rows too far apart for 32-bit offsets.  What bounds a product of few rows is reading B once, so nothing is
 // staged: a block owns 16 columns and 16 rows, its waves take every W-th k block, operands go from memory straight into
-// fragments (a lane has 32 consecutive bytes of its row, four lanes a line), kAhead blocks at a time, and the waves' sums meet
+// fragments (four lanes read 64 consecutive bytes of a row), kAhead blocks at a time, and the waves' sums meet
 // in LDS in wave order.  1 x 8192 x 2048: 5.4 us a pass, of which the launch is about 4.
 constexpr int kAhead = 4;
 template <int W, int FA, int FB, bool EXACT>
@@ -131,8 +131,8 @@ __global__ __launch_bounds__(64 * W) void gemm_f8_direct_kernel(GemmF8Params p) 
   auto in = [](int64_t r, int64_t rows) { return r < rows ? r : rows - 1; };
   auto scale_of = [](const uint8_t* t, int64_t r) { return t + (r & ~63LL) + (r & 15) * 4 + ((r & 63) >> 4); };
   const int64_t ra = in(m0 + L, p.M), rb = in(n0 + L, p.N);
-  const uint8_t* const pa = p.A + ra * p.lda + 32 * g;
-  const uint8_t* const pb = p.B + rb * p.ldb + 32 * g;
+  const uint8_t* const pa = p.A + ra * p.lda + 16 * g;
+  const uint8_t* const pb = p.B + rb * p.ldb + 16 * g;
   const uint8_t* const qa = scale_of(p.sa, ra);
   const uint8_t* const qb = scale_of(p.sb, rb);
   f32x4 acc = {};
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(64 * W) void gemm_f8_direct_kernel(GemmF8Params p) 
     for (int h = 0; h < 2; ++h) {
       const int64_t k = (int64_t)kb * kBK;
       i32x4 v = {};
-      if (k + 32 * g + 16 * h < p.K) v = *reinterpret_cast<const i32x4*>(q + k + 16 * h);
+      if (k + 16 * g + 64 * h < p.K) v = *reinterpret_cast<const i32x4*>(q + k + 64 * h);
 #pragma unroll
       for (int e = 0; e < 4; ++e) f[4 * h + e] = v[e];
     }
@@ -172,17 +172,22 @@ __global__ __launch_bounds__(64 * W) void gemm_f8_direct_kernel(GemmF8Params p) 
       }
     }
   };
+  const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
+  const bool mine = r < 16 && m0 + r < p.M && n0 + c < p.N;
+  EpiParams epi = p.epi;
+  float bias = 0.f;                        // on its way with the operands
+  if (mine && epi_has_bias(epi.mode) && epi.bias) bias = epi.bias[n0 + c];
+  epi.bias = nullptr;
   int kb = wave;
   for (; kb + (kAhead - 1) * W < total; kb += kAhead * W) several(kb, std::integral_constant<int, kAhead>{});
   for (; kb < total; kb += W) several(kb, std::integral_constant<int, 1>{});
   *reinterpret_cast<f32x4*>(&part[wave][L][4 * g]) = acc;
   __syncthreads();
-  const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
-  if (r < 16 && m0 + r < p.M && n0 + c < p.N) {
+  if (mine) {
     float v = part[0][r][c];
 #pragma unroll
     for (int w = 1; w < W; ++w) v += part[w][r][c];
-    epilogue1<true>(p.epi, m0 + r, n0 + c, v);
+    epilogue1<true>(epi, m0 + r, n0 + c, v + bias);
   }
 }
 
