@@ -6,16 +6,24 @@
 //
 //   g_t = dy_t + r_(t+1),  dx_t = g_t (1 - a_t),  df_t = g_t (h_(t-1) - x_t) a_t (1 - a_t),  dh_0 = r_1.
 //
-// A step is the map h -> a h + v, and maps compose: (P, S) after (p, s) is (P p, P s + S).  A thread takes 8 consecutive
-// steps of its four channels into registers and composes them, the quarters of a wave exchange their maps, the waves of a block
-// hand theirs over through LDS, and every thread then runs its steps again from the state in front of them: inputs are
-// read once, nothing but outputs is written.  A block of up to 8 waves has 64 channels (16 lanes of four, so that a row is
-// 128 or 256 bytes) and a tile of 32 steps per wave; it walks down its tiles with the state in registers, the next tile on its
-// way.  The forward pass keeps the state in front of each tile (fp32, one value per channel and tile); the backward pass
-// starts every tile from it and walks upwards.
+// A step is the map h -> a h + v, and maps compose: (P, S) after (p, s) is (P p, P s + S).  A thread takes 16 consecutive
+// steps of its two channels into registers and composes them, the two halves of a wave exchange their maps, the waves of a
+// block hand theirs over through LDS, and every thread then runs its steps again from the state in front of them: inputs are
+// read once, nothing but outputs is written.  A block has 64 channels, so that a row of it is a whole cache line of bf16, and a
+// tile of 32 steps for each of its up to 8 waves; it walks down its tiles with the state in registers.  The forward pass keeps
+// the state in front of each tile (fp32, one value per channel and tile); the backward pass starts every tile from it and
+// walks upwards.
 //
-// Few channels leave compute units idle.  The sequence is then cut into segments of whole tiles: a first launch composes
-// each segment into one map, the second composes the maps in front of its segment (behind it, backward) and goes on as above.
+// The least traffic is three arrays forward and five backward.  bf16 tiles come by direct loads into LDS while the one before
+// is at work (registers hold one tile: 205 of 256 in the backward pass; the forward pass is kept to 128, so that two blocks of a
+// second round fit a unit: 12 x 1024 x 2048 50.2 -> 46.9 us).  8 x 1024 x 2048 bf16: 28 us forward (3.6 TB/s; a copy reaches 5.15),
+// 48.4 us backward.  Without its stores the forward pass takes 23, without the exponentials 25, without both 19: with two waves
+// to a SIMD neither hides all of the other.  Blocks of 32 channels, two to a unit, read and write half lines: 33 and 52 us.  A
+// second tile ahead wins nothing.  16 steps to a thread halve the exchanges that 8 steps take.
+//
+// Few channels leave compute units idle.  The sequence is then cut into segments of whole tiles (plan_of): a first launch
+// composes each segment into one map, the second composes the maps in front of its segment (behind it, backward) and goes on as
+// above.  1 x 16384 x 512 bf16: 24.7 us forward, 31.1 backward.
 //
 // Steps behind the end of a sequence (lens) are the identity map with outputs of zero; their inputs are not read.
 // Sums, states and gates are fp32; y, df and dx are rounded once.  All orders are fixed: the same bits on every run.
@@ -39,9 +47,6 @@ constexpr int kWaveSteps = kSteps * kParts;
 constexpr int kMostWaves = 8;
 constexpr int kChannels = kVec * kLanes;
 constexpr int64_t kMostLd = 1 << 21;     // a tile's rows are within 32 bits of offset
-// Blocks next to each other in memory share a cache line where a row of theirs is 64 bytes: they start on the same XCD then (ids
-// go round the eight of them).
-constexpr bool kSwap = kChannels < 64;
 
 int waves_of(int T) {
   const int w = (int)(((int64_t)T + kWaveSteps - 1) / kWaveSteps);
@@ -56,13 +61,14 @@ struct Params {
   int64_t ldf, ldx, ldy, lddf, lddx;     // ldy: of y (forward) or dy (backward)
   const float *h0, *dh_end;
   float *h_end, *dh0, *states;
-  float2* maps;                          // [B][segments][D]
+  float2* maps;                          // [block of channels][segments][kChannels]
   const int32_t* lens;
   int T, D, tiles, segments, seg_tiles;
+  uint32_t groups, base;                 // groups of channels of a sequence; the launch's first block of channels
   int dma;                               // pairs of bf16 channels start on four bytes everywhere
 };
 
-// Four adjacent channels, wherever they start.
+// The channels of a thread, wherever they start.
 template <class T> struct Raw;
 template <> struct Raw<bf16> { typedef __bf16 type __attribute__((ext_vector_type(kVec), aligned(2))); };
 template <> struct Raw<float> { typedef float type __attribute__((ext_vector_type(kVec), aligned(4))); };
@@ -91,14 +97,14 @@ struct Where {
 };
 __device__ __forceinline__ Where where(const Params& p) {
   Where w;
-  w.b = blockIdx.y;
+  const uint32_t id = p.base + blockIdx.x;
+  const int g = (int)(id % p.groups);
+  w.b = id / p.groups;
   w.wave = threadIdx.x >> 6;
   w.part = (threadIdx.x / kLanes) % kParts;
   w.li = threadIdx.x % kLanes;
   w.sub = kParts * w.wave + w.part;
   w.nw = blockDim.x >> 6;
-  int g = blockIdx.x;
-  if (kSwap && g < (int)(gridDim.x & ~15u)) g = (g & ~15) | ((g & 7) << 1) | ((g >> 3) & 1);
   w.c = (g * kLanes + w.li) * kVec;
   w.n = p.D - w.c < 0 ? 0 : (p.D - w.c < kVec ? p.D - w.c : kVec);
   w.whole = (g + 1) * kChannels <= p.D;
@@ -257,6 +263,9 @@ __device__ __forceinline__ void compose(Map<DIRS>* slot, const Where& w, const M
   }
 }
 
+__device__ __forceinline__ float2* maps_of(const Params& p, const Where& w) {
+  return p.maps + (int64_t)blockIdx.x * p.segments * kChannels + w.li * kVec;
+}
 // What reaches segment `seg`: the maps of the slots 0 .. seg (down) or segments - 1 .. seg (up), the first of which is a
 // constant.  Each part of a wave composes a stretch of them, then they meet as they do in a tile.
 template <int D>
@@ -272,7 +281,7 @@ __device__ __forceinline__ void segment_carry(Map<D>* slot, const Where& w, cons
   for (int i = 0; i < per; ++i) {
     const int k = D == kDown ? w.sub * per + i : n - 1 - ((subs - 1 - w.sub) * per + i);
     if (D == kDown ? k < n : k >= 0) {
-      const float2* q = p.maps + (w.b * p.segments + (D == kDown ? k : seg + k)) * p.D + w.c;
+      const float2* q = maps_of(p, w) + (D == kDown ? k : seg + k) * kChannels;
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
         if (j < w.n) {
@@ -377,7 +386,7 @@ __device__ __forceinline__ void put_row(float* p, const Where& w, const float (&
 
 // SUMMARY: only the map of the block's segment, into slot seg + 1.
 template <class T, bool SUMMARY>
-__global__ __launch_bounds__(64 * kMostWaves, 2) void scan_fwd_kernel(Params p) {
+__global__ __launch_bounds__(64 * kMostWaves, 4) void scan_fwd_kernel(Params p) {
   constexpr bool DMA = sizeof(T) == 2;
   __shared__ __attribute__((aligned(16))) Map<kDown> slots[2][kMostWaves * kLanes];
   extern __shared__ __attribute__((aligned(16))) uint8_t next[];
@@ -388,7 +397,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 2) void scan_fwd_kernel(Params p) 
   float h[kVec] = {}, prod[kVec], up[kVec] = {}, in_up[kVec];
 #pragma unroll
   for (int j = 0; j < kVec; ++j) prod[j] = 1.f;
-  float2* const maps = p.maps + w.b * p.segments * p.D + w.c;
+  float2* const maps = maps_of(p, w);
   const Column<T> qf(p.f, p.ldf, w, p.T), qx(p.x, p.ldx, w, p.T), qy(p.y, p.ldy, w, p.T, true);
   const Ahead<2> ahead(next, w);
   auto all_of = [&](int k) { return (k + 1) * tile <= w.len; };      // wave-uniform
@@ -476,7 +485,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 2) void scan_fwd_kernel(Params p) 
     if constexpr (SUMMARY) {
 #pragma unroll
       for (int j = 0; j < kVec; ++j)
-        if (j < w.n) maps[(int64_t)(seg + 1) * p.D + j] = make_float2(seg == 0 ? 0.f : prod[j], h[j]);
+        if (j < w.n) maps[(seg + 1) * kChannels + j] = make_float2(seg == 0 ? 0.f : prod[j], h[j]);
     } else if (p.h_end && seg == p.segments - 1) {
       put_row(p.h_end + w.b * p.D, w, h);
     }
@@ -498,7 +507,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 2) void scan_bwd_kernel(Params p) 
   float r[kVec] = {}, prod[kVec];
 #pragma unroll
   for (int j = 0; j < kVec; ++j) prod[j] = 1.f;
-  float2* const maps = p.maps + w.b * p.segments * p.D + w.c;
+  float2* const maps = maps_of(p, w);
   const Column<T> qf(p.f, p.ldf, w, p.T), qx(p.x, p.ldx, w, p.T), qd(p.dy, p.ldy, w, p.T), of(p.df, p.lddf, w, p.T, true),
       ox(p.dx, p.lddx, w, p.T, true);
   const Ahead<N> ahead(next, w);
@@ -518,7 +527,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 2) void scan_bwd_kernel(Params p) 
     if (SUMMARY && behind && w.sub == 0) {
 #pragma unroll
       for (int j = 0; j < kVec; ++j)
-        if (j < w.n) maps[(int64_t)seg * p.D + j] = make_float2(0.f, r[j]);
+        if (j < w.n) maps[seg * kChannels + j] = make_float2(0.f, r[j]);
     }
   } else {
     segment_carry<kUp>(reinterpret_cast<Map<kUp>*>(slots[1]), w, p, seg, r);
@@ -614,21 +623,27 @@ __global__ __launch_bounds__(64 * kMostWaves, 2) void scan_bwd_kernel(Params p) 
     if constexpr (SUMMARY) {
 #pragma unroll
       for (int j = 0; j < kVec; ++j)
-        if (j < w.n) maps[(int64_t)(seg - 1) * p.D + j] = make_float2(behind ? 0.f : prod[j], r[j]);
+        if (j < w.n) maps[(seg - 1) * kChannels + j] = make_float2(behind ? 0.f : prod[j], r[j]);
     } else if (p.dh0 && seg == 0) {
       put_row(p.dh0 + w.b * p.D, w, r);
     }
   }
 }
 
-// How many segments: as many as bring the launch to a block per compute unit, and no more than there are tiles.
-int segments_of(int64_t B, int T, int D) {
-  const int64_t blocks = B * ((D + kChannels - 1) / kChannels), tiles = tiles_of(T);
-  int64_t n = blocks >= 192 ? 1 : (256 + blocks - 1) / blocks;
+// Blocks of channels run a round of one per compute unit at a time.  Those of the last round are cut into segments where they
+// leave three quarters of the units idle or more, which costs reading the gates and one more array again: as many segments as
+// still fit a round, no more than there are tiles.  Forward and backward in us, bf16, cut and not, of 2048 channels:
+// 1 x 1024 steps 12.9 + 17.1 and 19.0 + 28.8, 9 x 1024 44.3 + 67.9 and 47.4 + 74.8, 10 x 4096 147 + 224 and 170 + 268; half a
+// round or three tiles win nothing: 4 x 2048 45.3 + 65.0 and 42.4 + 70.3, 10 x 768 36.5 + 57.3 and 34.4 + 58.0.
+constexpr int kUnits = 256, kCutFrom = 4;
+struct Plan { int64_t whole, rest; int segments; };        // blocks of channels taken whole, the others, and into how many
+Plan plan_of(int64_t B, int T, int D) {
+  const int64_t blocks = B * ((D + kChannels - 1) / kChannels), left = blocks % kUnits, tiles = tiles_of(T);
+  if (left == 0 || left > kUnits / 4 || tiles < kCutFrom) return {blocks, 0, 1};
+  int64_t n = kUnits / left;
   if (n > tiles) n = tiles;
-  if (n <= 1) return 1;
   const int64_t per = (tiles + n - 1) / n;
-  return (int)((tiles + per - 1) / per);
+  return {blocks - left, left, (int)((tiles + per - 1) / per)};
 }
 bool dims_ok(int64_t B, int64_t T, int64_t D) {
   return B >= 0 && T >= 0 && D >= 0 && B <= 65535 && T <= (1 << 30) && D <= kMostLd;
@@ -644,12 +659,28 @@ Params params_of(const ScanArgs& a, float* ws) {
   p.f = a.f; p.x = a.x; p.ldf = a.ldf; p.ldx = a.ldx;
   p.h0 = a.h0; p.lens = a.lens;
   p.T = a.T; p.D = a.D;
+  p.groups = ((uint32_t)a.D + kChannels - 1) / kChannels;
   p.tiles = tiles_of(a.T);
-  p.segments = segments_of(a.B, a.T, a.D);
-  p.seg_tiles = (p.tiles + p.segments - 1) / p.segments;
   p.maps = reinterpret_cast<float2*>(ws);
   return p;
 }
+// The launches of a plan: launch(params, blocks, segments, summaries).
+template <class F> void run(const Plan& plan, Params p, F&& launch) {
+  constexpr int64_t most = 1 << 22;            // threads of a launch are counted in 32 bits
+  p.segments = 1;
+  p.seg_tiles = p.tiles;
+  for (int64_t done = 0; done < plan.whole; done += most) {
+    p.base = (uint32_t)done;
+    launch(p, plan.whole - done < most ? plan.whole - done : most, 1, false);
+  }
+  if (!plan.rest) return;
+  p.base = (uint32_t)plan.whole;
+  p.segments = plan.segments;
+  p.seg_tiles = (p.tiles + plan.segments - 1) / plan.segments;
+  launch(p, plan.rest, plan.segments - 1, true);
+  launch(p, plan.rest, plan.segments, false);
+}
+
 }  // namespace
 
 hipError_t scan_init() {
@@ -670,8 +701,8 @@ int64_t scan_state_floats(int64_t B, int64_t T, int64_t D) {
 int64_t scan_ws_floats(int64_t B, int64_t T, int64_t D) {
   if (!dims_ok(B, T, D)) return -1;
   if (B == 0 || T == 0 || D == 0) return 0;
-  const int64_t n = segments_of(B, (int)T, (int)D);
-  return n == 1 ? 0 : 2 * B * n * D;
+  const Plan p = plan_of(B, (int)T, (int)D);
+  return 2 * p.rest * p.segments * kChannels;
 }
 
 hipError_t launch_scan_fwd(hipStream_t s, const ScanArgs& a, void* y, int64_t ldy, float* h_end, float* states, float* ws) {
@@ -679,15 +710,19 @@ hipError_t launch_scan_fwd(hipStream_t s, const ScanArgs& a, void* y, int64_t ld
   if ((((uintptr_t)h_end | (uintptr_t)states) & 3) || ((uintptr_t)ws & 7)) return hipErrorInvalidValue;
   if (a.B == 0 || a.D == 0) return hipSuccess;
   Params p = params_of(a, ws);
-  if (p.segments > 1 && !ws) return hipErrorInvalidValue;
+  const Plan plan = plan_of(a.B, a.T, a.D);
+  if (plan.rest && !ws) return hipErrorInvalidValue;
   p.y = y; p.ldy = ldy; p.h_end = h_end; p.states = states;
   p.dma = a.D % 2 == 0 && !(((uintptr_t)a.f | (uintptr_t)a.x) & 3) && !((a.ldf | a.ldx) & 1);
-  const dim3 threads(64 * waves_of(a.T)), grid((a.D + kChannels - 1) / kChannels, a.B, p.segments), summaries(grid.x, a.B, p.segments - 1);
+  const int waves = waves_of(a.T);
   auto go = [&](auto t) {
     using T = decltype(t);
-    auto lds = [&](int bytes) { return sizeof(T) == 2 ? (size_t)waves_of(a.T) * bytes : 0; };
-    if (p.segments > 1) scan_fwd_kernel<T, true><<<summaries, threads, lds(Ahead<2>::kBytes), s>>>(p);
-    scan_fwd_kernel<T, false><<<grid, threads, lds(Ahead<2>::kBytes), s>>>(p);
+    run(plan, p, [&](const Params& q, int64_t blocks, int segments, bool summaries) {
+      const dim3 grid((unsigned)blocks, 1, (unsigned)segments);
+      const auto lds = [&](int bytes) { return sizeof(T) == 2 ? (size_t)waves * bytes : 0; };
+      if (summaries) scan_fwd_kernel<T, true><<<grid, 64 * waves, lds(Ahead<2>::kBytes), s>>>(q);
+      else scan_fwd_kernel<T, false><<<grid, 64 * waves, lds(Ahead<2>::kBytes), s>>>(q);
+    });
   };
   if (a.dtype == kBF16) go(bf16{});
   else go(float{});
@@ -703,16 +738,20 @@ hipError_t launch_scan_bwd(hipStream_t s, const ScanArgs& a, const void* dy, int
   if ((((uintptr_t)dh_end | (uintptr_t)states | (uintptr_t)dh0) & 3) || ((uintptr_t)ws & 7)) return hipErrorInvalidValue;
   if (a.B == 0 || a.D == 0) return hipSuccess;
   Params p = params_of(a, ws);
-  if ((!states && a.T > 0) || (p.segments > 1 && !ws)) return hipErrorInvalidValue;
+  const Plan plan = plan_of(a.B, a.T, a.D);
+  if ((!states && a.T > 0) || (plan.rest && !ws)) return hipErrorInvalidValue;
   p.dy = dy; p.ldy = lddy; p.dh_end = dh_end; p.states = const_cast<float*>(states);
   p.dma = a.D % 2 == 0 && !(((uintptr_t)a.f | (uintptr_t)a.x | (uintptr_t)dy) & 3) && !((a.ldf | a.ldx | lddy) & 1);
   p.df = df; p.lddf = lddf; p.dx = dx; p.lddx = lddx; p.dh0 = dh0;
-  const dim3 threads(64 * waves_of(a.T)), grid((a.D + kChannels - 1) / kChannels, a.B, p.segments), summaries(grid.x, a.B, p.segments - 1);
+  const int waves = waves_of(a.T);
   auto go = [&](auto t) {
     using T = decltype(t);
-    auto lds = [&](int bytes) { return sizeof(T) == 2 ? (size_t)waves_of(a.T) * bytes : 0; };
-    if (p.segments > 1) scan_bwd_kernel<T, true><<<summaries, threads, lds(Ahead<2>::kBytes), s>>>(p);
-    scan_bwd_kernel<T, false><<<grid, threads, lds(Ahead<3>::kBytes), s>>>(p);
+    run(plan, p, [&](const Params& q, int64_t blocks, int segments, bool summaries) {
+      const dim3 grid((unsigned)blocks, 1, (unsigned)segments);
+      const auto lds = [&](int bytes) { return sizeof(T) == 2 ? (size_t)waves * bytes : 0; };
+      if (summaries) scan_bwd_kernel<T, true><<<grid, 64 * waves, lds(Ahead<2>::kBytes), s>>>(q);
+      else scan_bwd_kernel<T, false><<<grid, 64 * waves, lds(Ahead<3>::kBytes), s>>>(q);
+    });
   };
   if (a.dtype == kBF16) go(bf16{});
   else go(float{});

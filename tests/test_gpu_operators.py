@@ -536,6 +536,14 @@ def test_recurrence_layouts_and_missing_states(ctx, bf16):
     scan(ctx, 600, 5, 16, bf16)                                  # many short sequences: one segment
 
 
+@pytest.mark.parametrize("lens", [None, [800, 0, 31, 770]])
+def test_recurrence_of_more_blocks_than_units(ctx, lens):
+    """260 blocks of 64 channels: 256 of whole sequences, the others' sequences in segments."""
+    B, T, D = 65, 800, 250
+    assert 0 < pwb.scan_ws_floats(B, T, D) < 2 * 64 * 4 * 5
+    scan(ctx, B, T, D, True, lens=None if lens is None else (lens * 17)[:B], seed=3)
+
+
 def test_recurrence_states_in_place(ctx):
     """h_end over h0 and dh0 over dh_end, in one segment and in several."""
     for B, T, D in ((4, 1, 64), (1, 3000, 64), (5, 33, 70)):
