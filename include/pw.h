@@ -551,8 +551,9 @@ int64_t pw_f8_scale_bytes(int64_t rows, int64_t cols);
  * both outputs, as weights want it.  e is the smallest integer in [-127, 127] for which no finite element of the block
  * exceeds the format's largest value times 2^e (-127 for a block of zeros); elements are rounded to nearest, ties to even.
  * NaN stays NaN; infinities become NaN in e4m3 and stay infinities in e5m2; neither touches the scale of its block.
- * The scale tables are 4-byte aligned; q, qt 16-byte aligned, ldq >= cols and ldqt >= rows, both multiples of 16; rows are filled with zeros up to the next multiple
- * of 16 elements, so that this length can be the K of a product; bytes behind that are left as they were. */
+ * The scale tables are 4-byte aligned; q, qt 16-byte aligned, ldq >= cols and ldqt >= rows, both multiples of 16; rows are
+ * filled with zeros up to the next multiple of 16 elements, so that this length can be the K of a product; bytes behind that
+ * are left as they were.  Outputs overlap neither x nor each other. */
 typedef struct {
   int32_t dtype;             /* of x: PW_F32 or PW_BF16 */
   int32_t format;            /* pw_f8_format */
@@ -570,8 +571,8 @@ pw_status pw_op_f8_quantize(pw_ctx* ctx, const pw_f8_quantize_args* args);
 
 /* C[M, N] = A[M, K] . B[N, K]^T of two such operands (both contiguous along K), fp32 accumulation, and the epilogues
  * PW_EPI_STORE .. PW_EPI_GELU_BWD of pw_op_gemm with the same meaning (aux of PW_EPI_GELU_BWD is bf16; a residual and an
- * accumulating store need out_dtype PW_F32).  K, lda, ldb multiples of 16, ldc a multiple of 8, A, B, C, C2, aux, bias 16-byte
- * and the scale tables 4-byte aligned.  The table of an operand is the one of (rows, K).  With y = x W of the LM's layers, W
+ * accumulating store need out_dtype PW_F32).  M and N at most 2^26, K at most 2^30; K, lda, ldb multiples of 16, ldc a multiple
+ * of 8, A, B, C, C2, aux, bias 16-byte and the scale tables 4-byte aligned.  The table of an operand is the one of (rows, K).  With y = x W of the LM's layers, W
  * [in][out]: forward A = q(x), B = qt(W); data gradient A = q(dy), B = q(W); weight gradient dW = A = qt(x), B = qt(dy), K = the
  * rows of x rounded up to 16.  bf16 outputs come from the 8-bit matrix pipe, which drops what lies 2^-13 under the largest of eight
  * neighbouring products (1e-5 to 3e-5 of the result, in the norm); fp32 outputs come from the bf16 pipe, at half its rate, with
@@ -615,8 +616,8 @@ typedef struct {
 pw_status pw_op_dropout_fwd(pw_ctx* ctx, const pw_dropout_args* args, const void* x, const float* bias, const float* res, void* y);
 /* dx = keep dy / (1 - p) (the residual's gradient is dy itself); dbias: null, or fp32 [cols] that receives the column sums of
  * dx before its rounding (overwritten, or added into when accumulate = 1).  ws: fp32 workspace of
- * pw_dropout_bwd_ws_floats(rows, cols) floats if dbias is wanted (may be null where that is 0), else null.  dx may be the same array as dy where type and
- * stride are the same. */
+ * pw_dropout_bwd_ws_floats(rows, cols) floats if dbias is wanted (may be null where that is 0), else null.  dx may be the same
+ * array as dy where type and stride are the same. */
 pw_status pw_op_dropout_bwd(pw_ctx* ctx, const pw_dropout_args* args, const void* dy, void* dx, float* dbias, float* ws, int accumulate);
 int64_t pw_dropout_bwd_ws_floats(int64_t rows, int64_t cols);   /* -1 for impossible sizes */
 
@@ -630,7 +631,7 @@ typedef struct {
   const void* f;
   const void* x;
   int64_t ldf, ldx;
-  int32_t B, T, D;           /* B at most 65535, T at most 2^30, D at most 2^24 */
+  int32_t B, T, D;           /* B at most 65535, T at most 2^30, D and all strides at most 2^21 */
   const float* h0;           /* [B, D], or null: zeros */
   const int32_t* lens;       /* device, [B], or null: T everywhere.  Sequence b has lens[b] steps (clamped to 0 .. T); behind
                                 them y, df and dx are zero, the state stays, and what f, x and dy hold does not matter */
@@ -639,7 +640,8 @@ typedef struct {
  * backward call needs, or null; ws: workspace of pw_scan_ws_floats(B, T, D) floats (8-byte aligned; may be null where that is 0). */
 pw_status pw_op_scan_fwd(pw_ctx* ctx, const pw_scan_args* args, void* y, int64_t ldy, float* h_end, float* states, float* ws);
 /* Gradients from dy (rows lddy apart) and dh_end (fp32 [B, D], or null: zeros): df, dx rows lddf, lddx apart (they may be
- * columns of one array), dh0 fp32 [B, D] or null (may be the same array as dh_end).  args and states as in the forward call. */
+ * columns of one array), dh0 fp32 [B, D] or null (may be the same array as dh_end).  args and states as in the forward call.
+ * Of either call no output overlaps an input otherwise. */
 pw_status pw_op_scan_bwd(pw_ctx* ctx, const pw_scan_args* args, const void* dy, int64_t lddy, const float* dh_end,
                          const float* states, void* df, int64_t lddf, void* dx, int64_t lddx, float* dh0, float* ws);
 int64_t pw_scan_state_floats(int64_t B, int64_t T, int64_t D);   /* -1 for impossible sizes */

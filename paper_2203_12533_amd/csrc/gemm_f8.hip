@@ -471,10 +471,11 @@ hipError_t prepare_formats() {
   if (e == hipSuccess) e = prepare<MidOne, FA, FB, false>();
   return e == hipSuccess ? prepare_both<FA, FB, Mid, Half, Split, Few>() : e;
 }
+constexpr int64_t kMostThreads = (1LL << 32) - 1;     // of a launch
 template <class S, int FA, int FB, bool EXACT>
 hipError_t launch(hipStream_t s, GemmF8Params p) {
   const int64_t tm = (p.M + S::BM - 1) / S::BM, tn = (p.N + S::BN - 1) / S::BN;
-  if (tm * tn > (1LL << 26)) return hipErrorInvalidValue;
+  if (tm * tn * S::kThreads > kMostThreads) return hipErrorInvalidValue;
   p.tiles_m = (int)tm;
   p.tiles_n = (int)tn;
   gemm_f8_tile_kernel<S, FA, FB, EXACT><<<(int)(tm * tn), S::kThreads, S::kSmem, s>>>(p);
@@ -483,7 +484,7 @@ hipError_t launch(hipStream_t s, GemmF8Params p) {
 template <int W, int FA, int FB>
 hipError_t launch_direct(hipStream_t s, GemmF8Params p, bool exact) {
   const int64_t tm = (p.M + 15) / 16, tn = (p.N + 15) / 16;
-  if (tm * tn > (1LL << 30)) return hipErrorInvalidValue;
+  if (tm * tn * 64 * W > kMostThreads) return hipErrorInvalidValue;
   p.tiles_m = (int)tm;
   p.tiles_n = (int)tn;
   if (exact) gemm_f8_direct_kernel<W, FA, FB, true><<<(int)(tm * tn), 64 * W, 0, s>>>(p);
@@ -526,8 +527,8 @@ hipError_t gemm_f8_init() {
 }
 
 hipError_t launch_gemm_f8(hipStream_t s, const GemmF8Args& a) {
-  const int64_t most = 1LL << 30;
-  if (!a.A || !a.B || !a.a_scale || !a.b_scale || !a.C || a.M < 0 || a.N < 0 || a.K < 0 || a.M > most || a.N > most || a.K > most)
+  const int64_t most = 1LL << 26;
+  if (!a.A || !a.B || !a.a_scale || !a.b_scale || !a.C || a.M < 0 || a.N < 0 || a.K < 0 || a.M > most || a.N > most || a.K > (1LL << 30))
     return hipErrorInvalidValue;
   if ((a.a_format != kE4M3 && a.a_format != kE5M2) || (a.b_format != kE4M3 && a.b_format != kE5M2)) return hipErrorInvalidValue;
   if (a.epilogue < kEpiStore || a.epilogue > kEpiGeluBwd || (a.out_dtype != kF32 && a.out_dtype != kBF16)) return hipErrorInvalidValue;

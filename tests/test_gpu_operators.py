@@ -327,6 +327,32 @@ def test_f8_product_repeats_its_bits(ctx):
     assert torch.equal(x[0], x[1]) and torch.equal(x[0], x[2])
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("M,N", [(1, 40), (40, 70), (300, 200), (300, 2050), (1000, 760), (1500, 4096), (4096, 4096)])
+def test_products_over_nothing(ctx, M, N, bf16):
+    """K = 0: the bias alone, in every tile; with PW_EPI_STORE zeros, or what was there where the output accumulates."""
+    ldc = up(N, 8)
+    bias = torch.randn(ldc, device="cuda")
+    c = torch.full((M, ldc), 7.0, dtype=act(bf16), device="cuda")
+    q, s = torch.zeros(64, dtype=torch.uint8, device="cuda"), torch.zeros(64, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+
+    def run(epilogue, accumulate):
+        c.fill_(7.0)
+        torch.cuda.synchronize()
+        ctx.f8_gemm(pwb.F8GemmArgs(M=M, N=N, K=0, lda=0, ldb=0, ldc=ldc, epilogue=epilogue, out_dtype=pwb.PW_BF16 if bf16 else pwb.PW_F32,
+                                   accumulate=accumulate, A=q.data_ptr(), B=q.data_ptr(), a_scale=s.data_ptr(), b_scale=s.data_ptr(),
+                                   bias=bias.data_ptr(), C=c.data_ptr()))
+        ctx.synchronize()
+        assert (c[:, N:] == 7.0).all()
+        return c[:, :N]
+
+    assert (run(pwb.PW_EPI_BIAS, 0) == bias[:N].to(act(bf16))).all()
+    assert (run(pwb.PW_EPI_STORE, 0) == 0).all()
+    if not bf16:
+        assert (run(pwb.PW_EPI_STORE, 1) == 7.0).all()
+
+
 # ---- dropout ---------------------------------------------------------------------------------------------------
 
 def dropout(ctx, rows, cols, bf16, out_bf16, p, res=True, bias=True, seed=(1 << 40) + 17, site=3, step=11, step_dev=None, ldx=None,

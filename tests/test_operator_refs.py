@@ -117,6 +117,8 @@ int main() {
   REFUSE(G, g0, A = (char*)P + 8) REFUSE(G, g0, C = (char*)P + 8) REFUSE(G, g0, bias = (float*)((char*)P + 4)) REFUSE(G, g0, a_scale = S + 2)
   REFUSE(G, g0, epilogue = kEpiAdam) REFUSE(G, g0, epilogue = -1) REFUSE(G, g0, epilogue = kEpiBiasResidual) REFUSE(G, g0, epilogue = kEpiGeluBwd)
   REFUSE(G, g0, epilogue = kEpiBiasGelu) REFUSE(G, g0, out_dtype = kI32)
+  REFUSE(G, g0, M = (1LL << 26) + 1) REFUSE(G, g0, N = (1LL << 26) + 8)
+  { auto a = g0; a.M = a.N = a.ldc = 1LL << 26; expect("more tiles than a launch has", G, no); a.lda = 1LL << 24; expect("nor apart", G, no); }
   { auto a = g0; a.out_dtype = kBF16; a.accumulate = 1; expect("bf16 accumulate", G, no); }
   { auto a = g0; a.epilogue = kEpiBias; a.accumulate = 1; expect("bias accumulate", G, no); }
   { auto a = g0; a.epilogue = kEpiBiasResidual; a.aux = P; a.out_dtype = kBF16; expect("bf16 residual", G, no); }
@@ -142,6 +144,11 @@ int main() {
   REFUSE(SF, s0, dtype = kI32) REFUSE(SF, s0, f = nullptr) REFUSE(SF, s0, x = nullptr) REFUSE(SF, s0, ldf = 7) REFUSE(SB, s0, ldx = 7)
   REFUSE(SF, s0, B = -1) REFUSE(SF, s0, T = -1) REFUSE(SB, s0, D = -1) REFUSE(SF, s0, B = 65536) REFUSE(SF, s0, f = (char*)P + 1)
   REFUSE(SF, s0, h0 = (float*)((char*)P + 2)) REFUSE(SF, s0, lens = (int32_t*)((char*)P + 1)) REFUSE(SF, s0, D = (1 << 24) + 1)
+  REFUSE(SF, s0, D = (1 << 21) + 1) REFUSE(SF, s0, ldf = (1 << 21) + 1) REFUSE(SB, s0, ldx = (1 << 21) + 1)
+  { auto a = s0; const int64_t far = (1 << 21) + 1; expect("far y", launch_scan_fwd(nullptr, a, P, far, nullptr, nullptr, nullptr), no);
+    expect("far dy", launch_scan_bwd(nullptr, a, P, far, nullptr, F, P, 8, P, 8, nullptr, nullptr), no);
+    expect("far df", launch_scan_bwd(nullptr, a, P, 8, nullptr, F, P, far, P, 8, nullptr, nullptr), no);
+    expect("far dx", launch_scan_bwd(nullptr, a, P, 8, nullptr, F, P, 8, P, far, nullptr, nullptr), no); }
   { auto a = s0; expect("null y", launch_scan_fwd(nullptr, a, nullptr, 8, nullptr, nullptr, nullptr), no);
     expect("short ldy", launch_scan_fwd(nullptr, a, P, 7, nullptr, nullptr, nullptr), no);
     expect("no states", launch_scan_bwd(nullptr, a, P, 8, nullptr, nullptr, P, 8, P, 8, nullptr, nullptr), no);
