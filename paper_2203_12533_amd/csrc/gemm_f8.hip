@@ -73,9 +73,14 @@ template <class S> struct Finish {
 
 // One operand of a group's tile: R rows of 128 bytes, fetched by G waves in pieces of 1 KiB (8 rows); chunk c (16 bytes) of row
 // r lies at position c ^ ((r >> 1) & 7) of the row, so that the 16 rows of a fragment read hit all banks.
-template <int R, int G>
+// HALVES: the first half of a wave's pieces are the first 64 of each 128 rows.
+template <int R, int G, bool HALVES>
 struct Operand {
   static constexpr int kPer = R / 8 / G;
+  static_assert(!HALVES || (G == 8 && kPer == 4), "two times 128 rows");
+  __device__ __forceinline__ static int piece(int gw, int j) {
+    return HALVES ? (gw >> 2) * 16 + (j >> 1) * 8 + (gw & 3) * 2 + (j & 1) : gw * kPer + j;
+  }
   const uint8_t* base;
   uint32_t off[kPer];
   __device__ __forceinline__ static int k_of(int instr, int lane) { return ((lane & 7) ^ (((instr * 8 + (lane >> 3)) >> 1) & 7)) * 16; }
@@ -84,17 +89,18 @@ struct Operand {
     const int last = (int)(rows - row0 < R ? rows - row0 : R) - 1;     // rows past the end are fetched from the last one
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const int instr = gw * kPer + j, r = instr * 8 + (lane >> 3);
+      const int instr = piece(gw, j), r = instr * 8 + (lane >> 3);
       off[j] = (uint32_t)((r < last ? r : last) * (int)ld + k_of(instr, lane));
     }
   }
-  __device__ __forceinline__ void issue_one(int j, uint32_t lds_off, int gw) const { dma16_s(base, off[j], lds_off + (gw * kPer + j) * 1024); }
+  __device__ __forceinline__ void issue_one(int j, uint32_t lds_off, int gw) const { dma16_s(base, off[j], lds_off + piece(gw, j) * 1024); }
   // The next k tile, of which `left` bytes exist (a multiple of 16; whole, partial or none): the rest comes from zeros.
-  __device__ __forceinline__ void issue(int64_t left, uint32_t lds_off, int gw, int lane) const {
+  __device__ __forceinline__ void issue(int64_t left, uint32_t lds_off, int gw, int lane, int from = 0, int to = kPer) const {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
+      if (j < from || j >= to) continue;
       const uint8_t* const g = base + off[j];
-      dma16(k_of(gw * kPer + j, lane) < left ? g : reinterpret_cast<const uint8_t*>(kZeros), lds_off + (gw * kPer + j) * 1024);
+      dma16(k_of(piece(gw, j), lane) < left ? g : reinterpret_cast<const uint8_t*>(kZeros), lds_off + piece(gw, j) * 1024);
     }
   }
 };
@@ -213,8 +219,9 @@ template <int FA, int FB> __device__ __forceinline__ f32x4 mfma(const i32x8& b, 
 template <class S, int FA, int FB, bool EXACT>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_kernel(GemmF8Params p) {
   constexpr int FM = S::FM, FN = S::FN, G = S::G, WN = S::WN;
-  using OpA = Operand<S::BM, G>;
-  using OpB = Operand<S::BN, G>;
+  constexpr bool SPLIT = FM == 8;
+  using OpA = Operand<S::BM, G, SPLIT>;
+  using OpB = Operand<S::BN, G, false>;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   int tm, tn;
   tile_of_block(blockIdx.x, p.tiles_m * p.tiles_n, p.tiles_m, p.tiles_n, tm, tn);
@@ -245,18 +252,23 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_ke
   const bool of_a = word < S::kScalesA / 4;
   const int64_t sp_step = of_a ? Ra : Rb, sp_row = (of_a ? m0 & ~63LL : n0) + (w >> 4) * 64;
   const uint8_t* const sp = (of_a ? p.sa : p.sb) + (sp_row < sp_step - 64 ? sp_row : sp_step - 64) + (w & 15) * 4;
-  auto issue_scales = [&](int t, uint32_t st) {
-    const int kb = first + t < total ? first + t : total - 1;
-    dma4(sp + kb * sp_step, st + S::kOperands + gw % kSets * 256);
+  const uint8_t* sq = sp + first * sp_step;      // of the tile that is asked for next; the last one's again behind it
+  auto issue_scales = [&](int t, uint32_t st, bool last) {
+    dma4(sq, st + S::kOperands + gw % kSets * 256);
+    if (!last || first + t + 1 < total) sq += sp_step;
   };
-  auto issue = [&](int t, uint32_t at) {       // k tile t into the stage at `at`; zeros where it does not exist
+  // k tile t into the stage at `at`; zeros where it does not exist.  part: 1 all but the second half of A, 2 that, 0 both.
+  auto issue = [&](int t, uint32_t at, int part) {
     const int64_t left = p.K - (int64_t)(first + t) * kBK;
     const uint32_t st = ring + at;
-    oa.issue(left, st, gw, lane);
-    ob.issue(left, st + S::BM * kBK, gw, lane);
-    oa.base += kBK;
-    ob.base += kBK;
-    issue_scales(t, st);
+    if (part != 2) {
+      ob.issue(left, st + S::BM * kBK, gw, lane);
+      ob.base += kBK;
+      issue_scales(t, st, true);
+      oa.issue(left, st, gw, lane, 0, SPLIT ? OpA::kPer / 2 : OpA::kPer);
+    }
+    if (SPLIT && part != 1) oa.issue(left, st, gw, lane, OpA::kPer / 2);
+    if (!SPLIT || part != 1) oa.base += kBK;
   };
   // Addresses of this lane's fragments: block j of an operand is 16 j rows of 128 bytes further on, which leaves the swizzle
   // of the row as it is.
@@ -270,16 +282,24 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_ke
   auto word_a = [&](int v) { return FM % 4 ? v >> ((rows_at & 63) / 2) : v; };
   auto word_b = [&](int v) { return FN % 4 ? v >> ((cols_at & 63) / 2) : v; };
   constexpr int kPer = OpA::kPer + OpB::kPer, kLoads = kPer + 1;    // direct loads of a wave per k tile
-  // All but the direct loads of the `later` tiles asked for last are there, and this wave's LDS reads are done ...
-  auto landed = [&](auto later) { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(later)::value * kLoads) : "memory"); };
+  // All but the `later` direct loads asked for last are there, and this wave's LDS reads are done ...
+  auto landed = [&](auto later) { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(later)::value) : "memory"); };
   auto meet = [&] {                            // ... and those of the group's other waves
     if (G > 1) __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
   i32x8 fa[2], fb[FN];
   int sa[GA], sb[GB], nsa[GA], nsb[GB];
-  auto read_a = [&](uint32_t st, int i) { fa[i & 1] = read_fragment(a0 + st, a1 + st, i * 16 * kBK); };
-  auto read_b = [&](uint32_t st, int j) { fb[j] = read_fragment(b0 + st, b1 + st, j * 16 * kBK); };
+  // Addresses of a tile's fragments: kept whole, so that what is constant in them goes into the instructions.
+  struct At { uint32_t v[4]; };
+  auto at_of = [&](uint32_t st) {
+    At r{{a0 + st, a1 + st, b0 + st, b1 + st}};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(r.v[k]));
+    return r;
+  };
+  auto read_a = [&](const At& at, int i) { fa[i & 1] = read_fragment(at.v[0], at.v[1], i * 16 * kBK); };
+  auto read_b = [&](const At& at, int j) { fb[j] = read_fragment(at.v[2], at.v[3], j * 16 * kBK); };
   auto read_scale = [&](uint32_t st, int g) {
     if (g < GA) nsa[g] = read_scales(s_a + st + g * 64);
     else nsb[g - GA] = read_scales(s_b + st + (g - GA) * 64);
@@ -290,38 +310,53 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_ke
 #pragma unroll
     for (int g = 0; g < GB; ++g) sb[g] = word_b(nsb[g]);
   };
-  auto issue_one = [&](int t, int m, uint32_t at) {       // of the whole tile t
+  auto issue_one = [&](int t, int m, uint32_t at) {       // load m of the whole tile t
     const uint32_t st = ring + at;
-    if (m < OpA::kPer) oa.issue_one(m, st, gw);
-    else ob.issue_one(m - OpA::kPer, st + S::BM * kBK, gw);
-    if (m == kPer - 1) {
-      oa.base += kBK;
+    if (m < OpB::kPer) ob.issue_one(m, st + S::BM * kBK, gw);
+    else oa.issue_one(m - OpB::kPer, st, gw);
+    if (m == OpB::kPer - 1) {
       ob.base += kBK;
-      issue_scales(t, st);
+      issue_scales(t, st, false);
     }
+    if (m == kPer - 1) oa.base += kBK;
   };
   bf16x8 wa[EXACT ? 2 : 1][4], wb[EXACT ? FN : 1][4];
   auto byte_of = [](const int* w, int i) { return (w[i / 4] >> (8 * (i % 4))) & 255; };
   // MFMAs run across k tiles without a pause.  A unit is one block of rows against all columns of the wave.
-  //  8-bit pipe: the next block's fragments are read while a unit runs.  All of a tile has been asked for one unit before its
+  //  8-bit pipe: the next block's fragments are read while a unit runs.  All of a tile has been read from LDS one unit before its
   //    end; the next tile's columns take the place of this one's as those are used for the last time.
+  //  The same of 256 x 256, whose two stages fill LDS (SPLIT): the tile's columns and scales are in registers when it begins, so
+  //    halfway, where the waves meet once more, their place and that of the first half of its rows is free for tile t + 2; that of
+  //    the second half is at kTurn.  Loads are on their way for one and a half tiles then instead of one, and go out all the
+  //    time: 8192 x 8192 x 8192 428 -> 402 us; with all waits for them taken out it takes 400, without the loads 332.
   //  bf16 pipe: the next block is widened while a unit runs and the one after it read; the columns are widened between the MFMAs
-  //    of the first unit, and their bytes' registers are free from there on.  All of a tile has been asked for two units before
-  //    its end.
+  //    of the first unit, and their bytes' registers are free from there on.  All of a tile has been read two units before its
+  //    end.
   // There (kTurn) the waves meet, the next tile is there, and the stage of this one is free for tile t + NS, whose direct loads
   // go out between the MFMAs that are left.
+  // What bounds the largest: power.  8192 x 8192 x 8192 runs at 1.8 GHz, 69 of 100 cycles with an MFMA, 2.8 PFLOP/s; of its 392
+  // us the MFMAs alone take 292, reading fragments 40, bringing operands 70.  Addresses of fragments kept whole and a running
+  // pointer to the scales, fewer instructions between the MFMAs, won 4 of 100.  Four waves of 128 x 128, which read a third
+  // less from LDS, leave nothing to a SIMD while its wave waits: 395 us, and 139 instead of 130 with k = 2048.
   // STREAM: tile t + NS is a whole one; MORE: tile t + 1 exists (t + NS, where it does not, is made of zeros nobody reads).  No
   // branches inside: the compiler would move MFMAs past them.
   constexpr int kTurn = EXACT ? FM - 2 : FM - 1, kSlots = (FM - kTurn) * FN;
+  constexpr int kHalf = FM / 2 - 1, kSecond = SPLIT ? OpA::kPer / 2 : kPer, kFirst = kPer - kSecond;
   static_assert(FM % 2 == 0 && GA + GB <= FN && (!EXACT || 4 % FN == 0), "two fragments of rows in turn; a slot for each word of scales");
   auto tile = [&](int t, uint32_t st, uint32_t next, auto streaming, auto follows) {
     constexpr bool STREAM = decltype(streaming)::value, more = decltype(follows)::value;
+    const At here = at_of(st), there = at_of(next);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      if (i == kTurn && more) {
-        landed(std::integral_constant<int, S::NS - 2>{});
+      if (SPLIT && i == kHalf) {
+        landed(std::integral_constant<int, kLoads>{});
         meet();
-        if (!STREAM) issue(t + S::NS, st);
+        if (more && !STREAM) issue(t + S::NS, st, 1);
+      }
+      if (i == kTurn && more) {
+        landed(std::integral_constant<int, SPLIT ? kLoads : (S::NS - 2) * kLoads>{});
+        meet();
+        if (!STREAM) issue(t + S::NS, st, SPLIT ? 2 : 0);
       }
 #pragma unroll
       for (int jj = 0; jj < FN; ++jj) {
@@ -329,19 +364,24 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_ke
         const int j = (i & 1) || i == 0 ? jj : FN - 1 - jj, slot = (i - kTurn) * FN + jj;
         __builtin_amdgcn_sched_barrier(0);
         if (EXACT) {
-          if (i < FM - 2 && jj == 0) read_a(st, i + 2);
+          if (i < FM - 2 && jj == 0) read_a(here, i + 2);
         } else {                               // behind the first MFMA of a tile, so that its wait does not cover this
-          if (i < FM - 1 && jj == (i == 0 ? 1 : 0)) read_a(st, i + 1);
+          if (i < FM - 1 && jj == (i == 0 ? 1 : 0)) read_a(here, i + 1);
         }
         if (slot >= 0 && more) {
           if (slot < GA + GB) read_scale(next, slot);
-          if (slot == 0) read_a(next, 0);
-          if (EXACT && slot == FN) read_a(next, 1);
-          if (EXACT && (slot & 1)) read_b(next, slot >> 1);
+          if (slot == 0) read_a(there, 0);
+          if (EXACT && slot == FN) read_a(there, 1);
+          if (EXACT && (slot & 1)) read_b(there, slot >> 1);
           if (STREAM) {
 #pragma unroll
-            for (int m = slot * kPer / kSlots; m < (slot + 1) * kPer / kSlots; ++m) issue_one(t + S::NS, m, st);
+            for (int m = slot * kSecond / kSlots; m < (slot + 1) * kSecond / kSlots; ++m) issue_one(t + S::NS, kFirst + m, st);
           }
+        }
+        if (SPLIT && STREAM && i >= kHalf && i < kTurn) {
+          const int at = (i - kHalf) * FN + jj, slots = (kTurn - kHalf) * FN;
+#pragma unroll
+          for (int m = at * kFirst / slots; m < (at + 1) * kFirst / slots; ++m) issue_one(t + S::NS, m, st);
         }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (EXACT) {
@@ -360,7 +400,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_ke
           acc[i][j] = mfma<FA, FB>(fb[j], fa[i & 1], acc[i][j], j % 4, sb[j / 4], i % 4, sa[i / 4]);
           if (i == FM - 1 && more) {           // the column block's last use
             __builtin_amdgcn_sched_barrier(0);
-            read_b(next, j);
+            read_b(there, j);
           }
         }
       }
@@ -370,17 +410,18 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_ke
   };
   if (n > 0) {
 #pragma unroll
-    for (int i = 0; i < S::NS; ++i) issue(i, i * S::kStage);
-    landed(std::integral_constant<int, S::NS - 1>{});
+    for (int i = 0; i < S::NS; ++i) issue(i, i * S::kStage, 0);
+    landed(std::integral_constant<int, (S::NS - 1) * kLoads + (SPLIT ? kSecond : 0)>{});
     meet();
 #pragma unroll
     for (int g = 0; g < GA + GB; ++g) read_scale(0, g);
     take_scales();
-    read_a(0, 0);
+    const At here = at_of(0);
+    read_a(here, 0);
 #pragma unroll
-    for (int j = 0; j < FN; ++j) read_b(0, j);
+    for (int j = 0; j < FN; ++j) read_b(here, j);
     if constexpr (EXACT) {
-      read_a(0, 1);
+      read_a(here, 1);
 #pragma unroll
       for (int s = 0; s < 4; ++s) wa[0][s] = widen8<FA>(fa[0], s, byte_of(sa, 0));
     }
@@ -498,10 +539,11 @@ hipError_t launch_direct(hipStream_t s, GemmF8Params p, bool exact) {
 //   Few       256 x 2048 x 2048 6.1 (Split 7.1), 64 x 2048 x 8192 11.4 (16.0), fp32 7.6 (9.5); 512 x 2048 x 2048, two rounds, 10.5 (7.4)
 //   Split     512 x 2048 x 2048 7.4 (Half 9.7), 1024 x 1024 x 1024 6.0 (7.2), fp32 7.7 (9.9); 1024 x 2048 x 2048 13.6 (10.3)
 //   Half      1024 x 2048 x 2048 10.3 (Mid 14.8, MidOne 13.5), fp32 16.8 (20.5)
-//   MidOne    1024 x 4096 x 2048 14.8 (Mid 15.8, Half 15.5), 2048 x 2048 x 8192 37.8 (44.4, 43.5); fp32 66.2 (66.1, 72.7): left to Mid
-//   Mid       1500 x 4096 x 2048 19.7 (MidOne 27.2, Half 23.4, Big 31.0), fp32 32.1 (40.8, 35.3)
-//   Big       a round from 144 tiles on, 2304 x 4096 x 2048 30.1 (Mid 31.1), 2816 x 3840 x 8192 89 (96); beyond one where few of the last
-//             are idle: 384 tiles, 6144 x 4096 x 2048, 60.3 (58.2), 320 59.8 (53.4), 272 60.5 (50.1), 512, k = 512, 30.9 (33.7)
+//   MidOne    1024 x 4096 x 2048 14.8 (Mid 15.8, Half 15.5), 2048 x 2048 x 8192 34.6 (42.8, 43.5); fp32 66.2 (66.1, 72.7): left to Mid
+//   Mid       1500 x 4096 x 2048 20.1 (MidOne 24.7, Half 23.4, Big 27.6), fp32 32.1 (40.8, 35.3); 128 tiles of 256 x 256, 2048 x 4096 x 2048,
+//             22.9 (Big 27.2)
+//   Big       a round from 144 tiles on, 2304 x 4096 x 2048 27.5 (Mid 30.8), 2816 x 3840 x 8192 81 (97); beyond one where few of the last
+//             are idle: 272 tiles, 4352 x 4096 x 2048, 52.1 (46.4), 320 51.7 (46.2), 352 51.8 (52.0), 384 52.6 (53.6)
 template <int FA, int FB>
 hipError_t choose(hipStream_t s, const GemmF8Params& p, bool exact) {
   auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
@@ -512,7 +554,7 @@ hipError_t choose(hipStream_t s, const GemmF8Params& p, bool exact) {
   if (tiles(Half::BM, Half::BN) <= 256) return exact ? launch<Half, FA, FB, true>(s, p) : launch<Half, FA, FB, false>(s, p);
   if (exact) return launch<Mid, FA, FB, true>(s, p);
   const int64_t big = tiles(Big::BM, Big::BN), slots = (big + 255) / 256 * 256;
-  if (big <= 256 ? big >= 144 : 100 * big > 78 * slots) return launch<Big, FA, FB, false>(s, p);
+  if (big <= 256 ? big >= 144 : 100 * big > 72 * slots) return launch<Big, FA, FB, false>(s, p);
   return tiles(Mid::BM, Mid::BN) <= 256 ? launch<MidOne, FA, FB, false>(s, p) : launch<Mid, FA, FB, false>(s, p);
 }
 
