@@ -126,7 +126,7 @@ template <int FMT> __device__ __forceinline__ bf16x8 widen8(const i32x8& f, int 
 // Few rows, and rows too far apart for 32-bit offsets.  What bounds a product of few rows is reading B once, so nothing is
 // staged: a block owns 16 columns and 16 rows, its waves take every W-th k block, operands go from memory straight into
 // fragments (four lanes read 64 consecutive bytes of a row), kAhead blocks at a time, and the waves' sums meet
-// in LDS in wave order.  1 x 8192 x 2048: 5.4 us a pass, of which the launch is about 4.
+// in LDS in wave order.  1 x 8192 x 2048: 5.6 us a pass, of which the launch is about 4.
 constexpr int kAhead = 4;
 template <int W, int FA, int FB, bool EXACT>
 __global__ __launch_bounds__(64 * W) void gemm_f8_direct_kernel(GemmF8Params p) {
