@@ -570,6 +570,25 @@ def test_recurrence_of_more_blocks_than_units(ctx, lens):
     scan(ctx, B, T, D, True, lens=None if lens is None else (lens * 17)[:B], seed=3)
 
 
+def test_recurrence_step_of_more_blocks_than_a_launch_takes(ctx):
+    """65535 sequences of one step and 4160 channels: 4259775 blocks.  Rows from both ends and around the launches' border."""
+    B, D = 65535, 4160
+    g = torch.Generator(device="cuda").manual_seed(4)
+    f, x = (torch.randn(B, D, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    y = torch.full_like(f, 7.0)
+    torch.cuda.synchronize()
+    assert pwb.scan_ws_floats(B, 1, D) == 0
+    a = pwb.ScanArgs(dtype=pwb.PW_BF16, f=f.data_ptr(), x=x.data_ptr(), ldf=D, ldx=D, B=B, T=1, D=D)
+    ctx.scan_fwd(a, y.data_ptr(), D, None, None, None)
+    ctx.synchronize()
+    border = (1 << 22) // 65
+    rows = torch.tensor(list(range(40)) + list(range(border - 20, border + 20)) + list(range(B - 40, B)), device="cuda")
+    want = torch.sigmoid(-f[rows].double()) * x[rows].double()
+    # half a step of bf16 (2^-8) for the output, 2^-20 for what fp32 adds before it
+    assert ((y[rows].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -20) * want.abs() + 2.0 ** -120).all()
+    assert (y != 7.0).all()
+
+
 def test_recurrence_states_in_place(ctx):
     """h_end over h0 and dh0 over dh_end, in one segment and in several."""
     for B, T, D in ((4, 1, 64), (1, 3000, 64), (5, 33, 70)):
