@@ -45,9 +45,12 @@ __device__ __forceinline__ Philox philox(uint32_t c0, uint32_t c1, uint32_t c2, 
 
 struct Mask {
   uint32_t k0, k1, site, step, threshold;   // kept where the 16 bits are at least the threshold (0 .. 65536)
-  float scale;                              // 65536 / (65536 - threshold), 0 where everything is dropped
+  // 65536 / (65536 - threshold) in two parts, so that fp32 values are rounded once by it; 0 where everything is dropped.  The
+  // second is positive whatever the first: an infinity stays one.
+  float scale, rest;
   const uint32_t* step_dev;
 };
+__device__ __forceinline__ float scaled(const Mask& m, float v) { return __builtin_fmaf(v, m.scale, v * m.rest); }
 // Bit j: column j of the group is kept.
 __device__ __forceinline__ uint32_t keep_bits(const Mask& m, uint32_t step, uint32_t group, uint32_t row) {
   const Philox r = philox(group, row, m.site, step, m.k0, m.k1);
@@ -126,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void dropout_fwd_kernel(const T* x, const
     const uint32_t bits = keep_bits(m, step, (uint32_t)g, (uint32_t)r);
 #pragma unroll
     for (int j = 0; j < kGroup; ++j) {
-      const float k = (bits >> j) & 1u ? (v[j] + b[j]) * m.scale : 0.f;
+      const float k = (bits >> j) & 1u ? scaled(m, v[j] + b[j]) : 0.f;
       v[j] = RES ? e[j] + k : k;
     }
     store8(y + r * ldy + c, n, v);
@@ -167,7 +170,7 @@ __global__ __launch_bounds__(NT) void dropout_bwd_kernel(const TO* dy, T* dx, fl
       const uint32_t bits = keep_bits(m, step, (uint32_t)g, (uint32_t)r);
 #pragma unroll
       for (int j = 0; j < kGroup; ++j) {
-        v[j] = (bits >> j) & 1u ? v[j] * m.scale : 0.f;
+        v[j] = (bits >> j) & 1u ? scaled(m, v[j]) : 0.f;
         if (SUMS) sum[j] += v[j];
       }
       store8(dx + r * ldx + c, n, v);
@@ -214,7 +217,14 @@ Shape sum_shape(int64_t rows, int64_t cols) {
 bool mask_of(const DropoutArgs& a, Mask& m) {
   if (!(a.p >= 0.f && a.p <= 1.f)) return false;
   m.threshold = (uint32_t)(int)rintf(a.p * 65536.f);
-  m.scale = m.threshold < 65536 ? 65536.f / (float)(65536 - m.threshold) : 0.f;
+  m.scale = m.rest = 0.f;
+  if (m.threshold < 65536) {
+    const double whole = 65536.0 / (65536 - (int)m.threshold);
+    m.scale = (float)whole;
+    if (m.scale > whole) m.scale = nextafterf(m.scale, 0.f);
+    m.rest = (float)(whole - m.scale);
+    if (m.rest < 0x1p-126f) m.rest = 0x1p-126f;
+  }
   m.k0 = (uint32_t)a.seed;
   m.k1 = (uint32_t)(a.seed >> 32);
   m.site = a.site;
