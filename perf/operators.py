@@ -115,6 +115,9 @@ def _up(n, m):
 
 
 def prepare(case, seed):
+    if own:
+        _ctx()
+        _take_stream()                     # inputs are made on the stream that the operators run on
     c, r, fam = dict(case), _Draw(seed), case["family"]
     s = {"case": c}
     if fam == "gemm":
@@ -322,13 +325,23 @@ _context = _stream = None
 
 
 def _ctx():
-    """One context per program, as in any program that uses the library, on a stream of the program's."""
+    """One context per program, as in any program that uses the library, on a stream of the program's that is its current one from
+    here on: what makes inputs, the operators and what reads their outputs follow one another."""
     global _context, _stream
     if _context is None:
         from paper_2203_12533_amd import binding
         _stream = torch.cuda.Stream()
         _context = binding.Context(0, _stream.cuda_stream)
+        _take_stream()
     return _context
+
+
+def _take_stream():
+    """The program's stream is current, behind what is under way on the one that was.  A program that makes another one current
+    between this and a pass orders the two itself."""
+    if torch.cuda.current_stream() != _stream:
+        _stream.wait_stream(torch.cuda.current_stream())
+        torch.cuda.set_stream(_stream)
 
 
 def _buffers(s, c):
@@ -374,14 +387,14 @@ def _buffers(s, c):
 
 
 def _own_run(s, c):
+    ctx = _ctx()                           # first: buffers belong to the stream that is current then
     if "own" not in s:
         s["own"] = _buffers(s, c)
-    o, ctx, fam = s["own"], _ctx(), c["family"]
+    o, fam = s["own"], c["family"]
     p = lambda x: x.data_ptr() if x is not None else None  # noqa: E731
     if fam == "gemm":
         if c["epilogue"] == "add":
-            with torch.cuda.stream(_stream):
-                s["c"].copy_(s["c0"])
+            s["c"].copy_(s["c0"])
         ctx.f8_gemm(o["args"])
         out = s["c"][:, :c["n"]]
         return {"u": out, "h": o["c2"][:, :c["n"]]} if c["epilogue"] == "gelu" else {"c": out}
