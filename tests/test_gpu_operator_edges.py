@@ -51,3 +51,157 @@ def test_a_pass_comes_after_its_inputs_and_before_its_readers():
         if m._context is not None:
             m._context.close()
         torch.cuda.set_stream(before)
+
+
+# ---- quantisation ----------------------------------------------------------------------------------------------
+
+BF16_MAX = float.fromhex("0x1.fep127")
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("block", [1, 128])
+def test_bf16_quantisation_of_every_kind_of_value(ctx, fmt, block):
+    """As in fp32, with values that bf16 holds: zeros, subnormals, the largest numbers, maxima at a border of the scale, ties, scales
+    clamped at 2^-127, and NaN or infinities in either half of a word and in either row of a pair of rows."""
+    x = G.low(G.rnd(7, 140, 300), True)
+    x[3] = 0.0
+    x[4] = -0.0
+    x[5, :128] = 2.0 ** -133 * np.arange(1, 129)                  # subnormal in bf16: steps of 2^-133
+    x[6, :128] = 2.0 ** -133
+    x[7, 128:256] = BF16_MAX
+    x[8, 128:256] = -BF16_MAX
+    x[8, 0], x[8, 1:128] = 1.75, G.low(np.linspace(-1.7, 1.7, 127), True)
+    x[9, 0], x[9, 1:128] = 1.75 + 2.0 ** -7, G.low(np.linspace(-1.7, 1.7, 127), True)
+    grid = R.decode_table(fmt)[:128]
+    grid = grid[np.isfinite(grid)]
+    mid = ((grid[1:] + grid[:-1]) / 2)[-100:]
+    x[10, :mid.size], x[10, mid.size:128] = mid, R.TOP[fmt]       # ties, of at most five bits
+    x[11, :128] = mid[:128].repeat(2)[:128] * 2.0 ** -100
+    x[11, 0] = R.TOP[fmt] * 2.0 ** -100
+    for row, col, v in ((20, 4, np.nan), (23, 5, np.nan), (24, 138, np.inf), (27, 139, -np.inf), (30, 270, -np.inf), (33, 299, np.nan),
+                        (130, 0, np.inf), (139, 1, np.nan)):
+        x[row, col] = v
+        x[row, (col + 1) % 300], x[row ^ 1, col] = 3e30, -5e-30   # its neighbours are ordinary
+    x[40, :128] = np.nan
+    x[41, 128:256] = np.inf
+    x[42:44, 250:] = -np.inf
+    x[44, :128] = 2.0 ** -119 * np.linspace(0.01, 1.75, 128)      # around where the scale stops at 2^-127
+    x[45, :128] = 2.0 ** -119 * np.linspace(0.01, 1.76, 128)
+    x[46, :128] = 2.0 ** -112 * np.linspace(0.01, 1.75, 128)
+    x[47, :128] = 2.0 ** -125 * np.linspace(-1, 1.75, 128)
+    G.check_quantized(ctx, x, fmt, block, True)
+    G.check_quantized(ctx, x[:, :77], fmt, block, True, ldx=81, offset=1)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_quantisation_around_the_smallest_scale(ctx, fmt, bf16):
+    """Blocks whose scale is 2^-127 or next to it, each row a factor of two above the one before."""
+    x = G.rnd(3, 40, 256) * 2.0 ** (np.arange(40) - 140.0)[:, None]
+    G.check_quantized(ctx, x, fmt, 1, bf16)
+
+
+# ---- products --------------------------------------------------------------------------------------------------
+
+TILES = [(3, 200), (40, 200), (260, 300), (500, 1300), (1300, 1100), (1700, 1900), (2100, 2600), (2304, 4096)]
+
+
+def multiply(ctx, a, ea, b, eb, fa, fb, bf16, M, N, K):
+    """C of operands given as bytes and scale exponents (128 stands for the byte 255)."""
+    at, bt = (torch.from_numpy(np.ascontiguousarray(v)).cuda() for v in (a, b))
+    sa, sb = (torch.from_numpy(R.scale_table(e)).cuda() for e in (ea, eb))
+    ldc = G.up(N, 8)
+    c = torch.full((M, ldc), 7.0, dtype=G.act(bf16), device="cuda")
+    torch.cuda.synchronize()
+    ctx.f8_gemm(pwb.F8GemmArgs(a_format=G.F8[fa], b_format=G.F8[fb], M=M, N=N, K=K, lda=K, ldb=K, ldc=ldc, epilogue=pwb.PW_EPI_STORE,
+                               out_dtype=DT[bf16], A=at.data_ptr(), B=bt.data_ptr(), a_scale=sa.data_ptr(), b_scale=sb.data_ptr(),
+                               C=c.data_ptr()))
+    ctx.synchronize()
+    assert (c[:, N:] == 7.0).all()
+    return G.back(c[:, :N])
+
+
+def scaled(q, e, fmt):
+    """The operand's values in 64 bits; a block with the byte 255 is NaN, its zeros too."""
+    with np.errstate(invalid="ignore"):
+        return R.decode_table(fmt)[q] * np.where(e == 128, np.nan, 2.0 ** np.minimum(e, 127))[:, np.arange(q.shape[1]) // 128]
+
+
+def times(va, vb):
+    with np.errstate(invalid="ignore", over="ignore"):
+        return va @ vb.T
+
+
+SMALL = {"e4m3": [0x38, 0xB8, 0x40, 0xC0, 0x00, 0x80], "e5m2": [0x3C, 0xBC, 0x40, 0xC0, 0x00, 0x80]}      # 1, -1, 2, -2, 0, -0
+
+
+@pytest.mark.parametrize("fa,fb", [("e4m3", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("M,N", TILES)
+def test_sums_that_every_pipe_forms_exactly(ctx, M, N, bf16, fa, fb):
+    """Operands of 0, 1, 2 with scales of 1, 2 and 4 for each row and block: all products and sums are whole numbers under 2^13, so
+    nothing is cut off or rounded before the output is: every element is the one nearest to the result, in every tile."""
+    K = 400
+    rng = np.random.RandomState(M + N)
+    a, b = (np.array(SMALL[f], np.uint8)[rng.randint(0, 6, (n, K))] for n, f in ((M, fa), (N, fb)))
+    ea, eb = rng.randint(0, 3, (M, 4)), rng.randint(0, 3, (N, 4))
+    ref = times(scaled(a, ea, fa), scaled(b, eb, fb))
+    assert np.abs(ref).max() < 2 ** 13
+    assert np.array_equal(multiply(ctx, a, ea, b, eb, fa, fb, bf16, M, N, K), G.low(ref, bf16))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("M,N", TILES)
+def test_scale_bytes_at_both_ends(ctx, M, N, fmt, bf16):
+    """Bytes 0, 1, 253, 254 in single rows of either operand against scales that bring the result back into range, over zeros in the
+    other blocks; 255 makes its row (its column) NaN, over zeros too."""
+    K = 272
+    rng = np.random.RandomState(M)
+    a, b = (np.array(SMALL[fmt], np.uint8)[rng.randint(0, 6, (n, K))] for n in (M, N))
+    ea, eb = np.zeros((M, 3), int), np.zeros((N, 3), int)
+    # (byte - 127) of a row; with numbers of at most 2 on the other side at 2^0 .. 2^4 every product is a normal fp32 number
+    rows = rng.permutation(M)[:6] if M >= 6 else np.arange(M)
+    for r, e in zip(rows, (-127, 126, 128, -126, 127, 128)):
+        ea[r] = 0 if e == 128 else e
+        if e == 128:
+            ea[r, rng.randint(3)] = 128
+        if e == -127:
+            a[r] &= 0x80                        # +-2 only: 1 * 2^-127 is below what the bf16 pipe holds exactly
+            a[r] |= 0x40
+        if e in (126, 127):                     # one product: a sum would leave the range
+            a[r] = 0
+            a[r, 5] = SMALL[fmt][0]
+    b[:, 5] = SMALL[fmt][1]
+    cols = rng.permutation(N)[:2]
+    eb[cols[0], 2] = 128
+    b[cols[1]], eb[cols[1], 1] = 0, 128         # a column of zeros
+    va, vb = scaled(a, ea, fmt), scaled(b, eb, fmt)
+    ref, mag = times(va, vb), times(np.abs(va), np.abs(vb))
+    got = multiply(ctx, a, ea, b, eb, fmt, fmt, bf16, M, N, K)
+    # whole numbers of the smallest scale: exact up to the output's rounding; a result under 2^-126 may be taken as zero
+    tiny = np.abs(ref) < 2.0 ** -126
+    G.within(got, ref, np.where(tiny, 2.0 ** -126, G.EPS[bf16] * np.abs(ref)), "C")
+    assert np.isnan(ref[:, cols]).all() and (M < 6 or np.isnan(ref[rows[[2, 5]]]).all()) and np.isfinite(mag).any()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("M,N", TILES)
+def test_nan_and_infinite_operands(ctx, M, N, bf16):
+    """NaN (either format) and infinities (e5m2) stay in their row or column and follow the formula there; in the last, partial
+    block of k too."""
+    K = 400
+    rng = np.random.RandomState(N)
+    a = np.array(SMALL["e4m3"][:4], np.uint8)[rng.randint(0, 4, (M, K))]
+    b = np.array(SMALL["e5m2"], np.uint8)[rng.randint(0, 6, (N, K))]
+    a[0, 7], a[M - 1, K - 1] = 0x7F, 0xFF
+    cols = rng.permutation(N)[:7]
+    for c, (k, v) in zip(cols, ((0, 0x7C), (K - 1, 0xFC), (200, 0x7D), (130, 0xFF), (131, 0x7C), (255, 0xFC), (256, 0x7E))):
+        b[c, k] = v
+    b[cols[4], 140] = 0xFC                      # two infinities: a sum of one sign, or NaN
+    ea, eb = rng.randint(-2, 3, (M, 4)), rng.randint(-2, 3, (N, 4))
+    ref = times(scaled(a, ea, "e4m3"), scaled(b, eb, "e5m2"))
+    got = multiply(ctx, a, ea, b, eb, "e4m3", "e5m2", bf16, M, N, K)
+    G.within(got, ref, G.EPS[bf16] * np.abs(ref), "C")
+    keep = np.setdiff1d(np.arange(N), cols)
+    assert np.isfinite(got[1:M - 1][:, keep]).all() and (M < 4 or np.isinf(ref[1:M - 1][:, cols]).any())
