@@ -144,3 +144,57 @@ def scan_bwd(f, x, h0, dy, dh_end, lens=None):
         df[on, t] = g * (before - x[on, t]) * a * z
         r[on] = a * g
     return df, dx, r
+
+
+def scan_bounds(f, x, h0, dy, dh_end, lens=None):
+    """How far fp32 results may be off, element by element: allowances for y, h_end, df, dx, dh0 before y, df and dx are rounded.
+
+    With u = 2^-24.  The argument of exp2 is a rounded product with a rounded constant, so e^-f is off by 2 |f| u, and by 2 u of the
+    instruction (one unit in the last place); 1 + e^-f rounds, its reciprocal is good to 2 u: a is off by (1 - a) (2 |f| + 2) u + 3 u
+    and 1 - a, a product or a difference from the larger one, by (2 |f| + 2) u + 4 u.  A term of a state passes a product and an addition
+    in the thread's own chain, and two more wherever stretches of 16 steps and more meet: 4 u of the sum of magnitudes a step, and 16 u
+    once.  Errors fade as the state does, by a_t a step.  A gate under 2^-126 may come out as any number under it (exp2 gives 0 there), so
+    what it multiplies is off by 2^-126 of itself: 2^-120 in all, of 1 and of each magnitude, in every output."""
+    B, T, D = f.shape
+    u, tiny = 2.0 ** -24, 2.0 ** -120
+    lens = np.full(B, T) if lens is None else np.clip(lens, 0, T)
+    h0 = np.broadcast_to(np.asarray(h0, np.float64), (B, D))
+    a, z = _sigmoid(f), _sigmoid(-f)
+    da, dz = (z * (2 * np.abs(f) + 2) + 3) * u, (2 * np.abs(f) + 6) * u
+    with np.errstate(invalid="ignore", over="ignore"):
+        y, _ = scan_fwd(f, x, h0, lens)
+        m, e = np.abs(h0), np.zeros((B, D))
+        ey, eb = np.zeros((B, T, D)), np.zeros((B, T, D))        # of y; of the state in front of each step
+        for t in range(T):
+            on = t < lens
+            eb[:, t] = e + 16 * u * m + tiny * (1 + m)
+            v = z[on, t] * np.abs(x[on, t])
+            m2 = a[on, t] * m[on] + v
+            e[on] = a[on, t] * (e[on] + da[on, t] * m[on]) + dz[on, t] * v + 4 * u * m2
+            m[on] = m2
+            ey[on, t] = (e + 16 * u * m + tiny * (1 + m))[on]
+        eh = e + 16 * u * m + tiny * (1 + m)
+        n, e = np.abs(np.asarray(dh_end, np.float64)) * np.ones((B, D)), np.zeros((B, D))
+        edf, edx = np.zeros((B, T, D)), np.zeros((B, T, D))
+        for t in reversed(range(T)):
+            on = t < lens
+            before = y[on, t - 1] if t else h0[on]
+            gap = np.abs(before - x[on, t])
+            g = np.abs(dy[on, t]) + n[on]                        # bounds |g_t|
+            eg = e[on] + 16 * u * g + tiny * (1 + g)
+            edx[on, t] = z[on, t] * (eg + (dz[on, t] + 2 * u) * g) + tiny * (1 + g)
+            edf[on, t] = a[on, t] * z[on, t] * (eg * gap + g * (eb[on, t] + u * gap) + g * gap * (da[on, t] + dz[on, t] + 4 * u)
+                                                + eg * eb[on, t]) + tiny * (1 + g) * (1 + gap)
+            n[on] = a[on, t] * g
+            e[on] = a[on, t] * (e[on] + da[on, t] * g) + 4 * u * a[on, t] * g
+        return ey, eh, edf, edx, e + 16 * u * n + tiny * (1 + n)
+
+
+def exceeds(got, ref, allow, half_step=0.0):
+    """Where `got` is off by more than `allow` and a rounding of half_step on top: NaN and infinities have to be the same ones.  Steps
+    stop shrinking at 2^-126 (bf16: 2^-133 apart below it, half of which is 2^-8 * 2^-126; fp32: 2^-149, half is 2^-24 * 2^-126)."""
+    got, ref = np.asarray(got, np.float64), np.asarray(ref, np.float64)
+    fin = np.isfinite(ref)
+    with np.errstate(invalid="ignore", over="ignore"):
+        bad = ~(np.abs(got - ref) <= allow + half_step * np.maximum(np.abs(ref) + allow, 2.0 ** -126))
+    return np.where(fin, bad, ~((got == ref) | (np.isnan(got) & np.isnan(ref))))

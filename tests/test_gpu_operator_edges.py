@@ -205,3 +205,71 @@ def test_nan_and_infinite_operands(ctx, M, N, bf16):
     G.within(got, ref, G.EPS[bf16] * np.abs(ref), "C")
     keep = np.setdiff1d(np.arange(N), cols)
     assert np.isfinite(got[1:M - 1][:, keep]).all() and (M < 4 or np.isinf(ref[1:M - 1][:, cols]).any())
+
+
+# ---- gated recurrence ------------------------------------------------------------------------------------------
+
+def recur(ctx, f, x, h0, dy, dh, lens, bf16):
+    """-> y, h_end, df, dx, dh0 of f, x, dy [B, T, D] (values that the type holds)."""
+    B, T, D = f.shape
+    dt = G.act(bf16)
+    flat = lambda v: torch.from_numpy(np.ascontiguousarray(v, np.float32)).reshape(B * T, D).to(dt).cuda()  # noqa: E731
+    ft, xt, dyt = flat(f), flat(x), flat(dy)
+    h0t, dht = (torch.from_numpy(v.astype(np.float32)).cuda() for v in (h0, dh))
+    lt = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    y, df, dx = (torch.full((B * T, D), 7.0, dtype=dt, device="cuda") for _ in range(3))
+    he, dh0 = (torch.full((B, D), 7.0, device="cuda") for _ in range(2))
+    states = torch.full((max(1, pwb.scan_state_floats(B, T, D)),), float("nan"), device="cuda")
+    ws = torch.full((max(2, pwb.scan_ws_floats(B, T, D)),), float("nan"), device="cuda")
+    torch.cuda.synchronize()
+    a = pwb.ScanArgs(dtype=DT[bf16], f=ft.data_ptr(), x=xt.data_ptr(), ldf=D, ldx=D, B=B, T=T, D=D, h0=h0t.data_ptr(),
+                     lens=lt.data_ptr() if lt is not None else None)
+    ctx.scan_fwd(a, y.data_ptr(), D, he.data_ptr(), states.data_ptr(), ws.data_ptr())
+    ctx.scan_bwd(a, dyt.data_ptr(), D, dht.data_ptr(), states.data_ptr(), df.data_ptr(), D, dx.data_ptr(), D, dh0.data_ptr(), ws.data_ptr())
+    ctx.synchronize()
+    return tuple(G.back(v).reshape(s) for v, s in ((y, f.shape), (he, h0.shape), (df, f.shape), (dx, f.shape), (dh0, h0.shape)))
+
+
+NAMES = ("y", "h_end", "df", "dx", "dh0")
+
+
+def check_recurrence(ctx, f, x, h0, dy, dh, lens, bf16, names=NAMES):
+    f, x, dy = (G.low(v, bf16) for v in (f, x, dy))
+    h0, dh = (np.asarray(v, np.float32).astype(np.float64) for v in (h0, dh))
+    n = None if lens is None else np.array(lens)
+    with np.errstate(invalid="ignore", over="ignore"):
+        (y, he), (df, dx, dh0) = R.scan_fwd(f, x, h0, n), R.scan_bwd(f, x, h0, dy, dh, n)
+        ey, eh, edf, edx, edh = R.scan_bounds(f, x, h0, dy, dh, n)
+    got = dict(zip(NAMES, recur(ctx, f, x, h0, dy, dh, lens, bf16)))
+    half = G.EPS[bf16]
+    for name, ref, allow in (("y", y, ey), ("h_end", he, eh), ("df", df, edf), ("dx", dx, edx), ("dh0", dh0, edh)):
+        if name not in names:
+            continue
+        bad = R.exceeds(got[name], ref, allow, 0.0 if name in ("h_end", "dh0") else half)
+        at = np.argwhere(bad)[:3]
+        assert not bad.any(), (name, bad.mean(), [(tuple(i), got[name][tuple(i)], ref[tuple(i)]) for i in at])
+    return y, he, df, dx, dh0
+
+
+RUNS = [(1, 1, 1, None), (8, 1, 200, None), (2, 9, 30, None), (1, 17, 65, None), (2, 256, 64, None), (1, 257, 70, None), (1, 1000, 130, None),
+        (1, 4097, 8, None), (2, 2000, 3, None), (3, 1030, 70, [0, 513, 1030]), (3, 520, 70, [-3, 900, 255]), (1, 3000, 66, None),
+        (2, 600, 64, None), (65, 800, 250, None), (65, 800, 250, "mixed"), (3, 16384, 64, [16384, 9000, 77])]
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("B,T,D,lens", RUNS)
+def test_every_element_of_a_recurrence(ctx, B, T, D, lens, bf16):
+    lens = ([800, 0, 31, 770] * 17)[:B] if lens == "mixed" else lens
+    rng = np.random.RandomState(T + D)
+    f, x, dy = rng.randn(B, T, D) * 1.5 + 1, rng.randn(B, T, D), rng.randn(B, T, D)
+    check_recurrence(ctx, f, x, rng.randn(B, D), dy, rng.randn(B, D), lens, bf16)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("size", [20.0, 60.0, 80.0])
+def test_gates_far_from_zero(ctx, size, bf16):
+    """Gates near 0 or 1, each to the precision that the bound gives it."""
+    rng = np.random.RandomState(int(size))
+    B, T, D = 2, 700, 66
+    f = np.where(rng.rand(B, T, D) < 0.5, 1.0, -1.0) * size * (0.9 + 0.1 * rng.rand(B, T, D))
+    check_recurrence(ctx, f, rng.randn(B, T, D), rng.randn(B, D), rng.randn(B, T, D), rng.randn(B, D), None, bf16)

@@ -197,3 +197,68 @@ def test_argument_structures_match_the_header(tmp_path):
     got = [int(v) for v in subprocess.check_output([str(tmp_path / "s")], text=True).split()]
     want = [n for _, py in structs for n in [C.sizeof(py)] + [getattr(py, f[0]).offset for f in py._fields_]]
     assert got == want
+
+
+def bf16(a):
+    from paper_2203_12533_amd import inputs as I
+    return I.round_to_bf16(np.asarray(a, np.float32)).astype(np.float64)
+
+
+@pytest.mark.parametrize("B,T,D,lens", [(1, 1000, 130, None), (1, 4097, 8, None), (2, 2000, 3, None), (3, 1030, 70, [0, 513, 1030]), (1, 3000, 66, None),
+                                        (3, 520, 70, [-3, 900, 255]), (2, 600, 64, None), (5, 800, 25, None)])
+def test_recurrence_bounds_reject_mistakes(B, T, D, lens):
+    """The allowances for bf16 outputs let through results in fp32 and reject zeros, flipped signs, and a state or a gradient that is
+    lost where tiles of 256 steps or segments of them meet."""
+    rng = np.random.RandomState(T)
+    f, x, dy = (bf16(v) for v in (rng.randn(B, T, D) * 1.5 + 1, rng.randn(B, T, D), rng.randn(B, T, D)))
+    h0, dh = rng.randn(2, B, D).astype(np.float32).astype(np.float64)
+    lens = None if lens is None else np.array(lens)
+    y, he = R.scan_fwd(f, x, h0, lens)
+    df, dx, dh0 = R.scan_bwd(f, x, h0, dy, dh, lens)
+    ey, eh, edf, edx, edh = R.scan_bounds(f, x, h0, dy, dh, lens)
+    half = R.HALF_STEP["bf16"]
+    # fp32, step by step
+    n = np.full(B, T) if lens is None else np.clip(lens, 0, T)
+    h, hs, f4, x4, dy4 = h0.astype(np.float32), [], f.astype(np.float32), x.astype(np.float32), dy.astype(np.float32)
+    one = np.float32(1)
+    for t in range(T):
+        hs.append(h)
+        on = (t < n)[:, None]
+        h = np.where(on, (h + np.exp(-f4[:, t]) * x4[:, t]) / (one + np.exp(-f4[:, t])), h).astype(np.float32)
+    y4 = np.stack(hs[1:] + [h], 1) * (np.arange(T) < n[:, None])[:, :, None]
+    assert not R.exceeds(bf16(y4), y, ey, half).any() and not R.exceeds(h, he, eh).any()
+    r, df4, dx4 = dh.astype(np.float32), np.zeros((B, T, D), np.float32), np.zeros((B, T, D), np.float32)
+    for t in reversed(range(T)):
+        on = (t < n)[:, None]
+        a, z, g = one / (one + np.exp(-f4[:, t])), one / (one + np.exp(f4[:, t])), dy4[:, t] + r
+        df4[:, t], dx4[:, t] = np.where(on, g * (hs[t] - x4[:, t]) * a * z, 0), np.where(on, g * z, 0)
+        r = np.where(on, a * g, r).astype(np.float32)
+    assert not R.exceeds(bf16(df4), df, edf, half).any() and not R.exceeds(bf16(dx4), dx, edx, half).any()
+    assert not R.exceeds(r, dh0, edh).any()
+    # mistakes
+    for ref, allow in ((y, ey), (df, edf), (dx, edx)):
+        live = ref != 0
+        for wrong in (np.zeros_like(ref), -ref):
+            assert R.exceeds(bf16(wrong), ref, allow, half)[live].mean() > 0.99
+    for cut in range(256, T, 256):
+        b = int(np.argmax(n))
+        if n[b] <= cut:
+            continue
+        late = [v[b:b + 1, cut:n[b]] for v in (f, x, dy)]
+        early = [v[b:b + 1, :cut] for v in (f, x, dy)]
+        zero = np.zeros((1, D))
+        wrong_y = R.scan_fwd(late[0], late[1], zero)[0]
+        assert R.exceeds(bf16(wrong_y), y[b:b + 1, cut:n[b]], ey[b:b + 1, cut:n[b]], half).any()
+        wrong_df, _, _ = R.scan_bwd(late[0], late[1], zero, late[2], dh[b:b + 1])
+        assert R.exceeds(bf16(wrong_df), df[b:b + 1, cut:n[b]], edf[b:b + 1, cut:n[b]], half).any()
+        for wrong, ref, allow in zip(R.scan_bwd(early[0], early[1], h0[b:b + 1], early[2], zero), (df, dx), (edf, edx)):
+            assert R.exceeds(bf16(wrong), ref[b:b + 1, :cut], allow[b:b + 1, :cut], half).any()
+
+
+def test_exceeds_tells_infinities_and_nan_apart():
+    ref = np.array([1.0, np.inf, -np.inf, np.nan, 0.0])
+    assert not R.exceeds(ref, ref, 0.0).any()
+    for i, v in ((0, np.nan), (0, np.inf), (1, np.nan), (1, -np.inf), (1, 3e38), (2, np.inf), (3, 0.0), (3, np.inf), (4, np.nan), (4, 1e-30)):
+        got = ref.copy()
+        got[i] = v
+        assert R.exceeds(got, ref, 0.0).tolist() == [k == i for k in range(5)]
