@@ -625,7 +625,9 @@ int64_t pw_dropout_bwd_ws_floats(int64_t rows, int64_t cols);   /* -1 for imposs
  * h_t = a_t h_(t-1) + (1 - a_t) x_t with a_t = sigmoid(f_t), element by element over D channels, y_t = h_t, from h_0: it mixes
  * positions as attention does, in time linear in their number and with a state of one row.  Sequence b has its steps in rows
  * b T .. b T + T - 1 of f, x (and y, dy, df, dx); f and x may be columns of one array ([F|X] of one projection).  T = 1 with h0
- * and h_end (they may be one array) is a decoding step.  State and sums are fp32. */
+ * and h_end (they may be one array) is a decoding step.  State and sums are fp32.  a_t stays above 2^-126 and 1 - a_t at or above
+ * 2^-149, for infinite f_t too: an infinity in h_0, x, dy or dh_end passes every gate as it passes any positive number, at whatever
+ * distance (df alone is NaN where an infinite h_(t-1) - x_t meets g_t a_t (1 - a_t) below 2^-149). */
 typedef struct {
   int32_t dtype;             /* of f, x, y, dy, df, dx: PW_F32 or PW_BF16 */
   const void* f;

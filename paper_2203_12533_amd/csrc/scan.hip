@@ -72,20 +72,28 @@ struct Params {
 template <class T> struct Raw;
 template <> struct Raw<bf16> { typedef __bf16 type __attribute__((ext_vector_type(kVec), aligned(2))); };
 template <> struct Raw<float> { typedef float type __attribute__((ext_vector_type(kVec), aligned(4))); };
-// a = sigmoid(f) and z = 1 - a, each to full relative precision.
+// Gates and their products are positive, as sigmoid and its products are: where one falls below what fp32 holds it stays there, so
+// that an infinite state is one behind it too (0 times it would be NaN).  Of a finite one a shut gate leaves 2^-125.
+constexpr float kLeast = 0x1p-149f;
+__device__ __forceinline__ float positive(float p) { return __builtin_fmaxf(p, kLeast); }
+// e^-f, at most 2^125, whose reciprocal is not yet cut to 0; NaN with f.  Off by 2 |f| 2^-24 of itself: the argument is rounded.
+__device__ __forceinline__ float decay(float f) {
+  return __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(-1.4426950408889634f * f, 125.f));
+}
+// a = sigmoid(f) and z = 1 - a; neither comes from a difference that cancels.
 __device__ __forceinline__ void gate(float f, float& a, float& z) {
-  const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * f);
+  const float e = decay(f);
   a = __builtin_amdgcn_rcpf(1.f + e);
-  z = e > 1.f ? 1.f - a : e * a;               // e may be infinite, or NaN with f
+  z = __builtin_fmaf(e, a, kLeast);
 }
 // The same in one register: the smaller of the two, negative where that is a.  The other one is 1 minus it, to half a unit.
 __device__ __forceinline__ float packed_gate(float f) {
-  const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * f), a = __builtin_amdgcn_rcpf(1.f + e);
-  return e > 1.f ? -a : e * a;
+  const float e = decay(f), a = __builtin_amdgcn_rcpf(1.f + e);
+  return e > 1.f ? -a : __builtin_fmaf(e, a, kLeast);
 }
 __device__ __forceinline__ void unpack_gate(float g, float& a, float& z) {
   const float other = 1.f - __builtin_fabsf(g);
-  const bool of_a = (int)__float_as_uint(g) < 0;                  // -0 is an a of zero
+  const bool of_a = (int)__float_as_uint(g) < 0;
   a = of_a ? -g : other;
   z = of_a ? other : g;
 }
@@ -213,7 +221,7 @@ template <int DIRS> __device__ __forceinline__ Map<DIRS> joined(const Map<DIRS>&
   Map<DIRS> r;
 #pragma unroll
   for (int j = 0; j < kVec; ++j) {
-    r.p[j] = mine.p[j] * other.p[j];
+    r.p[j] = positive(mine.p[j] * other.p[j]);
     auto after = [&](float first, float p, float s) { return __builtin_fmaf(p, first, s); };
     if (DIRS & kDown) {
       constexpr int d = sum_of<DIRS, kDown>();
@@ -266,11 +274,13 @@ __device__ __forceinline__ void compose(Map<DIRS>* slot, const Where& w, const M
 __device__ __forceinline__ float2* maps_of(const Params& p, const Where& w) {
   return p.maps + (int64_t)blockIdx.x * p.segments * kChannels + w.li * kVec;
 }
-// What reaches segment `seg`: the maps of the slots 0 .. seg (down) or segments - 1 .. seg (up), the first of which is a
-// constant.  Each part of a wave composes a stretch of them, then they meet as they do in a tile.
+// What reaches segment `seg`: the maps of the slots 1 .. seg (down) or segments - 2 .. seg (up), the first of which is a
+// constant: what leaves the first (last) segment.  That one has a slot to itself, 0 (segments - 1), with what comes in.  Each part of
+// a wave composes a stretch of them, then they meet as they do in a tile.
 template <int D>
 __device__ __forceinline__ void segment_carry(Map<D>* slot, const Where& w, const Params& p, int seg, float (&carry)[kVec]) {
-  const int subs = kParts * w.nw, n = D == kDown ? seg + 1 : p.segments - seg, per = (n + subs - 1) / subs;
+  const int subs = kParts * w.nw, from = D == kDown && seg > 0 ? 1 : seg;
+  const int n = D == kDown ? seg + 1 - from : (seg < p.segments - 1 ? p.segments - 1 - seg : 1), per = (n + subs - 1) / subs;
   Map<D> m;
 #pragma unroll
   for (int j = 0; j < kVec; ++j) {
@@ -281,13 +291,13 @@ __device__ __forceinline__ void segment_carry(Map<D>* slot, const Where& w, cons
   for (int i = 0; i < per; ++i) {
     const int k = D == kDown ? w.sub * per + i : n - 1 - ((subs - 1 - w.sub) * per + i);
     if (D == kDown ? k < n : k >= 0) {
-      const float2* q = maps_of(p, w) + (D == kDown ? k : seg + k) * kChannels;
+      const float2* q = maps_of(p, w) + (from + k) * kChannels;
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
         if (j < w.n) {
           const float2 v = q[j];
           m.s[0][j] = __builtin_fmaf(v.x, m.s[0][j], v.y);
-          m.p[j] *= v.x;
+          m.p[j] = positive(m.p[j] * v.x);
         }
       }
     }
@@ -449,6 +459,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void scan_fwd_kernel(Params p) 
         m.s[0][j] = __builtin_fmaf(a[i][j], m.s[0][j], v[i][j]);
         m.p[j] *= a[i][j];
       }
+      m.p[j] = positive(m.p[j]);
     }
     float before[kVec];
 #pragma unroll
@@ -459,7 +470,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 4) void scan_fwd_kernel(Params p) 
     if constexpr (SUMMARY) {
       for (int i = 0; i < w.nw; ++i)
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) prod[j] *= slot[i * kLanes + w.li].p[j];
+        for (int j = 0; j < kVec; ++j) prod[j] = positive(prod[j] * slot[i * kLanes + w.li].p[j]);
     } else {
       auto emit = [&](auto full) {
 #pragma unroll
@@ -563,6 +574,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 2) void scan_bwd_kernel(Params p) 
         up = a * ((float)rd[i][j] + up);
         m.p[j] *= a;
       }
+      m.p[j] = positive(m.p[j]);
       m.s[sum_of<DIRS, kUp>()][j] = up;
       if constexpr (!SUMMARY) {
 #pragma unroll
@@ -581,7 +593,7 @@ __global__ __launch_bounds__(64 * kMostWaves, 2) void scan_bwd_kernel(Params p) 
     if constexpr (SUMMARY) {
       for (int i = 0; i < w.nw; ++i)
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) prod[j] *= slot[i * kLanes + w.li].p[j];
+        for (int j = 0; j < kVec; ++j) prod[j] = positive(prod[j] * slot[i * kLanes + w.li].p[j]);
     } else {
       float before[kSteps][kVec], a, z;
 #pragma unroll

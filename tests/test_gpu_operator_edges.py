@@ -273,3 +273,67 @@ def test_gates_far_from_zero(ctx, size, bf16):
     B, T, D = 2, 700, 66
     f = np.where(rng.rand(B, T, D) < 0.5, 1.0, -1.0) * size * (0.9 + 0.1 * rng.rand(B, T, D))
     check_recurrence(ctx, f, rng.randn(B, T, D), rng.randn(B, D), rng.randn(B, T, D), rng.randn(B, D), None, bf16)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("shift", [-6.0, -2.0, 0.0, 3.0])
+@pytest.mark.parametrize("B,T,D,lens", [(4, 1, 66, None), (2, 40, 66, None), (1, 300, 70, None), (3, 1030, 70, [0, 513, 1030]), (1, 4097, 64, None),
+                                        (1, 16384, 34, None)])
+def test_infinite_states_inputs_and_gradients(ctx, B, T, D, lens, shift, bf16):
+    """An infinity stays one whatever the gates behind it (their product over a tile is far below the smallest number), meets another
+    of either sign as the formula has it, and what lies in front of it is finite."""
+    rng = np.random.RandomState((T + int(shift)) % 2 ** 32)
+    f, x, dy = rng.randn(B, T, D) + shift, rng.randn(B, T, D), rng.randn(B, T, D)
+    h0, dh = rng.randn(B, D), rng.randn(B, D)
+    h0[:, 0], h0[:, 1], h0[:, 2] = np.inf, -np.inf, np.nan
+    dh[:, 3], dh[:, 4], dh[:, 5] = np.inf, -np.inf, np.nan
+    for c in range(6, 14):                               # somewhere in the sequence
+        x[:, rng.randint(T), c] = np.inf if c % 2 else -np.inf
+    for c in range(12, 20):
+        dy[:, rng.randint(T), c] = np.inf if c % 2 else -np.inf
+    x[:, T // 3, 20], x[:, T // 2, 20] = np.inf, -np.inf
+    x[:, T // 3, 21], dy[:, T // 2, 21] = np.nan, np.nan
+    f[:, T // 2, 22] = np.nan
+    y, he, df, dx, dh0 = check_recurrence(ctx, f, x, h0, dy, dh, lens, bf16)
+    assert np.isinf(he[:, :2]).all() and np.isinf(dh0[:, 3:5]).all()
+    assert np.isfinite(y[:, :, 23:]).all() and np.isfinite(df[:, :, 23:]).all()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("size", [90.0, 100.0, 200.0, 600.0])
+def test_infinities_and_gates_beyond_what_fp32_holds(ctx, size, bf16):
+    """Gates of 1e-39 to 1e-260: an infinite state passes them, and an infinite input."""
+    rng = np.random.RandomState(int(size))
+    B, T, D = 2, 600, 66
+    f = np.where(rng.rand(B, T, D) < 0.5, 1.0, -1.0) * size
+    x, h0, dh = rng.randn(B, T, D), rng.randn(B, D), rng.randn(B, D)
+    h0[:, 0], h0[:, 1], dh[:, 2], dh[:, 3] = np.inf, -np.inf, np.inf, -np.inf
+    for c in range(4, 24):
+        x[:, rng.randint(T), c] = np.inf if c % 2 else -np.inf
+    _, he, _, _, dh0 = check_recurrence(ctx, f, x, h0, rng.randn(B, T, D), dh, None, bf16, ("y", "h_end", "dx", "dh0"))
+    assert np.isinf(he[:, :2]).all() and np.isinf(he[:, 4:24]).all() and np.isinf(dh0[:, 2:4]).all()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("T", [1, 40, 3000])
+def test_gates_that_are_shut_or_open_for_good(ctx, T, bf16):
+    """f of either infinity: the state is the input, or stays; no more than 2^-125 of anything else comes through, within what a gate
+    is rounded by (exp2 and the reciprocal by one unit in the last place each, the product: 5 * 2^-24 < 2^-21)."""
+    rng = np.random.RandomState(T)
+    B, D = 2, 66
+    f, x, dy = np.where(np.arange(D) % 2, np.inf, -np.inf) * np.ones((B, T, D)), G.low(rng.randn(B, T, D), bf16), rng.randn(B, T, D)
+    x[:, ::3] = 0.0
+    h0, dh = rng.randn(B, D), rng.randn(B, D)
+    y, he, df, dx, dh0 = recur(ctx, f, x, h0, G.low(dy, bf16), dh, None, bf16)
+    h0, dh = (v.astype(np.float32).astype(np.float64) for v in (h0, dh))
+    dy = G.low(dy, bf16)
+    shut = 2.0 ** -125 * (1 + 2.0 ** -21)
+    least = shut * 8                                             # of states and gradients of up to 8
+    live = x[:, :, ::2] != 0
+    assert np.array_equal(y[:, :, ::2][live], x[:, :, ::2][live]) and (np.abs(y[:, :, ::2][~live]) <= least).all()
+    assert np.array_equal(he[:, 1::2], h0[:, 1::2]) and np.array_equal(y[:, :, 1::2], np.broadcast_to(G.low(h0, bf16)[:, None, 1::2], (B, T, D // 2)))
+    total = np.abs(dy).sum(1) + np.abs(dh)
+    assert (np.abs(df) <= least * total[:, None]).all() and (np.abs(dx[:, :, 1::2]) <= shut * total[:, None, 1::2]).all()
+    assert (np.abs(dh0[:, ::2]) <= shut * total[:, ::2]).all()
+    want = dh[:, 1::2] + dy[:, :, 1::2].sum(1)
+    assert (np.abs(dh0[:, 1::2] - want) <= 2.0 ** -24 * 2 * T * total[:, 1::2]).all()
