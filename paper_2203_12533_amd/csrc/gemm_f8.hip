@@ -33,6 +33,21 @@ struct GemmF8Params {
   EpiParams epi;
 };
 
+// EXACT kernels have fp32 outputs and the others bf16 ones, which take neither a residual nor an old value: the rest is not compiled.
+template <bool EXACT> __device__ __forceinline__ void narrow(EpiParams& e) {
+  e.out_bf16 = !EXACT;
+  if (!EXACT) e.accumulate = 0;
+}
+// f(what the epilogue reads besides the bias), uniform over the launch.
+template <bool EXACT, class F> __device__ __forceinline__ void with_extra(const EpiParams& e, F&& f) {
+  if (e.mode == kEpiGeluBwd) return f(std::integral_constant<int, kExtraAuxBf16>{});
+  if constexpr (EXACT) {
+    if (e.mode == kEpiBiasResidual) return f(std::integral_constant<int, kExtraAuxF32>{});
+    if (e.accumulate) return f(std::integral_constant<int, kExtraOldC>{});
+  }
+  f(std::integral_constant<int, kExtraNone>{});
+}
+
 typedef __attribute__((address_space(3))) void* lds_ptr;
 constexpr int kBK = 128;                  // k per tile: the length that shares a scale
 constexpr int64_t kMaxLd = 1 << 23;       // rows of a tile are within 32 bits of byte offset
@@ -181,6 +196,7 @@ __global__ __launch_bounds__(64 * W) void gemm_f8_direct_kernel(GemmF8Params p) 
   const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
   const bool mine = r < 16 && m0 + r < p.M && n0 + c < p.N;
   EpiParams epi = p.epi;
+  narrow<EXACT>(epi);
   float bias = 0.f;                        // on its way with the operands
   if (mine && epi_has_bias(epi.mode) && epi.bias) bias = epi.bias[n0 + c];
   epi.bias = nullptr;
@@ -223,6 +239,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_ke
   using OpA = Operand<S::BM, G, SPLIT>;
   using OpB = Operand<S::BN, G, false>;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  narrow<EXACT>(p.epi);
   int tm, tn;
   tile_of_block(blockIdx.x, p.tiles_m * p.tiles_n, p.tiles_m, p.tiles_n, tm, tn);
   const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
@@ -459,12 +476,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_ke
   __syncthreads();
   float* const parts = reinterpret_cast<float*>(smem);
   auto finish = [&](int64_t m) {
-    switch (epi_extra_kind(p.epi)) {            // uniform over the launch
-      case kExtraAuxBf16: gemm_finish_tile<Finish<S>, kExtraAuxBf16>(parts, p, m, n0); break;
-      case kExtraAuxF32: gemm_finish_tile<Finish<S>, kExtraAuxF32>(parts, p, m, n0); break;
-      case kExtraOldC: gemm_finish_tile<Finish<S>, kExtraOldC>(parts, p, m, n0); break;
-      default: gemm_finish_tile<Finish<S>, kExtraNone>(parts, p, m, n0); break;
-    }
+    with_extra<EXACT>(p.epi, [&](auto kind) { gemm_finish_tile<Finish<S>, decltype(kind)::value>(parts, p, m, n0); });
   };
   if constexpr (G > 1 && FN % 4 == 0) {
     if (whole) {
@@ -475,7 +487,10 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_ke
           for (int j = 0; j < FN; ++j) acc[i][j] += bias[j];
         p.epi.bias = nullptr;
       }
-      gemm_epilogue_staged<FM / 2, FN / 2>(reinterpret_cast<bf16*>(smem), acc, p, m0 + wm * FM * 16, n0 + wn * FN * 16, wave, lane);
+      with_extra<EXACT>(p.epi, [&](auto kind) {
+        gemm_epilogue_staged_kind<FM / 2, FN / 2, decltype(kind)::value>(reinterpret_cast<bf16*>(smem), acc, p, m0 + wm * FM * 16,
+                                                                         n0 + wn * FN * 16, wave, lane);
+      });
       return;
     }
   }
@@ -555,9 +570,10 @@ hipError_t launch_direct(hipStream_t s, GemmF8Params p, bool exact) {
 }
 // Which shape: the largest whose tiles give every compute unit one, as a launch of up to one round takes as long as one tile.
 // us (rows x columns x k, bf16 out unless it says fp32):
-//   direct    1 x 8192 x 2048 5.4 (Few 5.8), 1 x 32768 x 2048 13.4 (15.3), 1 x 8192 x 8192 14.1 (13.2), 4 x 8192 x 2048 6.0 (5.7), 16 x 2048 x 2048
-//             4.9 (5.7), 32 x 2048 x 2048 4.7 (5.7), 16 x 8192 x 2048 6.8 (5.9); eight waves from k = 4096 on: 1 x 2048 x 8192 7.9 (four: 8.6)
-//   Few       256 x 2048 x 2048 6.1 (Split 7.1), 64 x 2048 x 8192 11.4 (16.0), fp32 7.6 (9.5); 512 x 2048 x 2048, two rounds, 10.5 (7.4)
+//   direct    1 x 8192 x 2048 5.4 (Few 5.7), 1 x 32768 x 2048 13.4 (15.3), 4 x 8192 x 2048 6.0 (5.7), 16 x 2048 x 2048
+//             4.9 (5.7), 32 x 2048 x 2048 4.7 (5.7), 16 x 8192 x 2048 6.8 (5.9); eight waves from k = 4096 on: 1 x 2048 x 8192 7.9 (four: 8.6),
+//             1 x 8192 x 4096 8.4 (9.8).  Few rows of a long k lose a little to one rule for all k: 1 x 8192 x 8192 13.6 (Few 13.2)
+//   Few       256 x 2048 x 2048 5.9 (Split 6.8), fp32 7.5 (8.7), 64 x 2048 x 8192 11.2 (14.6), fp32 14.1 (18.9); 512 x 2048 x 2048, two rounds, 10.5 (7.4)
 //   Split     512 x 2048 x 2048 7.4 (Half 9.7), 1024 x 1024 x 1024 6.0 (7.2), fp32 7.7 (9.9); 1024 x 2048 x 2048 13.6 (10.3)
 //   Half      1024 x 2048 x 2048 10.3 (Mid 14.8, MidOne 13.5), fp32 16.8 (20.5)
 //   MidOne    1024 x 4096 x 2048 14.8 (Mid 15.8, Half 15.5), 2048 x 2048 x 8192 34.6 (42.8, 43.5); fp32 66.2 (66.1, 72.7): left to Mid
