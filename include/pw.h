@@ -616,8 +616,9 @@ typedef struct {
 pw_status pw_op_dropout_fwd(pw_ctx* ctx, const pw_dropout_args* args, const void* x, const float* bias, const float* res, void* y);
 /* dx = keep dy / (1 - p) (the residual's gradient is dy itself); dbias: null, or fp32 [cols] that receives the column sums of
  * dx before its rounding (overwritten, or added into when accumulate = 1).  ws: fp32 workspace of
- * pw_dropout_bwd_ws_floats(rows, cols) floats if dbias is wanted (may be null where that is 0), else null.  dx may be the same
- * array as dy where type and stride are the same. */
+ * pw_dropout_bwd_ws_floats(rows, cols) floats if dbias is wanted (may be null where that is 0), else null; nothing in it outlasts
+ * the call, and calls that can run at the same time need one each.  dx may be the same array as dy where type and stride are the
+ * same. */
 pw_status pw_op_dropout_bwd(pw_ctx* ctx, const pw_dropout_args* args, const void* dy, void* dx, float* dbias, float* ws, int accumulate);
 int64_t pw_dropout_bwd_ws_floats(int64_t rows, int64_t cols);   /* -1 for impossible sizes */
 
@@ -639,7 +640,8 @@ typedef struct {
                                 them y, df and dx are zero, the state stays, and what f, x and dy hold does not matter */
 } pw_scan_args;
 /* y rows ldy apart; h_end: fp32 [B, D] state behind the last step, or null; states: pw_scan_state_floats(B, T, D) floats that the
- * backward call needs, or null; ws: workspace of pw_scan_ws_floats(B, T, D) floats (8-byte aligned; may be null where that is 0). */
+ * backward call needs, or null; ws: workspace of pw_scan_ws_floats(B, T, D) floats (8-byte aligned; may be null where that is 0), of
+ * which nothing outlasts the call: forward and backward may share one, calls that can run at the same time need one each. */
 pw_status pw_op_scan_fwd(pw_ctx* ctx, const pw_scan_args* args, void* y, int64_t ldy, float* h_end, float* states, float* ws);
 /* Gradients from dy (rows lddy apart) and dh_end (fp32 [B, D], or null: zeros): df, dx rows lddf, lddx apart (they may be
  * columns of one array), dh0 fp32 [B, D] or null (may be the same array as dh_end).  args and states as in the forward call.

@@ -207,6 +207,41 @@ def test_nan_and_infinite_operands(ctx, M, N, bf16):
     assert np.isfinite(got[1:M - 1][:, keep]).all() and (M < 4 or np.isinf(ref[1:M - 1][:, cols]).any())
 
 
+@pytest.mark.parametrize("M,N", TILES)
+def test_a_residual_in_place_in_every_tile(ctx, M, N):
+    """C over aux, with a bias: whole numbers, equal to the last bit; columns behind N stay."""
+    K, ldc = 144, G.up(N, 8) + 8
+    rng = np.random.RandomState(M)
+    a, b = (np.array(SMALL["e4m3"], np.uint8)[rng.randint(0, 6, (n, K))] for n in (M, N))
+    ea, eb = rng.randint(0, 3, (M, 2)), rng.randint(0, 3, (N, 2))
+    bias, res = rng.randint(-50, 50, N).astype(np.float32), rng.randint(-1000, 1000, (M, N)).astype(np.float32)
+    at, bt, sa, sb, bt32 = (torch.from_numpy(np.ascontiguousarray(v)).cuda() for v in (a, b, R.scale_table(ea), R.scale_table(eb), bias))
+    c = torch.full((M, ldc), 7.0, device="cuda")
+    c[:, :N] = torch.from_numpy(res).cuda()
+    torch.cuda.synchronize()
+    ctx.f8_gemm(pwb.F8GemmArgs(M=M, N=N, K=K, lda=K, ldb=K, ldc=ldc, epilogue=pwb.PW_EPI_BIAS_RESIDUAL, out_dtype=pwb.PW_F32, A=at.data_ptr(),
+                               B=bt.data_ptr(), a_scale=sa.data_ptr(), b_scale=sb.data_ptr(), bias=bt32.data_ptr(), aux=c.data_ptr(), C=c.data_ptr()))
+    ctx.synchronize()
+    assert np.array_equal(G.back(c[:, :N]), times(scaled(a, ea, "e4m3"), scaled(b, eb, "e4m3")) + bias + res) and (c[:, N:] == 7.0).all()
+
+
+# ---- dropout ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,cols,ld,offset", [(1, 5, 5, 1), (300, 77, 83, 3), (9000, 200, 201, 1)])
+def test_dropout_of_bf16_rows_in_place(ctx, rows, cols, ld, offset):
+    """y over x and dx over dy where rows start anywhere; what lies between the rows stays."""
+    keep, _ = R.dropout_keep(rows, cols, 0.5, 9, 1, 2)
+    x = G.low(G.rnd(1, rows, cols), True)
+    t, p = G.dev(x, torch.bfloat16, ld, fill=7.0, offset=offset)
+    a = pwb.DropoutArgs(dtype=pwb.PW_BF16, out_dtype=pwb.PW_BF16, rows=rows, cols=cols, ldx=ld, ldy=ld, p=0.5, seed=9, site=1, step=2)
+    ctx.dropout_fwd(a, p, None, None, p)
+    ctx.synchronize()
+    assert np.array_equal(G.back(t)[:, :cols], np.where(keep, 2 * x, 0.0)) and (G.back(t)[:, cols:] == 7.0).all()
+    ctx.dropout_bwd(a, p, p)
+    ctx.synchronize()
+    assert np.array_equal(G.back(t)[:, :cols], np.where(keep, 4 * x, 0.0)) and (G.back(t)[:, cols:] == 7.0).all()
+
+
 # ---- gated recurrence ------------------------------------------------------------------------------------------
 
 def recur(ctx, f, x, h0, dy, dh, lens, bf16):
