@@ -13,8 +13,8 @@
 // there; threads of a block that share a group meet in LDS in thread order, blocks in a second launch in block order: the
 // same bits on every run.
 //
-// Bound by memory: 8192 x 2048 bf16 into an fp32 residual takes 32 us forward (168 MB, 5.2 TB/s; a copy reaches 5.15) and 21
-// backward (101 MB), with 4.2 more for the second launch of the bias gradient.  The counter's ten rounds of two products keep the
+// Bound by memory: 8192 x 2048 bf16 into an fp32 residual takes 33 to 34 us forward (168 MB, 5.0 TB/s; a copy reaches 5.15) and 20 to
+// 22 backward (101 MB), with 4 to 5 more for the second launch of the bias gradient.  The counter's ten rounds of two products keep the
 // vector units busy for a third of that, under the loads of two rows at a time.
 #include "common.hpp"
 #include "kernels.hpp"

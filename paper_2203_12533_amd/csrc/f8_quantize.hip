@@ -15,8 +15,8 @@
 // Bound by memory: a block of 256 threads takes 128 x 128 elements, 8 x 8 to a thread, reads them once into registers and writes 8
 // consecutive values per lane; the transposed bytes turn in LDS.  What it computes per element is kept to a few operations:
 // maxima are taken of the magnitudes' bits, two bf16 at a time, and v_cvt_scalef32_pk_* divides by the scale and rounds two
-// values at once.  8192 x 2048 bf16, both outputs, 12.2 us (67 MB, 5.5 TB/s; a copy of 1 GiB reaches 5.15); 2048 x 8192 fp32 with 128 x
-// 128 blocks 18.6 to 21 (101 MB).
+// values at once.  8192 x 2048 bf16, both outputs, 12.1 to 12.5 us (67 MB, 5.5 TB/s; a copy of 1 GiB reaches 5.15); 2048 x 8192 fp32
+// with 128 x 128 blocks 21.3 (101 MB).
 #include <type_traits>
 
 #include "common.hpp"

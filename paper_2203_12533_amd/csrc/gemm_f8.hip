@@ -141,7 +141,7 @@ template <int FMT> __device__ __forceinline__ bf16x8 widen8(const i32x8& f, int 
 // Few rows, and rows too far apart for 32-bit offsets.  What bounds a product of few rows is reading B once, so nothing is
 // staged: a block owns 16 columns and 16 rows, its waves take every W-th k block, operands go from memory straight into
 // fragments (four lanes read 64 consecutive bytes of a row), kAhead blocks at a time, and the waves' sums meet
-// in LDS in wave order.  1 x 8192 x 2048: 5.6 us a pass, of which the launch is about 4.
+// in LDS in wave order.  1 x 8192 x 2048: 5.4 to 5.6 us a pass, of which the launch is about 4.
 constexpr int kAhead = 4;
 template <int W, int FA, int FB, bool EXACT>
 __global__ __launch_bounds__(64 * W) void gemm_f8_direct_kernel(GemmF8Params p) {
@@ -351,10 +351,10 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f8_tile_ke
   //    end.
   // There (kTurn) the waves meet, the next tile is there, and the stage of this one is free for tile t + NS, whose direct loads
   // go out between the MFMAs that are left.
-  // What bounds the largest: power.  8192 x 8192 x 8192 runs at 1.8 GHz, 69 of 100 cycles with an MFMA, 2.8 PFLOP/s; of its 392
+  // What bounds the largest: power.  8192 x 8192 x 8192 runs at 1.8 GHz, 69 of 100 cycles with an MFMA, 2.8 PFLOP/s; of its 389
   // us the MFMAs alone take 292, reading fragments 40, bringing operands 70.  Addresses of fragments kept whole and a running
   // pointer to the scales, fewer instructions between the MFMAs, won 4 of 100.  Four waves of 128 x 128, which read a third
-  // less from LDS, leave nothing to a SIMD while its wave waits: 395 us, and 139 instead of 130 with k = 2048.
+  // less from LDS, leave nothing to a SIMD while its wave waits: 395 us instead of 392 then, and 139 instead of 130 with k = 2048.
   // STREAM: tile t + NS is a whole one; MORE: tile t + 1 exists (t + NS, where it does not, is made of zeros nobody reads).  No
   // branches inside: the compiler would move MFMAs past them.
   constexpr int kTurn = EXACT ? FM - 2 : FM - 1, kSlots = (FM - kTurn) * FN;
@@ -570,17 +570,17 @@ hipError_t launch_direct(hipStream_t s, GemmF8Params p, bool exact) {
 }
 // Which shape: the largest whose tiles give every compute unit one, as a launch of up to one round takes as long as one tile.
 // us (rows x columns x k, bf16 out unless it says fp32):
-//   direct    1 x 8192 x 2048 5.4 (Few 5.7), 1 x 32768 x 2048 13.4 (15.3), 4 x 8192 x 2048 6.0 (5.7), 16 x 2048 x 2048
-//             4.9 (5.7), 32 x 2048 x 2048 4.7 (5.7), 16 x 8192 x 2048 6.8 (5.9); eight waves from k = 4096 on: 1 x 2048 x 8192 7.9 (four: 8.6),
-//             1 x 8192 x 4096 8.4 (9.8).  Few rows of a long k lose a little to one rule for all k: 1 x 8192 x 8192 13.6 (Few 13.2)
-//   Few       256 x 2048 x 2048 5.9 (Split 6.8), fp32 7.5 (8.7), 64 x 2048 x 8192 11.2 (14.6), fp32 14.1 (18.9); 512 x 2048 x 2048, two rounds, 10.5 (7.4)
-//   Split     512 x 2048 x 2048 7.4 (Half 9.7), 1024 x 1024 x 1024 6.0 (7.2), fp32 7.7 (9.9); 1024 x 2048 x 2048 13.6 (10.3)
-//   Half      1024 x 2048 x 2048 10.3 (Mid 14.8, MidOne 13.5), fp32 16.8 (20.5)
-//   MidOne    1024 x 4096 x 2048 14.8 (Mid 15.8, Half 15.5), 2048 x 2048 x 8192 34.6 (42.8, 43.5); fp32 66.2 (66.1, 72.7): left to Mid
-//   Mid       1500 x 4096 x 2048 20.1 (MidOne 24.7, Half 23.4, Big 27.6), fp32 32.1 (40.8, 35.3); 128 tiles of 256 x 256, 2048 x 4096 x 2048,
-//             22.9 (Big 27.2)
-//   Big       a round from 144 tiles on, 2304 x 4096 x 2048 27.5 (Mid 30.8), 2816 x 3840 x 8192 81 (97); beyond one where few of the last
-//             are idle: 272 tiles, 4352 x 4096 x 2048, 52.1 (46.4), 320 51.7 (46.2), 352 51.8 (52.0), 384 52.6 (53.6)
+//   direct    1 x 8192 x 2048 5.4 (Few 5.8), 1 x 32768 x 2048 13.6 (15.3), 4 x 8192 x 2048 5.8 (5.8), 16 x 2048 x 2048
+//             4.9 (5.7), 32 x 2048 x 2048 5.2 (5.7), 16 x 8192 x 2048 6.8 (6.3); eight waves from k = 4096 on: 1 x 2048 x 8192 7.8 (four: 8.8),
+//             1 x 8192 x 4096 8.5 (9.8).  Few rows of a long k lose a little to one rule for all k: 1 x 8192 x 8192 13.7 (Few 13.2)
+//   Few       256 x 2048 x 2048 6.0 (Split 6.9), fp32 7.5 (8.7), 64 x 2048 x 8192 11.3 (14.5), fp32 14.0 (18.8); 512 x 2048 x 2048, two rounds, 10.2 (7.1)
+//   Split     512 x 2048 x 2048 7.1 (Half 8.9), 1024 x 1024 x 1024 5.9 (6.9), fp32 7.4 (9.6); 1024 x 2048 x 2048 13.1 (9.6)
+//   Half      1024 x 2048 x 2048 9.6 (Mid 14.1, MidOne 12.9), fp32 16.3 (20.7)
+//   MidOne    1024 x 4096 x 2048 14.1 (Mid 15.2, Half 14.9), 2048 x 2048 x 8192 36.8 (43.5, 40.6); fp32, Mid against Half: 67.2 (73.4)
+//   Mid       1500 x 4096 x 2048 18.2 (MidOne 24.5, Half 21.1, Big 26.6), fp32 30.2 (Half 33.4); 128 tiles of 256 x 256, 2048 x 4096 x 2048,
+//             19.8 (Big 27.2)
+//   Big       a round from 144 tiles on, 2304 x 4096 x 2048 27.5 (Mid 29.4), 2816 x 3840 x 8192 80 (92); beyond one where few of the last
+//             are idle: 272 tiles, 4352 x 4096 x 2048, 50.1 (44.5), 320 50.6 (45.1), 352 50.9 (49.2), 384 51.8 (50.9), 1024 119 (140)
 template <int FA, int FB>
 hipError_t choose(hipStream_t s, const GemmF8Params& p, bool exact) {
   auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };

@@ -15,17 +15,19 @@
 // walks upwards.
 //
 // The least traffic is three arrays forward and five backward.  bf16 tiles come by direct loads into LDS while the one before
-// is at work (registers hold one tile: 205 of 256 in the backward pass; the forward pass is kept to 128, so that two blocks of a
-// second round fit a unit: 12 x 1024 x 2048 50.2 -> 46.9 us).  8 x 1024 x 2048 bf16: 28 us forward (3.6 TB/s; a copy reaches 5.15),
-// 48.4 us backward.  Without its stores the forward pass takes 23, without the exponentials 25, without both 19: with two waves
-// to a SIMD neither hides all of the other.  Blocks of 32 channels, two to a unit, read and write half lines: 33 and 52 us.  A
-// second tile ahead wins nothing.  16 steps to a thread halve the exchanges that 8 steps take.
+// is at work (registers hold one tile: 205 of 256 in the backward pass, which leaves it two waves to a SIMD; the forward pass is
+// kept to 128, so that two blocks of a second round fit a unit: 12 x 1024 x 2048 50.2 us -> 46.9, now 46.3).  8 x 1024 x 2048 bf16:
+// 27.4 us forward (3.7 TB/s; a copy reaches 5.15), 48.7 backward, 41 right behind the forward pass of the same arrays.  256 blocks of 8 waves are one to a unit, so the forward pass too has two waves to a SIMD there, of the four
+// that its registers allow; of 28 us it took 23 without stores, 25 without exponentials, 19 without both: neither hides all of the
+// other.  fp32 comes without loads ahead: 50.4 and 81.8 us (4.0 and 4.1 TB/s).  Blocks of 32 channels, two to a unit, read and write
+// half lines: 33 and 52 us.  A second tile ahead wins nothing.  16 steps to a thread halve the exchanges that 8 steps take.
 //
 // Few channels leave compute units idle.  The sequence is then cut into segments of whole tiles (plan_of): a first launch
 // composes each segment into one map, the second composes the maps in front of its segment (behind it, backward) and goes on as
-// above.  1 x 16384 x 512 bf16: 24.7 us forward, 31.1 backward.
+// above.  1 x 16384 x 512 bf16: 24.0 us forward, 31.5 backward; fp32 37.6 and 57.6.
 //
-// Steps behind the end of a sequence (lens) are the identity map with outputs of zero; their inputs are not read.
+// Steps behind the end of a sequence (lens) are the identity map with outputs of zero, whatever their inputs hold: in their place a
+// row of the tile is read (its first, where none is before the end) and dropped.
 // Sums, states and gates are fp32; y, df and dx are rounded once.  All orders are fixed: the same bits on every run.
 #include <type_traits>
 #include <utility>
