@@ -103,7 +103,7 @@ def test_quantisation_around_the_smallest_scale(ctx, fmt, bf16):
 
 # ---- products --------------------------------------------------------------------------------------------------
 
-TILES = [(3, 200), (40, 200), (260, 300), (500, 1300), (1300, 1100), (1700, 1900), (2100, 2600), (2304, 4096)]
+TILES = [(3, 200), (40, 200), (260, 300), (500, 1300), (1300, 1100), (1700, 1900), (2100, 2600), (2304, 4096), (2300, 4090)]
 
 
 def multiply(ctx, a, ea, b, eb, fa, fb, bf16, M, N, K):
