@@ -651,6 +651,134 @@ pw_status pw_op_scan_bwd(pw_ctx* ctx, const pw_scan_args* args, const void* dy, 
 int64_t pw_scan_state_floats(int64_t B, int64_t T, int64_t D);   /* -1 for impossible sizes */
 int64_t pw_scan_ws_floats(int64_t B, int64_t T, int64_t D);
 
+/* ---- operands in 4-bit floating point -------------------------------------------------------------
+ * Values are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign), two to a byte, the first of them in the low half, with a scale 2^e for
+ * each block of 32 elements along the contraction, stored as the byte e + 127.  An operand of `rows` rows of `cols` elements is an array
+ * [rows][ld / 2] of bytes and a scale table of pw_f4_scale_bytes(rows, cols) bytes: block b (columns 32 b .. 32 b + 31) of row r has its byte at
+ *     (b / 4 * R + r / 64 * 64) * 4 + b % 4 * 64 + (r % 16) * 4 + (r % 64) / 16,   R = rows rounded up to a multiple of 64.
+ * Bytes of rows and blocks that do not exist are written as 0 and matter nowhere; the byte 255 (no number) makes its block NaN. */
+/* 256 ceil(rows / 64) ceil(cols / 128); -1 if either is negative or over 2^30. */
+int64_t pw_f4_scale_bytes(int64_t rows, int64_t cols);
+
+/* x [rows][ldx] in `dtype` to either or both of
+ *   q  [rows][ldq]:  x,            blocks along the columns of x, scale table of (rows, cols);
+ *   qt [cols][ldqt]: x transposed, blocks along the rows of x,    scale table of (cols, rows)
+ * (a null pointer leaves one out; then its scale pointer and stride are not looked at).  block_rows = 1: each row of q (of qt) has
+ * scales of its own, as activations and gradients want them.  block_rows = 32: one scale for 32 x 32 elements of x, the same in both
+ * outputs, as weights want it.  e is the smallest integer in [-127, 127] for which no element of the block exceeds 6 * 2^e (-127 for a
+ * block of zeros); elements are rounded to nearest, ties to even.  The format has neither infinities nor NaN: a block that
+ * holds one gets the scale byte 255 and codes of 0, so that products with it are NaN.
+ * ldq, ldqt: elements from row to row, multiples of 32, ldq >= cols, ldqt >= rows; rows are filled with zeros up to the next multiple of 32 elements,
+ * so that this length can be the K of a product; bytes behind that are left as they were.  q, qt and the scale tables are 16-byte aligned.
+ * Outputs overlap neither x nor each other. */
+typedef struct {
+  int32_t dtype;             /* of x: PW_F32 or PW_BF16 */
+  int32_t block_rows;        /* 1 or 32 */
+  const void* x;
+  int64_t rows, cols, ldx;   /* rows at most 128 * 65535, columns at most 2^30 */
+  void* q;
+  int64_t ldq;
+  uint8_t* q_scale;
+  void* qt;
+  int64_t ldqt;
+  uint8_t* qt_scale;
+} pw_f4_quantize_args;
+pw_status pw_op_f4_quantize(pw_ctx* ctx, const pw_f4_quantize_args* args);
+
+/* C[M, N] = A[M, K] . B[N, K]^T of two such operands (both contiguous along K), fp32 accumulation, and the epilogues
+ * PW_EPI_STORE .. PW_EPI_GELU_BWD of pw_op_gemm with the same meaning (aux of PW_EPI_GELU_BWD is bf16; a residual and an
+ * accumulating store need out_dtype PW_F32).  M and N at most 2^26, K at most 2^30; K, lda, ldb (elements) multiples of 32, ldc a multiple of 8; A, B,
+ * C, C2, aux, bias and the scale tables 16-byte aligned.  The table of an operand is the one of (rows, K).  With y = x W of the LM's layers,
+ * W [in][out]: forward A = q(x), B = qt(W); data gradient A = q(dy), B = q(W); weight gradient dW = A = qt(x), B = qt(dy), K = the
+ * rows of x rounded up to 32.  Outputs may overlap aux of PW_EPI_BIAS_RESIDUAL (the same array) and nothing else. */
+typedef struct {
+  int64_t M, N, K, lda, ldb, ldc;
+  int32_t epilogue;             /* pw_epilogue */
+  int32_t out_dtype;            /* PW_F32 or PW_BF16: type of C and C2 */
+  int32_t accumulate;           /* 1: C += result (fp32 output, PW_EPI_STORE only) */
+  const void* A;
+  const void* B;
+  const uint8_t* a_scale;
+  const uint8_t* b_scale;
+  const float* bias;            /* [N] or null */
+  const void* aux;              /* [M, ldc] or null */
+  void* C;
+  void* C2;
+} pw_f4_gemm_args;
+pw_status pw_op_f4_gemm(pw_ctx* ctx, const pw_f4_gemm_args* args);
+
+/* ---- root-mean-square norm -------------------------------------------------------------------------
+ * The residual stream takes a branch in and is normalised for the next one: x' = x + y, r = 1 / sqrt(mean over a row of x'^2 + eps),
+ * h = x' r g. */
+typedef struct {
+  int32_t dtype;             /* of y, h, dh and dy: PW_F32 or PW_BF16 */
+  int64_t rows, cols;        /* rows at most 2^31 - 1, columns 1 .. 16384 */
+  int64_t ldx;               /* elements from row to row of the fp32 arrays x, x_out, dres and dx */
+  int64_t ldh;               /* of y, h, dh and dy */
+  float eps;                 /* >= 0 */
+  const float* g;            /* [cols] */
+} pw_rmsnorm_args;
+/* An output as pw_op_f8_quantize writes its q with block_rows = 1: the same layout, alignments, scales and rounding. */
+typedef struct {
+  int32_t format;            /* pw_f8_format */
+  void* q;                   /* [rows][ldq] */
+  int64_t ldq;
+  uint8_t* scale;            /* pw_f8_scale_bytes(rows, cols) */
+} pw_f8_out;
+/* y: the branch, or null.  x_out: receives x', or null; it may be the same array as x.  h, q: at least one of the two is wanted, the other may be null; q
+ * holds h rounded once, from 32 bits.  rstd: fp32 [rows] for the backward call, or null.  The outputs overlap nothing else. */
+pw_status pw_op_rmsnorm_fwd(pw_ctx* ctx, const pw_rmsnorm_args* args, const float* x, const void* y, float* x_out, void* h, const pw_f8_out* q,
+                            float* rstd);
+/* Gradients from dh, with x the x' of the forward call: dx = dres + r (dh g - xh mean(dh g xh)) with xh = x' r, fp32, the gradient
+ * of x (and of y); dres: gradient that reaches x' past the norm, or null; it may be the same array as dx.  dy: dx in `dtype`, or null.
+ * dg: fp32 [cols], sum over rows of dh xh (overwritten, or added into when accumulate = 1), or null.  ws: workspace of
+ * pw_rmsnorm_bwd_ws_floats(rows, cols) floats, 16-byte aligned (not looked at where dg is null); nothing in it outlasts the call, and calls that can run at the
+ * same time need one each.  The outputs overlap nothing else. */
+pw_status pw_op_rmsnorm_bwd(pw_ctx* ctx, const pw_rmsnorm_args* args, const void* dh, const float* x, const float* rstd, const float* dres,
+                            float* dx, void* dy, float* dg, float* ws, int accumulate);
+int64_t pw_rmsnorm_bwd_ws_floats(int64_t rows, int64_t cols);   /* -1 for impossible sizes */
+
+/* ---- log probabilities -----------------------------------------------------------------------------
+ * Of rows of logits z, times a scale s (1 / temperature): p = softmax(s z), the log probability of one given token per row, the entropy
+ * H = -sum p log p and the k likeliest tokens; and the gradient of the logits from gradients of the first two.  A logit of -infinity is a
+ * token that cannot occur: p = 0, and it adds nothing to H.  A row of them only has no distribution: its logp is -infinity, H is 0, it has no alternatives
+ * and no gradient.  A row that holds a NaN or +infinity has none either: its logp, H, top_logp and gradients are NaN, its top_id -1. */
+typedef struct {
+  int32_t dtype;             /* of z and dz: PW_F32 or PW_BF16 */
+  const void* z;
+  int64_t ldz;               /* elements from row to row */
+  int64_t rows, vocab;       /* rows at most 2^31 - 1, vocab 1 .. 2^28 */
+  const int32_t* targets;    /* device, [rows], or null.  A token outside [0, vocab) is none: the row's logp is 0 and dlogp is not looked at */
+  float scale;               /* s: positive and finite */
+} pw_logprob_args;
+/* logp, entropy: fp32 [rows], or null (logp needs targets).  stats: fp32 [rows][2], 8-byte aligned, for the backward call, or null: the largest z and the log of sum
+ * exp(s (z - that)).  top_id: int32 [rows][k] and top_logp: fp32 [rows][k], the k tokens of largest z in descending order, the lowest index first among
+ * equals, and their log probabilities; k at most 32 (0: both null); places that no token is left for hold -1 and -infinity.
+ * ws: workspace of pw_logprob_ws_floats(rows, vocab, k) floats, 8-byte aligned (may be null where that is 0); nothing in it outlasts the call, and calls that can run at the
+ * same time need one each.  The outputs overlap nothing else. */
+pw_status pw_op_logprob_fwd(pw_ctx* ctx, const pw_logprob_args* args, float* logp, float* entropy, float* stats, int k, int32_t* top_id,
+                            float* top_logp, float* ws);
+int64_t pw_logprob_ws_floats(int64_t rows, int64_t vocab, int k);   /* -1 for impossible sizes */
+/* dz = s [dlogp (onehot(target) - p) - dentropy p (log p + H)], rows lddz apart; it may be the same array as z.  stats and entropy: what the
+ * forward call wrote (entropy may be null where dentropy is).  dlogp, dentropy: fp32 [rows]; either may be null (dlogp needs targets). */
+pw_status pw_op_logprob_bwd(pw_ctx* ctx, const pw_logprob_args* args, const float* stats, const float* entropy, const float* dlogp,
+                            const float* dentropy, void* dz, int64_t lddz);
+
+/* ---- clipping by the norm of all gradients -----------------------------------------------------------
+ * norm = sqrt(sum of the squares of all elements of all tensors), summed in 64 bits in a fixed order; factor = max_norm / norm where norm
+ * exceeds max_norm, else 1 (NaN where the norm is NaN); out = g factor, rounded once. */
+typedef struct {
+  const void* g;             /* device, aligned to its elements; may be null where n is 0 */
+  void* out;                 /* like g; may be g itself; null: this tensor counts and is not scaled */
+  int64_t n;                 /* elements */
+  int32_t dtype;             /* PW_F32 or PW_BF16 */
+} pw_grad_tensor;
+/* tensors: host array of `count`, read during the call; count at most 2^20, elements at most 2^40 altogether.  max_norm >= 0 (infinity: factor is 1).  result: device, fp32 [2], receives norm and
+ * factor.  ws: workspace of pw_grad_clip_ws_floats() floats, 8-byte aligned; nothing in it outlasts the call, and calls that can run at the same time need one each.
+ * An output overlaps nothing but its own g (as a whole).  If one tensor is refused nothing is enqueued. */
+pw_status pw_op_grad_clip(pw_ctx* ctx, const pw_grad_tensor* tensors, int count, float max_norm, float* result, float* ws);
+int64_t pw_grad_clip_ws_floats(void);
+
 /* ---- measurement aid ----------------------------------------------------------------------------
  * Between pw_profile_begin and pw_profile_end every MFMA GEMM launched on the executor stream (by a train
  * step or by pw_op_gemm) is bracketed by a pair of timing HIP events on that stream.  pw_profile_end

@@ -116,6 +116,36 @@ class ScanArgs(C.Structure):
                 ("B", C.c_int32), ("T", C.c_int32), ("D", C.c_int32), ("h0", C.c_void_p), ("lens", C.c_void_p)]
 
 
+class F4QuantizeArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("block_rows", C.c_int32), ("x", C.c_void_p),
+                ("rows", C.c_int64), ("cols", C.c_int64), ("ldx", C.c_int64),
+                ("q", C.c_void_p), ("ldq", C.c_int64), ("q_scale", C.c_void_p),
+                ("qt", C.c_void_p), ("ldqt", C.c_int64), ("qt_scale", C.c_void_p)]
+
+
+class F4GemmArgs(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("M", "N", "K", "lda", "ldb", "ldc")] + \
+               [(n, C.c_int32) for n in ("epilogue", "out_dtype", "accumulate")] + \
+               [(n, C.c_void_p) for n in ("A", "B", "a_scale", "b_scale", "bias", "aux", "C", "C2")]
+
+
+class RmsnormArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32)] + [(n, C.c_int64) for n in ("rows", "cols", "ldx", "ldh")] + [("eps", C.c_float), ("g", C.c_void_p)]
+
+
+class F8Out(C.Structure):
+    _fields_ = [("format", C.c_int32), ("q", C.c_void_p), ("ldq", C.c_int64), ("scale", C.c_void_p)]
+
+
+class LogprobArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("z", C.c_void_p)] + [(n, C.c_int64) for n in ("ldz", "rows", "vocab")] + \
+               [("targets", C.c_void_p), ("scale", C.c_float)]
+
+
+class GradTensor(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
 class PwError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < len(STATUS_NAMES) else status}: {msg}")
@@ -221,6 +251,17 @@ _SIGS = {
                                  C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
     "pw_scan_state_floats": (C.c_int64, [C.c_int64] * 3),
     "pw_scan_ws_floats": (C.c_int64, [C.c_int64] * 3),
+    "pw_f4_scale_bytes": (C.c_int64, [C.c_int64] * 2),
+    "pw_op_f4_quantize": (C.c_int, [C.c_void_p, C.POINTER(F4QuantizeArgs)]),
+    "pw_op_f4_gemm": (C.c_int, [C.c_void_p, C.POINTER(F4GemmArgs)]),
+    "pw_op_rmsnorm_fwd": (C.c_int, [C.c_void_p, C.POINTER(RmsnormArgs)] + [C.c_void_p] * 4 + [C.POINTER(F8Out), C.c_void_p]),
+    "pw_op_rmsnorm_bwd": (C.c_int, [C.c_void_p, C.POINTER(RmsnormArgs)] + [C.c_void_p] * 8 + [C.c_int]),
+    "pw_rmsnorm_bwd_ws_floats": (C.c_int64, [C.c_int64] * 2),
+    "pw_op_logprob_fwd": (C.c_int, [C.c_void_p, C.POINTER(LogprobArgs)] + [C.c_void_p] * 3 + [C.c_int] + [C.c_void_p] * 3),
+    "pw_logprob_ws_floats": (C.c_int64, [C.c_int64] * 2 + [C.c_int]),
+    "pw_op_logprob_bwd": (C.c_int, [C.c_void_p, C.POINTER(LogprobArgs)] + [C.c_void_p] * 5 + [C.c_int64]),
+    "pw_op_grad_clip": (C.c_int, [C.c_void_p, C.POINTER(GradTensor), C.c_int, C.c_float, C.c_void_p, C.c_void_p]),
+    "pw_grad_clip_ws_floats": (C.c_int64, []),
     "pw_op_sgd": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_float]),
     "pw_op_adam": (C.c_int, [C.c_void_p] + [C.c_void_p] * 5 + [C.c_int64] + [C.c_float] * 4 + [C.c_int]),
 }
@@ -490,6 +531,31 @@ class Context:
                  dh0: int | None, ws: int | None):
         self._check(lib().pw_op_scan_bwd(self._h, C.byref(args), dy, lddy, dh_end, states, df, lddf, dx, lddx, dh0, ws))
 
+    def f4_quantize(self, args: "F4QuantizeArgs"):
+        self._check(lib().pw_op_f4_quantize(self._h, C.byref(args)))
+
+    def f4_gemm(self, args: "F4GemmArgs"):
+        self._check(lib().pw_op_f4_gemm(self._h, C.byref(args)))
+
+    def rmsnorm_fwd(self, args: "RmsnormArgs", x: int, y: int | None, x_out: int | None, h: int | None, q: "F8Out | None" = None,
+                    rstd: int | None = None):
+        self._check(lib().pw_op_rmsnorm_fwd(self._h, C.byref(args), x, y, x_out, h, C.byref(q) if q is not None else None, rstd))
+
+    def rmsnorm_bwd(self, args: "RmsnormArgs", dh: int, x: int, rstd: int, dres: int | None, dx: int, dy: int | None = None,
+                    dg: int | None = None, ws: int | None = None, accumulate: int = 0):
+        self._check(lib().pw_op_rmsnorm_bwd(self._h, C.byref(args), dh, x, rstd, dres, dx, dy, dg, ws, accumulate))
+
+    def logprob_fwd(self, args: "LogprobArgs", logp: int | None, entropy: int | None, stats: int | None = None, k: int = 0,
+                    top_id: int | None = None, top_logp: int | None = None, ws: int | None = None):
+        self._check(lib().pw_op_logprob_fwd(self._h, C.byref(args), logp, entropy, stats, k, top_id, top_logp, ws))
+
+    def logprob_bwd(self, args: "LogprobArgs", stats: int, entropy: int | None, dlogp: int | None, dentropy: int | None, dz: int, lddz: int):
+        self._check(lib().pw_op_logprob_bwd(self._h, C.byref(args), stats, entropy, dlogp, dentropy, dz, lddz))
+
+    def grad_clip(self, tensors, max_norm: float, result: int, ws: int):
+        """tensors: what grad_tensors() made."""
+        self._check(lib().pw_op_grad_clip(self._h, tensors, len(tensors), max_norm, result, ws))
+
     def gemm_group(self, kws: list):
         arr = (GemmArgs * len(kws))()
         keep = []
@@ -516,6 +582,27 @@ def scan_state_floats(B: int, T: int, D: int) -> int:
 
 def scan_ws_floats(B: int, T: int, D: int) -> int:
     return lib().pw_scan_ws_floats(B, T, D)
+
+
+def f4_scale_bytes(rows: int, cols: int) -> int:
+    return lib().pw_f4_scale_bytes(rows, cols)
+
+
+def rmsnorm_bwd_ws_floats(rows: int, cols: int) -> int:
+    return lib().pw_rmsnorm_bwd_ws_floats(rows, cols)
+
+
+def logprob_ws_floats(rows: int, vocab: int, k: int) -> int:
+    return lib().pw_logprob_ws_floats(rows, vocab, k)
+
+
+def grad_clip_ws_floats() -> int:
+    return lib().pw_grad_clip_ws_floats()
+
+
+def grad_tensors(tensors) -> "C.Array":
+    """(g, out or None, elements, dtype) of each tensor, addresses as ints -> the array that Context.grad_clip takes; it can be kept."""
+    return (GradTensor * len(tensors))(*[GradTensor(*t) for t in tensors])
 
 
 def _gemm_args(kw: dict, a: "GemmArgs | None" = None) -> "GemmArgs":

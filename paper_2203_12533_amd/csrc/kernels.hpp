@@ -188,6 +188,77 @@ hipError_t launch_scan_fwd(hipStream_t s, const ScanArgs& a, void* y, int64_t ld
 hipError_t launch_scan_bwd(hipStream_t s, const ScanArgs& a, const void* dy, int64_t lddy, const float* dh_end, const float* states,
                            void* df, int64_t lddf, void* dx, int64_t lddx, float* dh0, float* ws);
 
+// f4_quantize.hip, gemm_f4.hip: operands in 4-bit floating point; see pw.h for the layouts.
+struct F4QuantizeArgs {
+  int dtype, block_rows;
+  const void* x;
+  int64_t rows, cols, ldx;
+  void* q;
+  int64_t ldq;
+  uint8_t* q_scale;
+  void* qt;
+  int64_t ldqt;
+  uint8_t* qt_scale;
+};
+int64_t f4_scale_bytes(int64_t rows, int64_t cols);
+hipError_t launch_f4_quantize(hipStream_t s, const F4QuantizeArgs& a);
+struct GemmF4Args {
+  int64_t M, N, K, lda, ldb, ldc;
+  int epilogue, out_dtype, accumulate;
+  const void* A;
+  const void* B;
+  const uint8_t* a_scale;
+  const uint8_t* b_scale;
+  const float* bias;
+  const void* aux;
+  void* C;
+  void* C2;
+};
+hipError_t launch_gemm_f4(hipStream_t s, const GemmF4Args& a);
+hipError_t gemm_f4_init();   // one-time set-up of kernel attributes (dynamic LDS); call once before any capture
+
+// rmsnorm.hip
+struct RmsnormArgs {
+  int dtype;
+  int64_t rows, cols, ldx, ldh;
+  float eps;
+  const float* g;
+};
+struct F8Out {               // q null: not wanted
+  int format;
+  void* q;
+  int64_t ldq;
+  uint8_t* scale;
+};
+hipError_t launch_rmsnorm_fwd(hipStream_t s, const RmsnormArgs& a, const float* x, const void* y, float* x_out, void* h, const F8Out& q, float* rstd);
+int64_t rmsnorm_bwd_ws_floats(int64_t rows, int64_t cols);
+hipError_t launch_rmsnorm_bwd(hipStream_t s, const RmsnormArgs& a, const void* dh, const float* x, const float* rstd, const float* dres, float* dx,
+                              void* dy, float* dg, float* ws, int accumulate);
+
+// logprob.hip
+struct LogprobArgs {
+  int dtype;
+  const void* z;
+  int64_t ldz, rows, vocab;
+  const int32_t* targets;
+  float scale;
+};
+int64_t logprob_ws_floats(int64_t rows, int64_t vocab, int k);
+hipError_t launch_logprob_fwd(hipStream_t s, const LogprobArgs& a, float* logp, float* entropy, float* stats, int k, int32_t* top_id, float* top_logp,
+                              float* ws);
+hipError_t launch_logprob_bwd(hipStream_t s, const LogprobArgs& a, const float* stats, const float* entropy, const float* dlogp, const float* dentropy,
+                              void* dz, int64_t lddz);
+
+// grad_clip.hip
+struct GradTensor {
+  const void* g;
+  void* out;
+  int64_t n;
+  int dtype;
+};
+int64_t grad_clip_ws_floats();
+hipError_t launch_grad_clip(hipStream_t s, const GradTensor* t, int count, float max_norm, float* result, float* ws);
+
 // attention.hip
 // Multi-head attention of Tq queries over Tk keys per (batch, head), scale 1/sqrt(hd).  q, k, v point at element
 // (batch 0, row 0, feature 0) of arrays in `dtype`; rows are ldq (q) and ldkv (k and v) elements apart, batch b

@@ -1,0 +1,400 @@
+// Root-mean-square norm with the residual's addition in front and an 8-bit output behind, and its backward pass:
+//
+//   x' = x + y,  r = 1 / sqrt(mean x'^2 + eps),  h = x' r g,  q = h in 8 bits with a scale for each 128 columns (f8_quantize.hip)
+//   dx = dres + r (dh g - xh mean(dh g xh)),  xh = x' r;   dg = sum over rows of dh xh
+//
+// Bound by memory: a row is read once into registers (a wave to a row of up to 2048 columns, a block beyond), four consecutive columns to a
+// lane, so that every load and store of 4, 2 or 1 byte an element covers whole lines; 32 lanes hold a block of 128 columns, whose largest
+// magnitude takes five moves between lanes.  What the separate passes would move besides: x' once more for the norm, h once more for the
+// quantisation.  Sums, r and h are fp32; q rounds h once, and so does h in bf16.
+#include <type_traits>
+
+#include "common.hpp"
+#include "kernels.hpp"
+#include "lanes.hpp"
+#include "quantize_common.hpp"
+
+namespace pw {
+
+namespace {
+
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));        // wherever an element may be
+typedef unsigned short u16x4u __attribute__((ext_vector_type(4), aligned(2)));
+
+// Columns c .. c + 3 of a row of d; zeros behind its end.
+__device__ __forceinline__ f32x4 load4(const float* p, int c, int d) {
+  if (c + 4 <= d) return *reinterpret_cast<const f32x4u*>(p + c);
+  f32x4 v = {};
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (c + e < d) v[e] = p[c + e];
+  return v;
+}
+struct Bf4 { u16x4u v; };
+template <class T> struct Stored;            // four elements as they are stored
+template <> struct Stored<float> {
+  typedef f32x4 type;
+  static __device__ __forceinline__ type load(const float* p, int c, int d) { return load4(p, c, d); }
+  static __device__ __forceinline__ f32x4 wide(type v) { return v; }
+};
+template <> struct Stored<bf16> {
+  typedef uint2 type;
+  static __device__ __forceinline__ type load(const bf16* p, int c, int d) {
+    u16x4u v = {};
+    if (c + 4 <= d) {
+      v = *reinterpret_cast<const u16x4u*>(p + c);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (c + e < d) v[e] = __builtin_bit_cast(unsigned short, p[c + e]);
+    }
+    return make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
+  }
+  static __device__ __forceinline__ f32x4 wide(type v) {
+    return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
+  }
+};
+__device__ __forceinline__ void store4(float* p, int c, int d, const f32x4& v) {
+  if (c + 4 <= d) {
+    *reinterpret_cast<f32x4u*>(p + c) = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (c + e < d) p[c + e] = v[e];
+  }
+}
+__device__ __forceinline__ void store4(bf16* p, int c, int d, const f32x4& v) {
+  const bf16x4 o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+  if (c + 4 <= d) {
+    *reinterpret_cast<u16x4u*>(p + c) = __builtin_bit_cast(u16x4u, o);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (c + e < d) p[c + e] = o[e];
+  }
+}
+
+struct RmsFwdParams {
+  const float* x;
+  const void* y;
+  const float* g;
+  float* x_out;
+  void* h;
+  uint8_t *q, *scale;
+  float* rstd;
+  int64_t rows, ldx, ldh, ldq;
+  int d;
+  float eps;
+};
+
+// NT threads to a row, VEC times four columns to a thread; a block of 64 threads per row has four rows.  F8: 0 no 8-bit output, 1 e4m3, 2 e5m2.
+template <int NT> constexpr int kBlock = NT < 256 ? 256 : NT;
+template <class T, int NT, int VEC, int F8>
+__global__ __launch_bounds__(kBlock<NT>) void rmsnorm_fwd_kernel(RmsFwdParams p) {
+  constexpr int kTeams = kBlock<NT> / NT, kWaves = NT / 64;
+  __shared__ float red[3][NT > 64 ? kWaves : 1];
+  const int team = NT < 256 ? threadIdx.x / NT : 0, t = threadIdx.x % NT, d = p.d;
+  const int64_t step = (int64_t)gridDim.x * kTeams;
+  const float inv_d = 1.f / (float)d;
+  f32x4 v[VEC], nx[VEC];
+  typename Stored<T>::type ny[VEC];
+  // The next row of this team travels while the current one is reduced and stored.
+  auto fetch = [&](int64_t n) {
+    const float* const xr = p.x + n * p.ldx;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) nx[i] = load4(xr, 4 * (t + i * NT), d);
+    if (p.y) {
+      const T* const yr = reinterpret_cast<const T*>(p.y) + n * p.ldh;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) ny[i] = Stored<T>::load(yr, 4 * (t + i * NT), d);
+    }
+  };
+  // Over the team; the sums of two calls in turn lie apart, so that one barrier is enough.
+  auto across = [&](float s, int place) {
+    s = lanes_sum(s);
+    if constexpr (NT > 64) {
+      if ((t & 63) == 0) red[place][t >> 6] = s;
+      __syncthreads();
+      s = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) s += red[place][w];
+    }
+    return s;
+  };
+  int64_t n = (int64_t)blockIdx.x * kTeams + team;
+  if (NT == 64 && n >= p.rows) return;
+  if (n < p.rows) fetch(n);
+  int phase = 0;
+  for (; n < p.rows; n += step, phase ^= 1) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      v[i] = nx[i];
+      if (p.y) v[i] += Stored<T>::wide(ny[i]);
+    }
+    if (n + step < p.rows) fetch(n + step);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) s += (v[i][0] * v[i][0] + v[i][1] * v[i][1]) + (v[i][2] * v[i][2] + v[i][3] * v[i][3]);
+    s = across(s, phase);
+    float r = 1.f / sqrtf(s * inv_d + p.eps);
+    // Squares that leave the range of 32 bits: once more, of values scaled by a power of two (uniform over the team).
+    const float mean = s * inv_d + p.eps;
+    if (!(mean > 0x1p-110f && s < INFINITY)) {
+      const float k = s < INFINITY ? 0x1p100f : 0x1p-80f;
+      s = 0.f;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const f32x4 w = v[i] * k;
+        s += (w[0] * w[0] + w[1] * w[1]) + (w[2] * w[2] + w[3] * w[3]);
+      }
+      r = k / sqrtf(across(s, 2) * inv_d + p.eps * k * k);
+    }
+    if (p.rstd && t == 0) p.rstd[n] = r;
+    if (p.x_out) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) store4(p.x_out + n * p.ldx, 4 * (t + i * NT), d, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const int c = 4 * (t + i * NT);
+      f32x4 h = v[i] * r;
+      if (c < d) h *= load4(p.g, c, d);
+      if (p.h) store4(reinterpret_cast<T*>(p.h) + n * p.ldh, c, d, h);
+      if constexpr (F8 != 0) {
+        constexpr bool E5M2 = F8 == 2;
+        uint32_t m = 0;
+        if (c + 4 > d) {                     // zeros behind the row, also where r is NaN
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[e] = c + e < d ? h[e] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t a = __float_as_uint(h[e]) & 0x7fffffffu;
+          m = max(m, a < 0x7f800000u ? a : 0u);
+        }
+        const uint32_t byte = scale_byte<E5M2>(lanes_max_bits<32>(m));
+        const uint32_t o = pack_f32<E5M2>(__float_as_uint(h[0]), __float_as_uint(h[1]), __float_as_uint(h[2]), __float_as_uint(h[3]),
+                                          __uint_as_float(byte << 23));
+        if (c < ((d + 15) & ~15)) *reinterpret_cast<uint32_t*>(p.q + n * p.ldq + c) = o;
+        if ((t & 31) == 0 && c < d) {
+          p.scale[scale_at(n, c >> 7, p.rows)] = (uint8_t)byte;
+          if (n == p.rows - 1)               // rows that do not exist
+            for (int64_t k = p.rows; k < ((p.rows + 63) & ~63LL); ++k) p.scale[scale_at(k, c >> 7, p.rows)] = 0;
+        }
+      }
+    }
+  }
+}
+
+// f(threads to a row, vectors to a thread) for rows of d columns.
+template <class F> void by_width(int64_t d, F&& f) {
+  using std::integral_constant;
+  if (d <= 256) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  else if (d <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  else if (d <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  else if (d <= 2048) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  else if (d <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  else if (d <= 8192) f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+  else f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+}
+constexpr int64_t kMaxCols = 16384, kMaxRows = (1LL << 31) - 1;
+
+// ---- backward ----------------------------------------------------------------------------------------------------
+// ROWS rows at a time to a team of NT threads; dg's running sums stay in registers, a team's go to ws[team][:] and a second kernel adds the
+// teams in order (the same bits on every run); one team writes dg itself.
+struct RmsBwdParams {
+  const void* dh;
+  const float *x, *g, *rstd, *dres;
+  float* dx;
+  void* dy;
+  float* part;                               // [teams][stride], or null: dg is not wanted
+  int64_t rows, ldx, ldh, stride;
+  int d, accumulate;                         // accumulate: one team adds into dg
+};
+template <class T, int NT, int VEC, int ROWS>
+__global__ __launch_bounds__(NT) void rmsnorm_bwd_kernel(RmsBwdParams p) {
+  constexpr int kWaves = NT / 64;
+  __shared__ float red[2][ROWS][kWaves];
+  const int t = threadIdx.x, d = p.d;
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  const float inv_d = 1.f / (float)d;
+  f32x4 gv[VEC], acc[VEC], xv[ROWS][VEC], rv[ROWS][VEC];
+  typename Stored<T>::type dv[ROWS][VEC];
+  float rs[ROWS];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    gv[i] = load4(p.g, 4 * (t + i * NT), d);
+    acc[i] = f32x4{};
+  }
+  auto fetch = [&](int64_t n0) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const int64_t n = n0 + r;
+      if (n >= p.rows) break;                // uniform
+      rs[r] = p.rstd[n];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const int c = 4 * (t + i * NT);
+        xv[r][i] = load4(p.x + n * p.ldx, c, d);
+        dv[r][i] = Stored<T>::load(reinterpret_cast<const T*>(p.dh) + n * p.ldh, c, d);
+        if (p.dres) rv[r][i] = load4(p.dres + n * p.ldx, c, d);
+      }
+    }
+  };
+  int64_t n0 = (int64_t)blockIdx.x * ROWS;
+  constexpr bool kAhead = NT < 1024;         // 128 registers to a thread hold a row's arrays once
+  if (kAhead && n0 < p.rows) fetch(n0);
+  int phase = 0;
+  for (; n0 < p.rows; n0 += step, phase ^= 1) {
+    if (!kAhead) fetch(n0);
+    f32x4 xh[ROWS][VEC], dg[ROWS][VEC], dr[ROWS][VEC];
+    float sum[ROWS], rr[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      sum[r] = 0.f;
+      rr[r] = rs[r];
+      if (n0 + r >= p.rows) continue;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const f32x4 dh = Stored<T>::wide(dv[r][i]);
+        xh[r][i] = xv[r][i] * rr[r];
+        if (p.dres) dr[r][i] = rv[r][i];
+        acc[i] += dh * xh[r][i];
+        dg[r][i] = dh * gv[i];
+        const f32x4 m = dg[r][i] * xh[r][i];
+        sum[r] += (m[0] + m[1]) + (m[2] + m[3]);
+      }
+    }
+    if (kAhead && n0 + step < p.rows) fetch(n0 + step);   // the next rows travel while these are reduced and stored
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) sum[r] = lanes_sum(sum[r]);
+    if constexpr (kWaves > 1) {
+      if ((t & 63) == 0) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) red[phase][r][t >> 6] = sum[r];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        sum[r] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum[r] += red[phase][r][w];
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const int64_t n = n0 + r;
+      if (n >= p.rows) break;
+      const float m = sum[r] * inv_d;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const int c = 4 * (t + i * NT);
+        f32x4 o = (dg[r][i] - xh[r][i] * m) * rr[r];
+        if (p.dres) o += dr[r][i];
+        store4(p.dx + n * p.ldx, c, d, o);
+        if (p.dy) store4(reinterpret_cast<T*>(p.dy) + n * p.ldh, c, d, o);
+      }
+    }
+  }
+  if (!p.part) return;
+  float* const out = p.part + (int64_t)blockIdx.x * p.stride;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    const int c = 4 * (t + i * NT);
+    if (p.accumulate) acc[i] += load4(out, c, d);
+    store4(out, c, d, acc[i]);
+  }
+}
+constexpr int kBwdTeams = 512;
+// Rows that a team takes at a time: what its registers hold twice over.
+template <int NT, int VEC> constexpr int kBwdRows = VEC <= 2 ? 4 : NT == 256 ? 2 : 1;
+// Threads to a row, vectors to a thread: registers are shared among more threads than in the forward pass, which holds less of a row.
+template <class F> void by_width_bwd(int64_t d, F&& f) {
+  using std::integral_constant;
+  if (d <= 256) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  else if (d <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  else if (d <= 1024) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (d <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  else if (d <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  else if (d <= 8192) f(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+  else f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+}
+int bwd_rows(int64_t d) {
+  int rows = 0;
+  by_width_bwd(d, [&](auto nt, auto vec) { rows = kBwdRows<decltype(nt)::value, decltype(vec)::value>; });
+  return rows;
+}
+int64_t bwd_teams(int64_t rows, int64_t d) {
+  const int per = bwd_rows(d);
+  const int64_t teams = (rows + per - 1) / per, most = d <= 512 ? 4 * kBwdTeams : kBwdTeams;
+  return teams < most ? teams : most;
+}
+
+hipError_t check(const RmsnormArgs& a) {
+  if ((a.dtype != kF32 && a.dtype != kBF16) || !a.g || a.rows < 0 || a.rows > kMaxRows || a.cols < 1 || a.cols > kMaxCols || a.ldx < a.cols ||
+      a.ldh < a.cols || !(a.eps >= 0.f) || ((uintptr_t)a.g & 3))
+    return hipErrorInvalidValue;
+  return hipSuccess;
+}
+bool misaligned(const void* p, int dtype) { return (uintptr_t)p & (dtype == kBF16 ? 1 : 3); }
+
+}  // namespace
+
+hipError_t launch_rmsnorm_fwd(hipStream_t s, const RmsnormArgs& a, const float* x, const void* y, float* x_out, void* h, const F8Out& q, float* rstd) {
+  if (check(a) != hipSuccess || !x || (!h && !q.q)) return hipErrorInvalidValue;
+  if (misaligned(x, kF32) || misaligned(y, a.dtype) || misaligned(x_out, kF32) || misaligned(h, a.dtype) || misaligned(rstd, kF32))
+    return hipErrorInvalidValue;
+  if (q.q && ((q.format != kE4M3 && q.format != kE5M2) || !q.scale || ((uintptr_t)q.scale & 3) || ((uintptr_t)q.q & 15) || q.ldq % 16 ||
+              q.ldq < a.cols || a.rows > (1LL << 30)))
+    return hipErrorInvalidValue;
+  if (a.rows == 0) return hipSuccess;
+  const RmsFwdParams p{x, y, a.g, x_out, h, (uint8_t*)q.q, q.scale, rstd, a.rows, a.ldx, a.ldh, q.ldq, (int)a.cols, a.eps};
+  auto run = [&](auto t, auto f8) {
+    by_width(a.cols, [&](auto nt, auto vec) {
+      constexpr int NT = decltype(nt)::value, VEC = decltype(vec)::value, kTeams = kBlock<NT> / NT;
+      const int64_t blocks = (a.rows + kTeams - 1) / kTeams, most = NT == 1024 ? 512 : NT == 256 ? 2048 : 1024;
+      rmsnorm_fwd_kernel<decltype(t), NT, VEC, decltype(f8)::value><<<(unsigned)(blocks < most ? blocks : most), kBlock<NT>, 0, s>>>(p);
+    });
+  };
+  auto format = [&](auto t) {
+    if (!q.q) run(t, std::integral_constant<int, 0>{});
+    else if (q.format == kE4M3) run(t, std::integral_constant<int, 1>{});
+    else run(t, std::integral_constant<int, 2>{});
+  };
+  if (a.dtype == kF32) format(float{});
+  else format(bf16{});
+  return hipGetLastError();
+}
+
+int64_t rmsnorm_bwd_ws_floats(int64_t rows, int64_t cols) {
+  if (rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxCols) return -1;
+  const int64_t teams = bwd_teams(rows, cols);
+  return teams > 1 ? teams * ((cols + 3) & ~3LL) : 0;
+}
+
+hipError_t launch_rmsnorm_bwd(hipStream_t s, const RmsnormArgs& a, const void* dh, const float* x, const float* rstd, const float* dres, float* dx,
+                              void* dy, float* dg, float* ws, int accumulate) {
+  if (check(a) != hipSuccess || !dh || !x || !rstd || !dx) return hipErrorInvalidValue;
+  if (misaligned(dh, a.dtype) || misaligned(x, kF32) || misaligned(rstd, kF32) || misaligned(dres, kF32) || misaligned(dx, kF32) ||
+      misaligned(dy, a.dtype) || misaligned(dg, kF32))
+    return hipErrorInvalidValue;
+  const int64_t teams = bwd_teams(a.rows, a.cols);
+  if (dg && teams > 1 && (!ws || ((uintptr_t)ws & 15))) return hipErrorInvalidValue;
+  if (a.rows == 0) return dg && !accumulate ? launch_reduce_parts(s, dg, dg, 0, 0, a.cols, 0) : hipSuccess;   // zeros
+  const int64_t stride = (a.cols + 3) & ~3LL;
+  const bool alone = teams == 1;
+  const RmsBwdParams p{dh, x, a.g, rstd, dres, dx, dy, dg ? (alone ? dg : ws) : nullptr, a.rows, a.ldx, a.ldh, stride, (int)a.cols,
+                       alone && accumulate};
+  auto run = [&](auto t) {
+    by_width_bwd(a.cols, [&](auto nt, auto vec) {
+      constexpr int NT = decltype(nt)::value, VEC = decltype(vec)::value;
+      rmsnorm_bwd_kernel<decltype(t), NT, VEC, kBwdRows<NT, VEC>><<<(unsigned)teams, NT, 0, s>>>(p);
+    });
+  };
+  if (a.dtype == kF32) run(float{});
+  else run(bf16{});
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || !dg || alone ? e : launch_reduce_parts(s, ws, dg, (int)teams, stride, a.cols, accumulate);
+}
+
+}  // namespace pw

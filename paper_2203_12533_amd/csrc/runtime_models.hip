@@ -358,6 +358,52 @@ pw_status pw_op_scan_bwd(pw_ctx* c, const pw_scan_args* a, const void* dy, int64
 int64_t pw_scan_state_floats(int64_t B, int64_t T, int64_t D) { return scan_state_floats(B, T, D); }
 int64_t pw_scan_ws_floats(int64_t B, int64_t T, int64_t D) { return scan_ws_floats(B, T, D); }
 
+int64_t pw_f4_scale_bytes(int64_t rows, int64_t cols) { return f4_scale_bytes(rows, cols); }
+pw_status pw_op_f4_quantize(pw_ctx* c, const pw_f4_quantize_args* a) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_f4_quantize(c->exec, F4QuantizeArgs{a->dtype, a->block_rows, a->x, a->rows, a->cols, a->ldx, a->q, a->ldq,
+                                                               a->q_scale, a->qt, a->ldqt, a->qt_scale}));
+}
+pw_status pw_op_f4_gemm(pw_ctx* c, const pw_f4_gemm_args* a) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_gemm_f4(c->exec, GemmF4Args{a->M, a->N, a->K, a->lda, a->ldb, a->ldc, a->epilogue, a->out_dtype, a->accumulate,
+                                                       a->A, a->B, a->a_scale, a->b_scale, a->bias, a->aux, a->C, a->C2}));
+}
+static RmsnormArgs rmsnorm_args_of(const pw_rmsnorm_args* a) { return RmsnormArgs{a->dtype, a->rows, a->cols, a->ldx, a->ldh, a->eps, a->g}; }
+pw_status pw_op_rmsnorm_fwd(pw_ctx* c, const pw_rmsnorm_args* a, const float* x, const void* y, float* x_out, void* h, const pw_f8_out* q,
+                            float* rstd) {
+  if (!c || !a || (q && !q->q)) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_rmsnorm_fwd(c->exec, rmsnorm_args_of(a), x, y, x_out, h, q ? F8Out{q->format, q->q, q->ldq, q->scale} : F8Out{}, rstd));
+}
+pw_status pw_op_rmsnorm_bwd(pw_ctx* c, const pw_rmsnorm_args* a, const void* dh, const float* x, const float* rstd, const float* dres, float* dx,
+                            void* dy, float* dg, float* ws, int accumulate) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_rmsnorm_bwd(c->exec, rmsnorm_args_of(a), dh, x, rstd, dres, dx, dy, dg, ws, accumulate));
+}
+int64_t pw_rmsnorm_bwd_ws_floats(int64_t rows, int64_t cols) { return rmsnorm_bwd_ws_floats(rows, cols); }
+static LogprobArgs logprob_args_of(const pw_logprob_args* a) {
+  return LogprobArgs{a->dtype, a->z, a->ldz, a->rows, a->vocab, a->targets, a->scale};
+}
+pw_status pw_op_logprob_fwd(pw_ctx* c, const pw_logprob_args* a, float* logp, float* entropy, float* stats, int k, int32_t* top_id, float* top_logp,
+                            float* ws) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_logprob_fwd(c->exec, logprob_args_of(a), logp, entropy, stats, k, top_id, top_logp, ws));
+}
+int64_t pw_logprob_ws_floats(int64_t rows, int64_t vocab, int k) { return logprob_ws_floats(rows, vocab, k); }
+pw_status pw_op_logprob_bwd(pw_ctx* c, const pw_logprob_args* a, const float* stats, const float* entropy, const float* dlogp, const float* dentropy,
+                            void* dz, int64_t lddz) {
+  if (!c || !a) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_logprob_bwd(c->exec, logprob_args_of(a), stats, entropy, dlogp, dentropy, dz, lddz));
+}
+pw_status pw_op_grad_clip(pw_ctx* c, const pw_grad_tensor* t, int count, float max_norm, float* result, float* ws) {
+  static_assert(sizeof(pw_grad_tensor) == sizeof(GradTensor) && offsetof(pw_grad_tensor, g) == offsetof(GradTensor, g) &&
+                offsetof(pw_grad_tensor, out) == offsetof(GradTensor, out) && offsetof(pw_grad_tensor, n) == offsetof(GradTensor, n) &&
+                offsetof(pw_grad_tensor, dtype) == offsetof(GradTensor, dtype), "read as they are");
+  if (!c) return PW_ERR_INVALID;
+  PW_OP_ON_DEVICE(c, launch_grad_clip(c->exec, reinterpret_cast<const GradTensor*>(t), count, max_norm, result, ws));
+}
+int64_t pw_grad_clip_ws_floats(void) { return grad_clip_ws_floats(); }
+
 pw_status pw_profile_begin(pw_ctx* c) {
   if (!c) return PW_ERR_INVALID;
   gemm_profile_begin();
