@@ -145,13 +145,360 @@ __device__ __forceinline__ int read_scales(uint32_t at) {
   return *(p)(uintptr_t)at;
 }
 
-// Fragments are read one block of rows ahead of their use and MFMAs run across k tiles without a pause; see the comment in gemm_f8.hip on the
-// order of reads, waits and loads, which is the same here with two instructions deep for one.
+// ---- whole tiles of 256 x 256, one workgroup to a compute unit, one tile after the other ---------------------------------------------------
+// What a launch of one tile per workgroup leaves idle is the time between tiles: the first loads of the next and the way of the
+// results out, 10 of 22 us where k = 2048.  So a workgroup keeps its place and the k tiles of its output tiles form one stream: while the
+// last k tiles of one are multiplied, the first of the next are on their way into LDS and into the first fragments, and the results
+// leave from registers, in stores that nobody waits for.
+// What lies behind k in the last k tile is never made zero: scales of 0 (2^-127) on both sides make a product of any two e2m1 numbers vanish
+// (36 * 2^-254), so the lanes that would read behind the row read its beginning again, and one loop body serves every k tile.
+template <int WM_, int WN_, int FM_, int FN_>
+struct Stream {
+  static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, G = WM * WN, kThreads = 64 * G;
+  static constexpr int BM = 16 * WM * FM, BN = 16 * WN * FN;
+  static constexpr int kHalfScales = (BM + BN) * 4, kPieces = 2 * kHalfScales / 16, kSets = kPieces / 64;
+  static constexpr int kOperands = (BM + BN) * kRowBytes, kStage = kOperands + kSets * 1024;
+  static constexpr int kBiases = 2;                       // the next output tile's is on its way while one is used
+  static constexpr size_t kSmem = 2 * kStage + kBiases * BN * 4;
+  static_assert(kSets <= G && G % kSets == 0 && kPieces % 64 == 0 && kSmem <= 160 * 1024);
+};
+
+// Four consecutive columns of a row as bf16.
+__device__ __forceinline__ uint2 pack4(const f32x4& v) {
+  return make_uint2(__builtin_bit_cast(uint32_t, bf16x2{(bf16)v[0], (bf16)v[1]}), __builtin_bit_cast(uint32_t, bf16x2{(bf16)v[2], (bf16)v[3]}));
+}
+// Lane 16 q + l has columns 16 j + 4 q .. of row l, j = 0, 1; afterwards 8 q .. 8 q + 7 of the 32.
+__device__ __forceinline__ uint4 join_columns(uint2 a, uint2 b) {
+  auto turn = [](uint32_t& x, uint32_t& y) {
+    const auto p = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    const auto r = __builtin_amdgcn_permlane16_swap(p[0], p[1], false, false);
+    x = r[0];
+    y = r[1];
+  };
+  turn(a.x, b.x);
+  turn(a.y, b.y);
+  return make_uint4(a.x, a.y, b.x, b.y);
+}
+
+// Results of a wave from registers: acc[i][j] is element (16 i + lane % 16, 16 j + 4 (lane / 16) + r) of its tile at (m0, n0).
+// WHOLE: all of it exists; rows leave in pieces of 64 bytes.  Else vectors of four columns where four exist, and elements.
+template <int FM, int FN, int KIND, bool F32, bool WHOLE>
+__device__ __forceinline__ void store_tile(f32x4 (&acc)[FM][FN], const EpiParams& e, int64_t M, int64_t N, int64_t m0, int64_t n0, int lane) {
+  static_assert(FN % 2 == 0);
+  const int L = lane & 15, q = lane >> 4;
+  const int64_t left = N - n0 - 4 * q;                    // columns from the lane's first on
+  const int tail = (int)left & 3, last = left < 0 ? -1 : left >= 16 * FN ? FN : (int)left >> 4;   // the block of columns that the row ends in ...
+  const bool odd = tail && last >= 0 && last < FN && left - 16 * last < 4;                   // ... among this lane's four
+  const bool two = e.mode == kEpiBiasGelu;
+  auto extra = [&](int64_t at) {                          // what the epilogue reads besides
+    if constexpr (KIND == kExtraAuxBf16) {
+      const uint2 u = *reinterpret_cast<const uint2*>(reinterpret_cast<const bf16*>(e.aux) + at);
+      return make_uint4(u.x, u.y, 0, 0);
+    } else {
+      return *reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(KIND == kExtraOldC ? e.C : e.aux) + at);
+    }
+  };
+  auto with = [&](const f32x4& a, const uint4& x) {
+    f32x4 v = a;
+    if constexpr (KIND == kExtraAuxBf16) {
+      const uint32_t w[2] = {x.x, x.y};
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] *= gelu_grad_f(__uint_as_float(r & 1 ? w[r / 2] & 0xffff0000u : w[r / 2] << 16));
+    } else if constexpr (KIND != kExtraNone) {
+      v += __builtin_bit_cast(f32x4, x);
+    }
+    return v;
+  };
+  auto gelu4 = [](const f32x4& v) { return f32x4{gelu_f(v[0]), gelu_f(v[1]), gelu_f(v[2]), gelu_f(v[3])}; };
+  uint4 x[FN];
+  auto fetch = [&](int i) {                               // a block of rows ahead
+    if constexpr (KIND != kExtraNone) {
+      const int64_t row = (m0 + 16 * i + L) * e.ldc + n0 + 4 * q;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        if (WHOLE || (m0 + 16 * i + L < M && 16 * j + 4 <= left)) x[j] = extra(row + 16 * j);
+    }
+  };
+  fetch(0);
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    const int64_t m = m0 + 16 * i + L, row = m * e.ldc + n0;
+    f32x4 v[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) v[j] = with(acc[i][j], x[j]);
+    if (i + 1 < FM) fetch(i + 1);
+    if constexpr (WHOLE) {
+      auto put = [&](void* to, auto&& value) {
+        if constexpr (F32) {
+#pragma unroll
+          for (int j = 0; j < FN; ++j) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(to) + row + 16 * j + 4 * q) = value(j);
+        } else {
+#pragma unroll
+          for (int j = 0; j < FN; j += 2)
+            *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(to) + row + 16 * j + 8 * q) = join_columns(pack4(value(j)), pack4(value(j + 1)));
+        }
+      };
+      put(e.C, [&](int j) { return v[j]; });
+      if (two) put(e.C2, [&](int j) { return gelu4(v[j]); });
+    } else {
+      if (m < M) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          if (16 * j + 4 <= left) {
+            const int64_t at = row + 16 * j + 4 * q;
+            if constexpr (F32) {
+              *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(e.C) + at) = v[j];
+              if (two) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(e.C2) + at) = gelu4(v[j]);
+            } else {
+              *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(e.C) + at) = pack4(v[j]);
+              if (two) *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(e.C2) + at) = pack4(gelu4(v[j]));
+            }
+          }
+        }
+        if (odd) {
+          f32x4 a = acc[i][0];
+#pragma unroll
+          for (int j = 1; j < FN; ++j) a = last == j ? acc[i][j] : a;
+          EpiParams bare = e;
+          bare.bias = nullptr;
+#pragma unroll 1
+          for (int r = 0; r < tail; ++r) epilogue1<true>(bare, m, n0 + 16 * last + 4 * q + r, r == 0 ? a[0] : r == 1 ? a[1] : a[2]);
+        }
+      }
+    }
+  }
+  // What was loaded is there, and the compiler knows: it would wait for everything in every k tile otherwise, the direct loads among it.
+  if (KIND != kExtraNone || !WHOLE) __builtin_amdgcn_s_waitcnt(0x0f70);
+}
+
+// The same number; what is computed from it is computed where it stands and not kept in registers across the loop.
+__device__ __forceinline__ int fresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+template <class S, bool F32>
+__global__ __launch_bounds__(S::kThreads, S::G / 4) void gemm_f4_stream_kernel(GemmF4Params p) {
+  constexpr int FM = S::FM, FN = S::FN, G = S::G, WN = S::WN;
+  using OpA = Operand<S::BM, G, true>;
+  using OpB = Operand<S::BN, G, false>;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  narrow<F32>(p.epi);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wm = wave / WN, wn = wave % WN, L = lane & 15, quarter = lane >> 4;
+  const int tiles = p.tiles_m * p.tiles_n, n = (int)((p.K + kF4BK - 1) / kF4BK);
+  const uint32_t ring = (uint32_t)(uintptr_t)(lds_ptr)smem, biases = ring + 2 * S::kStage;
+  const float* const bias = epi_has_bias(p.epi.mode) ? p.epi.bias : nullptr;
+  p.epi.bias = nullptr;                                     // added before the epilogue
+
+  // Where loads are: k tile `kt` of output tile `to`, the `count`-th of this workgroup (at least two k tiles to one).  Scales of a k tile as in the kernel below.
+  const int64_t Ra = ((p.M + 63) & ~63LL) * 4, Rb = ((p.N + 63) & ~63LL) * 4;
+  const int piece = wave % S::kSets * 64 + lane, half = piece / (S::kPieces / 2), pos = piece % (S::kPieces / 2) * 16;
+  const bool of_a = pos < S::BM * 4;
+  const int scale_block = half * 4 + (pos >> 6 & 3);
+  const int64_t step = of_a ? Ra : Rb;
+  OpA oa;
+  OpB ob;
+  const uint8_t* sq;
+  int kt = 0, to = blockIdx.x, count = 0;
+  const bool partial = p.K % kF4BK != 0;
+  auto begin = [&] {                                        // the loads of output tile `to`
+    int tm, tn;
+    tile_of_block(to, tiles, p.tiles_m, p.tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+    const int mine = fresh(lane);
+    oa.init(p.A, p.lda, m0, p.M, 0, wave, mine);
+    ob.init(p.B, p.ldb, n0, p.N, 0, wave, mine);
+    const int64_t row_at = of_a ? m0 * 4 + pos : n0 * 4 + pos - S::BM * 4;
+    sq = (of_a ? p.sa : p.sb) + (row_at < step ? row_at : step - 256 + (row_at & 255)) + half * step;
+    if (bias) {                                             // 64 columns by a wave, the same ones by several
+      const int64_t c = n0 + wave % (S::BN / 64) * 64 + mine;
+      dma4(reinterpret_cast<const uint8_t*>(bias + (c < p.N ? c : p.N - 1)), biases + (count % S::kBiases) * (S::BN * 4) + wave % (S::BN / 64) * 256);
+    }
+  };
+  constexpr int kPer = OpA::kPer + OpB::kPer, kLoads = kPer + 1;    // direct loads of a wave per k tile
+  constexpr int kSecond = OpA::kPer / 2, kFirst = kPer - kSecond;   // the first: all but the second half of A
+  // The last k tile of an output tile is a partial one: lanes whose place in it is behind the row go back to the tile's beginning.
+  auto shorten = [&] {
+    const int64_t left = (p.K - (int64_t)kt * kF4BK) / 2;
+    const int mine = fresh(lane);
+#pragma unroll
+    for (int j = 0; j < OpB::kPer; ++j) ob.off[j] -= OpB::k_of(OpB::piece(wave, j), mine) < left ? 0 : OpB::k_of(OpB::piece(wave, j), mine);
+#pragma unroll
+    for (int j = 0; j < OpA::kPer; ++j) oa.off[j] -= OpA::k_of(OpA::piece(wave, j), mine) < left ? 0 : OpA::k_of(OpA::piece(wave, j), mine);
+  };
+  auto issue_one = [&](int m, uint32_t at) {                // load m of the k tile into the stage at `at`
+    const uint32_t st = ring + at;
+    if (m < OpB::kPer) ob.issue_one(m, st + S::BM * kRowBytes, wave);
+    else oa.issue_one(m - OpB::kPer, st, wave);
+    if (m == OpB::kPer - 1) {
+      ob.base += kRowBytes;
+      const bool there = (int64_t)kt * kF4BK + scale_block * 32 < p.K;
+      dma16(there ? sq : reinterpret_cast<const uint8_t*>(kZeros), st + S::kOperands + wave % S::kSets * 1024);
+      sq += 2 * step;
+    }
+    if (m == kPer - 1) {
+      oa.base += kRowBytes;
+      ++kt;
+    }
+  };
+
+  const uint32_t row_a = ring + (wm * FM * 16 + L) * kRowBytes, row_b = ring + S::BM * kRowBytes + (wn * FN * 16 + L) * kRowBytes;
+  const uint32_t c0 = (quarter ^ (L >> 1)) << 4, c1 = ((quarter + 4) ^ (L >> 1)) << 4;
+  constexpr int GA = FM / 4, GB = FN / 4;                   // words of four scales for 128 k
+  static_assert(FM % 4 == 0 && FN % 4 == 0);
+  const uint32_t s_a = ring + S::kOperands + wm * FM * 64 + lane * 4, s_b = ring + S::kOperands + (S::BM + wn * FN * 16) * 4 + lane * 4;
+  // All but the `later` direct loads asked for last are there, and this wave's LDS reads are done; then those of all waves.
+  auto landed = [&](auto later) { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(later)::value) : "memory"); };
+  auto meet = [&] {
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  f32x4 acc[FM][FN];
+  i32x4 fa[2][2], fb[2][FN];                                // [k half][block]
+  int sa[2][GA], sb[2][GB], nsa[2][GA], nsb[2][GB];
+  struct At { uint32_t v[4]; };
+  auto at_of = [&](uint32_t st) {                           // kept whole, so that what is constant in them goes into the instructions
+    At r{{row_a + c0 + st, row_a + c1 + st, row_b + c0 + st, row_b + c1 + st}};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(r.v[k]));
+    return r;
+  };
+  auto read_a = [&](const At& at, int i) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) fa[h][i & 1] = read_fragment(at.v[h] + i * 16 * kRowBytes);
+  };
+  auto read_b = [&](const At& at, int j, int h) { fb[h][j] = read_fragment(at.v[2 + h] + j * 16 * kRowBytes); };
+  auto read_scale = [&](uint32_t st, int g) {
+    const int h = g / (GA + GB), w = g % (GA + GB);
+    if (w < GA) nsa[h][w] = read_scales(s_a + st + h * S::kHalfScales + w * 256);
+    else nsb[h][w - GA] = read_scales(s_b + st + h * S::kHalfScales + (w - GA) * 256);
+  };
+  auto take_scales = [&] {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int g = 0; g < GA; ++g) sa[h][g] = nsa[h][g];
+#pragma unroll
+      for (int g = 0; g < GB; ++g) sb[h][g] = nsb[h][g];
+    }
+  };
+  // A k tile: a unit is one block of rows against all columns of the wave.  The next block's fragments are read while a unit runs, the next
+  // k tile's columns take the place of this one's as those are used for the last time.  Columns and scales are in registers when the k tile
+  // begins, so halfway (kHalf), where the waves meet, the place of the columns and of the first half of the rows is free for the k tile after
+  // the next; that of the second half one unit before the end (kTurn), where the next k tile is there.  Loads go out between the MFMAs.
+  // No branches inside: the compiler would move MFMAs past them.
+  constexpr int kTurn = FM - 1, kHalf = FM / 2 - 1, kSlots = 2 * FN;
+  static_assert(2 * (GA + GB) <= kSlots, "a slot for each word of scales");
+  auto tile = [&](uint32_t st, uint32_t next) {
+    const At here = at_of(st), there = at_of(next);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      if (i == kHalf) {
+        landed(std::integral_constant<int, kLoads>{});
+        meet();
+      }
+      if (i == kTurn) {
+        landed(std::integral_constant<int, kLoads>{});
+        meet();
+      }
+#pragma unroll
+      for (int hj = 0; hj < 2 * FN; ++hj) {
+        const int h = hj / FN, jj = hj % FN;
+        // back and forth: consecutive MFMAs share an operand; the last unit and the next tile's first in one order
+        const int j = (i & 1) || i == 0 ? jj : FN - 1 - jj, slot = (i - kTurn) * 2 * FN + hj;
+        __builtin_amdgcn_sched_barrier(0);
+        if (i < FM - 1 && hj == (i == 0 ? 1 : 0)) read_a(here, i + 1);   // behind the first MFMA of a tile, so that its wait does not cover this
+        if (slot >= 0) {
+          if (slot < 2 * (GA + GB)) read_scale(next, slot);
+          if (slot == 0) read_a(there, 0);
+#pragma unroll
+          for (int m = slot * kSecond / kSlots; m < (slot + 1) * kSecond / kSlots; ++m) issue_one(kFirst + m, st);
+        }
+        if (i >= kHalf && i < kTurn) {
+          constexpr int slots = (kTurn - kHalf) * 2 * FN;
+          const int at = (i - kHalf) * 2 * FN + hj;
+#pragma unroll
+          for (int m = at * kFirst / slots; m < (at + 1) * kFirst / slots; ++m) issue_one(m, st);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        acc[i][j] = mfma(fb[h][j], fa[h][i & 1], acc[i][j], j % 4, sb[h][j / 4], i % 4, sa[h][i / 4]);
+        if (i == FM - 1) {           // the fragment's last use
+          __builtin_amdgcn_sched_barrier(0);
+          read_b(there, j, h);
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    take_scales();
+  };
+  begin();
+#pragma unroll 1
+  for (uint32_t at = 0; at <= S::kStage; at += S::kStage) {
+    if (partial && kt == n - 1) shorten();
+#pragma unroll
+    for (int m = 0; m < kPer; ++m) issue_one(m, at);
+  }
+  landed(std::integral_constant<int, kLoads + kSecond>{});
+  meet();
+#pragma unroll
+  for (int g = 0; g < 2 * (GA + GB); ++g) read_scale(0, g);
+  take_scales();
+  {
+    const At here = at_of(0);
+    read_a(here, 0);
+#pragma unroll
+    for (int j = 0; j < 2 * FN; ++j) read_b(here, j % FN, j / FN);
+  }
+  uint32_t st = 0;
+  int done = 0;
+  for (int o = blockIdx.x; o < tiles; o += gridDim.x, ++done) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < n; ++t) {
+      if (t + 2 == n) {                      // loads are two k tiles ahead; behind the last output tile they fetch it once more, for nobody
+        if (to + (int)gridDim.x < tiles) to += gridDim.x;
+        ++count;
+        kt = 0;
+        begin();
+      }
+      if (partial && kt == n - 1) shorten();
+      tile(st, S::kStage - st);
+      st = S::kStage - st;
+    }
+    int tm, tn;
+    tile_of_block(o, tiles, p.tiles_m, p.tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+    if (bias) {
+      typedef __attribute__((address_space(3))) const f32x4* at;
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const f32x4 b = *(at)(uintptr_t)(biases + (done % S::kBiases) * (S::BN * 4) + (wn * FN * 16 + 16 * j + 4 * (fresh(lane) >> 4)) * 4);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) acc[i][j] += b;
+      }
+    }
+    const bool whole = m0 + S::BM <= p.M && n0 + S::BN <= p.N;
+    with_extra<F32>(p.epi, [&](auto kind) {
+      constexpr int K = decltype(kind)::value;
+      if (whole) store_tile<FM, FN, K, F32, true>(acc, p.epi, p.M, p.N, m0 + wm * FM * 16, n0 + wn * FN * 16, fresh(lane));
+      else store_tile<FM, FN, K, F32, false>(acc, p.epi, p.M, p.N, m0 + wm * FM * 16, n0 + wn * FN * 16, fresh(lane));
+    });
+  }
+  landed(std::integral_constant<int, 0>{});  // nothing is on its way into LDS any more
+}
+
+// ---- one tile to a workgroup ----------------------------------------------------------------------------------------------------------------------
+// Fragments are read one block of rows ahead of their use and MFMAs run across k tiles without a pause.  All of a k tile has been read from
+// LDS one unit (a block of rows against all columns of the wave) before its end; there (kTurn) the waves of a group meet, the next k
+// tile is there, and the stage of this one is free for k tile t + NS.
 template <class S, bool F32>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f4_tile_kernel(GemmF4Params p) {
   constexpr int FM = S::FM, FN = S::FN, G = S::G, WN = S::WN;
-  constexpr bool SPLIT = FM == 8 && G == 8;
-  using OpA = Operand<S::BM, G, SPLIT>;
+  using OpA = Operand<S::BM, G, false>;
   using OpB = Operand<S::BN, G, false>;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   narrow<F32>(p.epi);
@@ -189,18 +536,15 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f4_tile_ke
     dma16(there ? sq : reinterpret_cast<const uint8_t*>(kZeros), to);
     sq += 2 * step;
   };
-  // k tile t into the stage at `at`; zeros where it does not exist.  part: 1 all but the second half of A, 2 that, 0 both.
-  auto issue = [&](int t, uint32_t at, int part) {
+  // k tile t into the stage at `at`; zeros where it does not exist.
+  auto issue = [&](int t, uint32_t at) {
     const int64_t left = (p.K - (int64_t)(first + t) * kF4BK) / 2;
     const uint32_t st = ring + at;
-    if (part != 2) {
-      ob.issue(left, st + S::BM * kRowBytes, gw, lane);
-      ob.base += kRowBytes;
-      issue_scales(t, st, false);
-      oa.issue(left, st, gw, lane, 0, SPLIT ? OpA::kPer / 2 : OpA::kPer);
-    }
-    if (SPLIT && part != 1) oa.issue(left, st, gw, lane, OpA::kPer / 2);
-    if (!SPLIT || part != 1) oa.base += kRowBytes;
+    ob.issue(left, st + S::BM * kRowBytes, gw, lane);
+    ob.base += kRowBytes;
+    issue_scales(t, st, false);
+    oa.issue(left, st, gw, lane);
+    oa.base += kRowBytes;
   };
   // Addresses of this lane's fragments: block j of an operand is 16 j rows of 128 bytes further on, which leaves the swizzle
   // of the row as it is.
@@ -261,22 +605,16 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f4_tile_ke
   // STREAM: tile t + NS is a whole one; MORE: tile t + 1 exists (t + NS, where it does not, is made of zeros nobody reads).  No
   // branches inside: the compiler would move MFMAs past them.
   constexpr int kTurn = FM - 1, kSlots = (FM - kTurn) * 2 * FN;
-  constexpr int kHalf = FM / 2 - 1, kSecond = SPLIT ? OpA::kPer / 2 : kPer, kFirst = kPer - kSecond;
   static_assert(FM % 2 == 0 && 2 * (GA + GB) <= 2 * FN, "two fragments of rows in turn; a slot for each word of scales");
   auto tile = [&](int t, uint32_t st, uint32_t next, auto streaming, auto follows) {
     constexpr bool STREAM = decltype(streaming)::value, more = decltype(follows)::value;
     const At here = at_of(st), there = at_of(next);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      if (SPLIT && i == kHalf) {
-        landed(std::integral_constant<int, kLoads>{});
-        meet();
-        if (more && !STREAM) issue(t + S::NS, st, 1);
-      }
       if (i == kTurn && more) {
-        landed(std::integral_constant<int, SPLIT ? kLoads : (S::NS - 2) * kLoads>{});
+        landed(std::integral_constant<int, (S::NS - 2) * kLoads>{});
         meet();
-        if (!STREAM) issue(t + S::NS, st, SPLIT ? 2 : 0);
+        if (!STREAM) issue(t + S::NS, st);
       }
 #pragma unroll
       for (int hj = 0; hj < 2 * FN; ++hj) {
@@ -290,14 +628,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f4_tile_ke
           if (slot == 0) read_a(there, 0);
           if (STREAM) {
 #pragma unroll
-            for (int m = slot * kSecond / kSlots; m < (slot + 1) * kSecond / kSlots; ++m) issue_one(t + S::NS, kFirst + m, st);
+            for (int m = slot * kPer / kSlots; m < (slot + 1) * kPer / kSlots; ++m) issue_one(t + S::NS, m, st);
           }
-        }
-        if (SPLIT && STREAM && i >= kHalf && i < kTurn) {
-          constexpr int slots = kTurn > kHalf ? (kTurn - kHalf) * 2 * FN : 1;
-          const int at = (i - kHalf) * 2 * FN + hj;
-#pragma unroll
-          for (int m = at * kFirst / slots; m < (at + 1) * kFirst / slots; ++m) issue_one(t + S::NS, m, st);
         }
         __builtin_amdgcn_sched_barrier(0);
         acc[i][j] = mfma(fb[h][j], fa[h][i & 1], acc[i][j], j % 4, sb[h][j / 4], i % 4, sa[h][i / 4]);
@@ -321,8 +653,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f4_tile_ke
   };
   if (n > 0) {
 #pragma unroll
-    for (int i = 0; i < S::NS; ++i) issue(i, i * S::kStage, 0);
-    landed(std::integral_constant<int, (S::NS - 1) * kLoads + (SPLIT ? kSecond : 0)>{});
+    for (int i = 0; i < S::NS; ++i) issue(i, i * S::kStage);
+    landed(std::integral_constant<int, (S::NS - 1) * kLoads>{});
     meet();
 #pragma unroll
     for (int g = 0; g < 2 * (GA + GB); ++g) read_scale(0, g);
@@ -399,12 +731,27 @@ __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f4_tile_ke
   }
 }
 
-using Big = Tile<2, 4, 8, 4, 1>;        // 256 x 256
+using Big = Stream<2, 4, 8, 4>;         // 256 x 256
 using Mid = Tile<2, 2, 4, 4, 1>;        // 128 x 128, two workgroups to a compute unit
 using Half = Tile<2, 2, 4, 2, 1, 3>;    // 128 x 64
 using Split = Tile<1, 1, 4, 4, 4>;      // 64 x 64, k over four waves
 using Few = Tile<1, 1, 2, 4, 4, 2>;     // 32 x 64, likewise
 
+constexpr int kUnits = 256;             // compute units
+hipError_t prepare_big() {
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_f4_stream_kernel<Big, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Big::kSmem);
+  return e != hipSuccess ? e : hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_f4_stream_kernel<Big, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)Big::kSmem);
+}
+hipError_t launch_big(hipStream_t s, GemmF4Params p, bool f32) {
+  const int64_t tm = (p.M + Big::BM - 1) / Big::BM, tn = (p.N + Big::BN - 1) / Big::BN;
+  if (tm * tn > (1LL << 30)) return hipErrorInvalidValue;
+  p.tiles_m = (int)tm;
+  p.tiles_n = (int)tn;
+  const int blocks = tm * tn < kUnits ? (int)(tm * tn) : kUnits;
+  if (f32) gemm_f4_stream_kernel<Big, true><<<blocks, Big::kThreads, Big::kSmem, s>>>(p);
+  else gemm_f4_stream_kernel<Big, false><<<blocks, Big::kThreads, Big::kSmem, s>>>(p);
+  return hipGetLastError();
+}
 template <class S>
 hipError_t prepare() {
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_f4_tile_kernel<S, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
@@ -439,14 +786,14 @@ hipError_t choose(hipStream_t s, const GemmF4Params& p, bool f32) {
   if (tiles(Split::BM, Split::BN) <= 256) return launch<Split>(s, p, f32);
   if (tiles(Half::BM, Half::BN) <= 256) return launch<Half>(s, p, f32);
   const int64_t big = tiles(Big::BM, Big::BN), slots = (big + 255) / 256 * 256;
-  if (big <= 256 ? big >= 144 : 100 * big > 72 * slots) return launch<Big>(s, p, f32);
+  if (p.K > kF4BK && (big <= 256 ? big >= 144 : 100 * big > 72 * slots)) return launch_big(s, p, f32);
   return launch<Mid>(s, p, f32);
 }
 
 }  // namespace
 
 hipError_t gemm_f4_init() {
-  hipError_t e = prepare<Big>();
+  hipError_t e = prepare_big();
   if (e == hipSuccess) e = prepare<Mid>();
   if (e == hipSuccess) e = prepare<Half>();
   if (e == hipSuccess) e = prepare<Split>();

@@ -6,6 +6,8 @@
 // operations per element where memory allows for ten.  Two launches for up to kGroup tensors, whose addresses travel with the launch: blocks
 // take chunks of tensors in turn and leave a sum each, then every block of the second adds those sums in the same order (4096 or fewer
 // bytes, from the cache) and scales its chunks.  Bound by memory: two reads and a write of 4 (2) bytes.
+#include <type_traits>
+
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -28,6 +30,76 @@ static_assert(sizeof(Group) <= 3500, "with the launch");
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+
+// A chunk's vectors of one thread: v[i] holds elements (i * kThreads + thread) * E .. of n; zeros behind the end.
+template <class T> struct Piece;
+template <> struct Piece<float> {
+  static constexpr int E = 4, kVecs = kChunk / E / kThreads;
+  f32x4u v[kVecs];
+  __device__ __forceinline__ void load(const float* g, int n) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int at = (i * kThreads + threadIdx.x) * E;
+      if (at + E <= n) {
+        v[i] = *reinterpret_cast<const f32x4u*>(g + at);
+      } else {
+        v[i] = f32x4u{};
+#pragma unroll
+        for (int e = 0; e < E - 1; ++e)
+          if (at + e < n) v[i][e] = g[at + e];
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int i, int e) const { return v[i][e]; }
+  __device__ __forceinline__ void store(float* o, int n, float f) const {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int at = (i * kThreads + threadIdx.x) * E;
+      if (at + E <= n) {
+        *reinterpret_cast<f32x4u*>(o + at) = v[i] * f;
+      } else {
+#pragma unroll
+        for (int e = 0; e < E - 1; ++e)
+          if (at + e < n) o[at + e] = v[i][e] * f;
+      }
+    }
+  }
+};
+template <> struct Piece<bf16> {
+  static constexpr int E = 8, kVecs = kChunk / E / kThreads;
+  u32x4u v[kVecs];
+  __device__ __forceinline__ void load(const bf16* g, int n) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int at = (i * kThreads + threadIdx.x) * E;
+      if (at + E <= n) {
+        v[i] = *reinterpret_cast<const u32x4u*>(g + at);
+      } else {
+        v[i] = u32x4u{};
+#pragma unroll
+        for (int e = 0; e < E - 1; ++e)
+          if (at + e < n) v[i][e / 2] |= (uint32_t)__builtin_bit_cast(unsigned short, g[at + e]) << (16 * (e & 1));
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int i, int e) const { return __uint_as_float(e & 1 ? v[i][e / 2] & 0xffff0000u : v[i][e / 2] << 16); }
+  __device__ __forceinline__ void store(bf16* o, int n, float f) const {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int at = (i * kThreads + threadIdx.x) * E;
+      if (at + E <= n) {
+        u32x4u w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)(get(i, 2 * e) * f), (bf16)(get(i, 2 * e + 1) * f)});
+        *reinterpret_cast<u32x4u*>(o + at) = w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < E - 1; ++e)
+          if (at + e < n) o[at + e] = (bf16)(get(i, e) * f);
+      }
+    }
+  }
+};
 
 // f(tensor, first element, elements) for the chunks of this block.
 template <class F> __device__ __forceinline__ void for_chunks(const Group& a, bool backwards, F&& f) {
@@ -59,47 +131,30 @@ __device__ __forceinline__ double block_sum64(double v) {
 }
 
 __global__ __launch_bounds__(kThreads) void grad_norm_kernel(Group a, double* part, int add) {
-  double s = 0.0, s2 = 0.0;
-  auto square = [](double& acc, float v) {
-    const double x = v;
-    acc = __builtin_fma(x, x, acc);
+  double s[2] = {0.0, 0.0};
+  auto squares = [&](auto&& x) {
+    typedef typename std::remove_reference<decltype(x)>::type P;
+#pragma unroll
+    for (int i = 0; i < P::kVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < P::E; ++e) {
+        const double v = x.get(i, e);
+        s[e & 1] = __builtin_fma(v, v, s[e & 1]);
+      }
   };
   for_chunks(a, false, [&](int k, int64_t from, int n) {
     if (a.bf16_[k]) {
-      const bf16* const g = reinterpret_cast<const bf16*>(a.g[k]) + from;
-      constexpr int kVecs = kChunk / 8 / kThreads;
-      if (n == kChunk) {
-        u32x4u v[kVecs];
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) v[i] = *reinterpret_cast<const u32x4u*>(g + (i * kThreads + threadIdx.x) * 8);
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            square(s, __uint_as_float(v[i][e] << 16));
-            square(s2, __uint_as_float(v[i][e] & 0xffff0000u));
-          }
-      } else {
-        for (int i = threadIdx.x; i < n; i += kThreads) square(s, (float)g[i]);
-      }
+      Piece<bf16> x;
+      x.load(reinterpret_cast<const bf16*>(a.g[k]) + from, n);
+      squares(x);
     } else {
-      const float* const g = reinterpret_cast<const float*>(a.g[k]) + from;
-      constexpr int kVecs = kChunk / 4 / kThreads;
-      if (n == kChunk) {
-        f32x4u v[kVecs];
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) v[i] = *reinterpret_cast<const f32x4u*>(g + (i * kThreads + threadIdx.x) * 4);
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) square(e & 1 ? s2 : s, v[i][e]);
-      } else {
-        for (int i = threadIdx.x; i < n; i += kThreads) square(s, g[i]);
-      }
+      Piece<float> x;
+      x.load(reinterpret_cast<const float*>(a.g[k]) + from, n);
+      squares(x);
     }
   });
-  s = block_sum64(s + s2);
-  if (threadIdx.x == 0) part[blockIdx.x] = add ? part[blockIdx.x] + s : s;
+  const double t = block_sum64(s[0] + s[1]);
+  if (threadIdx.x == 0) part[blockIdx.x] = add ? part[blockIdx.x] + t : t;
 }
 
 __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Group a, const double* part, int parts, float max_norm, float* result) {
@@ -115,39 +170,17 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Group a, const dou
     result[0] = (float)norm;
     result[1] = f;
   }
+  // Backwards: what the first launch read last is the likeliest to be in a cache still.
   for_chunks(a, true, [&](int k, int64_t from, int n) {
     if (!a.out[k] || (f == 1.f && a.out[k] == a.g[k])) return;     // times 1 in place: nothing to do
     if (a.bf16_[k]) {
-      const bf16* const g = reinterpret_cast<const bf16*>(a.g[k]) + from;
-      bf16* const o = reinterpret_cast<bf16*>(a.out[k]) + from;
-      constexpr int kVecs = kChunk / 8 / kThreads;
-      if (n == kChunk) {
-        u32x4u v[kVecs];
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) v[i] = *reinterpret_cast<const u32x4u*>(g + (i * kThreads + threadIdx.x) * 8);
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            v[i][e] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)(__uint_as_float(v[i][e] << 16) * f), (bf16)(__uint_as_float(v[i][e] & 0xffff0000u) * f)});
-          *reinterpret_cast<u32x4u*>(o + (i * kThreads + threadIdx.x) * 8) = v[i];
-        }
-      } else {
-        for (int i = threadIdx.x; i < n; i += kThreads) o[i] = (bf16)((float)g[i] * f);
-      }
+      Piece<bf16> x;
+      x.load(reinterpret_cast<const bf16*>(a.g[k]) + from, n);
+      x.store(reinterpret_cast<bf16*>(a.out[k]) + from, n, f);
     } else {
-      const float* const g = reinterpret_cast<const float*>(a.g[k]) + from;
-      float* const o = reinterpret_cast<float*>(a.out[k]) + from;
-      constexpr int kVecs = kChunk / 4 / kThreads;
-      if (n == kChunk) {
-        f32x4u v[kVecs];
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) v[i] = *reinterpret_cast<const f32x4u*>(g + (i * kThreads + threadIdx.x) * 4);
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) *reinterpret_cast<f32x4u*>(o + (i * kThreads + threadIdx.x) * 4) = v[i] * f;
-      } else {
-        for (int i = threadIdx.x; i < n; i += kThreads) o[i] = g[i] * f;
-      }
+      Piece<float> x;
+      x.load(reinterpret_cast<const float*>(a.g[k]) + from, n);
+      x.store(reinterpret_cast<float*>(a.out[k]) + from, n, f);
     }
   });
 }

@@ -176,23 +176,28 @@ __global__ __launch_bounds__(kBlock<NT>) void rmsnorm_fwd_kernel(RmsFwdParams p)
         const uint32_t o = pack_f32<E5M2>(__float_as_uint(h[0]), __float_as_uint(h[1]), __float_as_uint(h[2]), __float_as_uint(h[3]),
                                           __uint_as_float(byte << 23));
         if (c < ((d + 15) & ~15)) *reinterpret_cast<uint32_t*>(p.q + n * p.ldq + c) = o;
-        if ((t & 31) == 0 && c < d) {
-          p.scale[scale_at(n, c >> 7, p.rows)] = (uint8_t)byte;
-          if (n == p.rows - 1)               // rows that do not exist
-            for (int64_t k = p.rows; k < ((p.rows + 63) & ~63LL); ++k) p.scale[scale_at(k, c >> 7, p.rows)] = 0;
+        const int first = c & ~127;          // column of the block
+        if ((t & 31) == 0 && c < d) p.scale[scale_at(n, first >> 7, p.rows)] = (uint8_t)byte;
+        if (n == p.rows - 1 && first < d) {  // rows that do not exist
+          const int64_t end = (p.rows + 63) & ~63LL;
+          for (int64_t k = p.rows + (t & 31); k < end; k += 32) p.scale[scale_at(k, first >> 7, p.rows)] = 0;
         }
       }
     }
   }
 }
 
-// f(threads to a row, vectors to a thread) for rows of d columns.
-template <class F> void by_width(int64_t d, F&& f) {
+// f(threads to a row, vectors to a thread).  A wave to a row where there are enough rows to fill the chip, else a block, whose threads have less
+// of it to wait for.
+template <class F> void by_size(int64_t rows, int64_t d, F&& f) {
   using std::integral_constant;
+  const bool many = rows >= 1024;
   if (d <= 256) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  else if (d <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  else if (d <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-  else if (d <= 2048) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  else if (d <= 512 && many) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  else if (d <= 1024 && many) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  else if (d <= 2048 && many) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  else if (d <= 1024) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (d <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
   else if (d <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
   else if (d <= 8192) f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
   else f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
@@ -350,7 +355,7 @@ hipError_t launch_rmsnorm_fwd(hipStream_t s, const RmsnormArgs& a, const float* 
   if (a.rows == 0) return hipSuccess;
   const RmsFwdParams p{x, y, a.g, x_out, h, (uint8_t*)q.q, q.scale, rstd, a.rows, a.ldx, a.ldh, q.ldq, (int)a.cols, a.eps};
   auto run = [&](auto t, auto f8) {
-    by_width(a.cols, [&](auto nt, auto vec) {
+    by_size(a.rows, a.cols, [&](auto nt, auto vec) {
       constexpr int NT = decltype(nt)::value, VEC = decltype(vec)::value, kTeams = kBlock<NT> / NT;
       const int64_t blocks = (a.rows + kTeams - 1) / kTeams, most = NT == 1024 ? 512 : NT == 256 ? 2048 : 1024;
       rmsnorm_fwd_kernel<decltype(t), NT, VEC, decltype(f8)::value><<<(unsigned)(blocks < most ? blocks : most), kBlock<NT>, 0, s>>>(p);
