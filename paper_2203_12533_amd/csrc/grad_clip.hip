@@ -6,8 +6,6 @@
 // operations per element where memory allows for ten.  Two launches for up to kGroup tensors, whose addresses travel with the launch: blocks
 // take chunks of tensors in turn and leave a sum each, then every block of the second adds those sums in the same order (4096 or fewer
 // bytes, from the cache) and scales its chunks.  Bound by memory: two reads and a write of 4 (2) bytes.
-#include <type_traits>
-
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -18,104 +16,78 @@ namespace {
 constexpr int kThreads = 256, kGroup = 96, kParts = 1024;
 constexpr int64_t kChunk = 8192;             // elements
 
+struct Entry {
+  const void* g;
+  void* out;
+  int64_t n;
+  uint32_t first;                            // chunk of the launch that it begins with
+  uint32_t is_bf16;
+};
 struct Group {
-  const void* g[kGroup];
-  void* out[kGroup];
-  int64_t n[kGroup];
-  uint32_t first[kGroup + 1];                // chunk of the launch that a tensor begins with
-  uint8_t bf16_[kGroup];
-  int count;
+  Entry t[kGroup];                           // with elements, so that no two begin with the same chunk
+  uint32_t count, chunks;
 };
 static_assert(sizeof(Group) <= 3500, "with the launch");
 
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));     // wherever an element may be
 
-// A chunk's vectors of one thread: v[i] holds elements (i * kThreads + thread) * E .. of n; zeros behind the end.
-template <class T> struct Piece;
-template <> struct Piece<float> {
-  static constexpr int E = 4, kVecs = kChunk / E / kThreads;
-  f32x4u v[kVecs];
-  __device__ __forceinline__ void load(const float* g, int n) {
+// The tensor that chunk c of the launch is of: the last one that begins at or before it.  All lanes of a wave look at once.
+__device__ __forceinline__ int tensor_of(const Group& a, uint32_t c) {
+  int n = 0;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int at = (i * kThreads + threadIdx.x) * E;
-      if (at + E <= n) {
-        v[i] = *reinterpret_cast<const f32x4u*>(g + at);
-      } else {
-        v[i] = f32x4u{};
-#pragma unroll
-        for (int e = 0; e < E - 1; ++e)
-          if (at + e < n) v[i][e] = g[at + e];
-      }
-    }
+  for (int i = 0; i < kGroup; i += 64) {
+    const uint32_t at = i + (threadIdx.x & 63);
+    n += __popcll(__ballot(at < a.count && a.t[at < kGroup ? at : 0].first <= c));
   }
-  __device__ __forceinline__ float get(int i, int e) const { return v[i][e]; }
-  __device__ __forceinline__ void store(float* o, int n, float f) const {
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int at = (i * kThreads + threadIdx.x) * E;
-      if (at + E <= n) {
-        *reinterpret_cast<f32x4u*>(o + at) = v[i] * f;
-      } else {
-#pragma unroll
-        for (int e = 0; e < E - 1; ++e)
-          if (at + e < n) o[at + e] = v[i][e] * f;
-      }
-    }
+  return __builtin_amdgcn_readfirstlane(n - 1);
+}
+
+// A chunk's vectors of one thread, 16 bytes each: v[i] holds elements (i * kThreads + thread) * E .. of n; zeros behind the end.
+constexpr int kVecs = kChunk / 4 / kThreads;
+template <class T> struct Piece {
+  static constexpr int E = 16 / sizeof(T), kUsed = kChunk / E / kThreads;
+  static __device__ __forceinline__ float get(const u32x4& v, int e) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(v[e]);
+    else return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
   }
-};
-template <> struct Piece<bf16> {
-  static constexpr int E = 8, kVecs = kChunk / E / kThreads;
-  u32x4u v[kVecs];
-  __device__ __forceinline__ void load(const bf16* g, int n) {
+  static __device__ __forceinline__ void load(u32x4 (&v)[kVecs], const T* g, int n) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
+    for (int i = 0; i < kUsed; ++i) {
       const int at = (i * kThreads + threadIdx.x) * E;
       if (at + E <= n) {
         v[i] = *reinterpret_cast<const u32x4u*>(g + at);
       } else {
-        v[i] = u32x4u{};
+        v[i] = u32x4{};
 #pragma unroll
         for (int e = 0; e < E - 1; ++e)
-          if (at + e < n) v[i][e / 2] |= (uint32_t)__builtin_bit_cast(unsigned short, g[at + e]) << (16 * (e & 1));
+          if (at + e < n) {
+            if constexpr (sizeof(T) == 4) v[i][e] = __builtin_bit_cast(uint32_t, g[at + e]);
+            else v[i][e / 2] |= (uint32_t)__builtin_bit_cast(unsigned short, g[at + e]) << (16 * (e & 1));
+          }
       }
     }
   }
-  __device__ __forceinline__ float get(int i, int e) const { return __uint_as_float(e & 1 ? v[i][e / 2] & 0xffff0000u : v[i][e / 2] << 16); }
-  __device__ __forceinline__ void store(bf16* o, int n, float f) const {
+  static __device__ __forceinline__ void store(const u32x4 (&v)[kVecs], T* o, int n, float f) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
+    for (int i = 0; i < kUsed; ++i) {
       const int at = (i * kThreads + threadIdx.x) * E;
       if (at + E <= n) {
-        u32x4u w;
+        u32x4 w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)(get(i, 2 * e) * f), (bf16)(get(i, 2 * e + 1) * f)});
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(get(v[i], e) * f);
+          else w[e] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)(get(v[i], 2 * e) * f), (bf16)(get(v[i], 2 * e + 1) * f)});
+        }
         *reinterpret_cast<u32x4u*>(o + at) = w;
       } else {
 #pragma unroll
         for (int e = 0; e < E - 1; ++e)
-          if (at + e < n) o[at + e] = (bf16)(get(i, e) * f);
+          if (at + e < n) o[at + e] = from_f32<T>(get(v[i], e) * f);
       }
     }
   }
 };
-
-// f(tensor, first element, elements) for the chunks of this block.
-template <class F> __device__ __forceinline__ void for_chunks(const Group& a, bool backwards, F&& f) {
-  const uint32_t total = a.first[a.count];
-  for (uint32_t i = blockIdx.x; i < total; i += gridDim.x) {
-    const uint32_t c = backwards ? total - 1 - i : i;
-    int lo = 0, hi = a.count - 1;            // the last tensor that begins at or before c and has chunks
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (a.first[mid] <= c) lo = mid;
-      else hi = mid - 1;
-    }
-    const int64_t from = (int64_t)(c - a.first[lo]) * kChunk, left = a.n[lo] - from;
-    f(lo, from, (int)(left < kChunk ? left : kChunk));
-  }
-}
 
 __device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
@@ -132,27 +104,29 @@ __device__ __forceinline__ double block_sum64(double v) {
 
 __global__ __launch_bounds__(kThreads) void grad_norm_kernel(Group a, double* part, int add) {
   double s[2] = {0.0, 0.0};
-  auto squares = [&](auto&& x) {
-    typedef typename std::remove_reference<decltype(x)>::type P;
+  u32x4 v[kVecs];
+  auto squares = [&](auto type) {
+    typedef Piece<decltype(type)> P;
 #pragma unroll
-    for (int i = 0; i < P::kVecs; ++i)
+    for (int i = 0; i < P::kUsed; ++i)
 #pragma unroll
       for (int e = 0; e < P::E; ++e) {
-        const double v = x.get(i, e);
-        s[e & 1] = __builtin_fma(v, v, s[e & 1]);
+        const double x = P::get(v[i], e);
+        s[e & 1] = __builtin_fma(x, x, s[e & 1]);
       }
   };
-  for_chunks(a, false, [&](int k, int64_t from, int n) {
-    if (a.bf16_[k]) {
-      Piece<bf16> x;
-      x.load(reinterpret_cast<const bf16*>(a.g[k]) + from, n);
-      squares(x);
+  for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+    const Entry& k = a.t[tensor_of(a, c)];
+    const int64_t from = (int64_t)(c - k.first) * kChunk, left = k.n - from;
+    const int n = (int)(left < kChunk ? left : kChunk);
+    if (k.is_bf16) {
+      Piece<bf16>::load(v, reinterpret_cast<const bf16*>(k.g) + from, n);
+      squares(bf16{});
     } else {
-      Piece<float> x;
-      x.load(reinterpret_cast<const float*>(a.g[k]) + from, n);
-      squares(x);
+      Piece<float>::load(v, reinterpret_cast<const float*>(k.g) + from, n);
+      squares(float{});
     }
-  });
+  }
   const double t = block_sum64(s[0] + s[1]);
   if (threadIdx.x == 0) part[blockIdx.x] = add ? part[blockIdx.x] + t : t;
 }
@@ -164,25 +138,33 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Group a, const dou
     const int at = i * kThreads + threadIdx.x;
     if (at < parts) s += part[at];
   }
-  const double norm = sqrt(block_sum64(s));
-  const float f = norm > (double)max_norm ? (float)((double)max_norm / norm) : norm == norm ? 1.f : __builtin_nanf("");
-  if (result && blockIdx.x == 0 && threadIdx.x == 0) {
-    result[0] = (float)norm;
-    result[1] = f;
-  }
-  // Backwards: what the first launch read last is the likeliest to be in a cache still.
-  for_chunks(a, true, [&](int k, int64_t from, int n) {
-    if (!a.out[k] || (f == 1.f && a.out[k] == a.g[k])) return;     // times 1 in place: nothing to do
-    if (a.bf16_[k]) {
-      Piece<bf16> x;
-      x.load(reinterpret_cast<const bf16*>(a.g[k]) + from, n);
-      x.store(reinterpret_cast<bf16*>(a.out[k]) + from, n, f);
-    } else {
-      Piece<float> x;
-      x.load(reinterpret_cast<const float*>(a.g[k]) + from, n);
-      x.store(reinterpret_cast<float*>(a.out[k]) + from, n, f);
+  u32x4 v[kVecs];
+  float f = 0.f;
+  auto factor = [&] {                        // while the first chunk travels
+    const double norm = sqrt(block_sum64(s));
+    f = norm > (double)max_norm ? (float)((double)max_norm / norm) : norm == norm ? 1.f : __builtin_nanf("");
+    if (result && blockIdx.x == 0 && threadIdx.x == 0) {
+      result[0] = (float)norm;
+      result[1] = f;
     }
-  });
+  };
+  // Backwards: what the first launch read last is the likeliest to be in a cache still.
+  uint32_t i = blockIdx.x;
+  if (i >= a.chunks) factor();
+  for (; i < a.chunks; i += gridDim.x) {
+    const uint32_t c = a.chunks - 1 - i;
+    const Entry& k = a.t[tensor_of(a, c)];
+    const int64_t from = (int64_t)(c - k.first) * kChunk, left = k.n - from;
+    const int n = (int)(left < kChunk ? left : kChunk);
+    const bool first = i == blockIdx.x;
+    if (!first && f == 1.f && k.out == k.g) continue;              // times 1 in place: nothing to do
+    if (k.is_bf16) Piece<bf16>::load(v, reinterpret_cast<const bf16*>(k.g) + from, n);
+    else Piece<float>::load(v, reinterpret_cast<const float*>(k.g) + from, n);
+    if (first) factor();
+    if (f == 1.f && k.out == k.g) continue;
+    if (k.is_bf16) Piece<bf16>::store(v, reinterpret_cast<bf16*>(k.out) + from, n, f);
+    else Piece<float>::store(v, reinterpret_cast<float*>(k.out) + from, n, f);
+  }
 }
 
 }  // namespace
@@ -207,21 +189,14 @@ hipError_t launch_grad_clip(hipStream_t s, const GradTensor* t, int count, float
     bool done = false;
     for (int i = 0; i < count || !done;) {
       Group a;
-      a.count = 0;
-      a.first[0] = 0;
-      bool out = false;
+      a.count = a.chunks = 0;
       for (; i < count && a.count < kGroup; ++i) {
         if (t[i].n == 0 || (pass == 1 && !t[i].out)) continue;
-        const int k = a.count++;
-        a.g[k] = t[i].g;
-        a.out[k] = t[i].out;
-        a.n[k] = t[i].n;
-        a.bf16_[k] = t[i].dtype == kBF16;
-        a.first[k + 1] = a.first[k] + (uint32_t)((t[i].n + kChunk - 1) / kChunk);
-        out = true;
+        a.t[a.count++] = Entry{t[i].g, t[i].out, t[i].n, a.chunks, t[i].dtype == kBF16};
+        a.chunks += (uint32_t)((t[i].n + kChunk - 1) / kChunk);
       }
-      if (!out && done) continue;
-      const uint32_t chunks = a.first[a.count];
+      if (a.count == 0 && done) continue;
+      const uint32_t chunks = a.chunks;
       if (pass == 0) {
         const int blocks = done && chunks < (uint32_t)parts ? (int)chunks : parts;
         grad_norm_kernel<<<blocks, kThreads, 0, s>>>(a, part, done);

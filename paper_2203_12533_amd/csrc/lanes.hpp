@@ -18,10 +18,10 @@ template <class F> __device__ __forceinline__ uint32_t rows32(uint32_t v, F&& f)
   const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   return f(p[0], p[1]);
 }
-// Over 16, 32 or 64 lanes; f is associative and commutative.
+// Over N = 1, 2, 4 .. 64 neighbouring lanes; f is associative and commutative.
 template <int N, class F> __device__ __forceinline__ uint32_t all(uint32_t v, F&& f) {
-  v = f(v, move<kQuad1>(v));
-  v = f(v, move<kQuad2>(v));
+  if constexpr (N >= 2) v = f(v, move<kQuad1>(v));
+  if constexpr (N >= 4) v = f(v, move<kQuad2>(v));
   if constexpr (N >= 8) v = f(v, move<kHalfMirror>(v));
   if constexpr (N >= 16) v = f(v, move<kMirror>(v));
   if constexpr (N >= 32) v = rows16(v, f);

@@ -7,11 +7,11 @@
 // alike, by an amount that is known and taken off log S.  Every thread keeps a running maximum, S and sum of its own; they meet once per row.  Sums are fp32, of at most
 // vocab / threads terms before they meet in a tree.
 //
-// Alternatives.  A chunk of the row is in registers; the block's threads form 64 groups, and the k-th largest of the groups' maxima (the upper 16
-// bits of it) is a bound that k elements at least reach: usually few more do.  They go to a list in LDS with a key of value and index, 64 bits,
-// no two alike, so that the order in which they arrive does not matter; later chunks add what reaches the bound.  A list that is full
-// gets a tighter bound, and where that does not help - values that fall into few groups - the chunk's k best are taken out one by
-// one.  Ranks in the list are counted at the end.
+// Alternatives.  Every wave keeps a list in LDS of what can be among the k best of its columns, without a word to the others: with a part of the row in
+// registers, the k-th largest of its 64 lanes' maxima (the upper 16 bits of it) is a bound that k elements at least reach, and
+// usually few more do.  Those go to the list as keys of value and index, 64 bits, no two alike, placed by a ballot; what comes later in the row adds
+// what reaches the bound.  A list that is full gets a tighter bound, and where that does not help - values that fall into few
+// lanes - the k best are taken out one by one.  At the end a wave ranks its list by counting, and the block the waves' k best.
 //
 // Bound by memory: forward one read, backward one read and one write.
 #include <type_traits>
@@ -51,10 +51,10 @@ template <> struct Vec<bf16> {
   static __device__ __forceinline__ void store(bf16* p, const u32x4& v) { *reinterpret_cast<u32x4u2*>(p) = v; }
   static __device__ __forceinline__ float get(const u32x4& v, int e) { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
 };
-// Columns c .. of a row of n; -infinity behind its end.
-template <class T> __device__ __forceinline__ u32x4 load_vec(const T* row, int64_t c, int64_t n) {
+// Columns c .. of a row of n (2^28 at most: offsets of bytes are 32 bits beside a uniform address); -infinity behind its end.
+template <class T> __device__ __forceinline__ u32x4 load_vec(const T* row, uint32_t c, uint32_t n) {
   constexpr int E = Vec<T>::E;
-  if (c + E <= n) return Vec<T>::load(row + c);
+  if (c + E <= n) return Vec<T>::load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + c * (uint32_t)sizeof(T)));
   u32x4 v = {Vec<T>::kFill, Vec<T>::kFill, Vec<T>::kFill, Vec<T>::kFill};
 #pragma unroll
   for (int e = 0; e < E - 1; ++e)
@@ -86,7 +86,27 @@ __device__ __forceinline__ float value_of(uint64_t key) {
 }
 __device__ __forceinline__ uint32_t index_of(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
 
-constexpr int kMaxTop = 32, kCap = 1024;
+// f(key, how many of the n in the list are larger) for the keys i, i + step, ...  M: at most so many of them are a thread's. 
+template <int M, class F> __device__ __forceinline__ void ranks(const uint64_t* list, int n, int i, int step, F&& f) {
+  uint64_t key[M];
+  int rank[M];
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    key[m] = i + m * step < n ? list[i + m * step] : ~0ull;
+    rank[m] = 0;
+  }
+#pragma unroll 8
+  for (int j = 0; j < n; ++j) {
+    const uint64_t other = list[j];
+#pragma unroll
+    for (int m = 0; m < M; ++m) rank[m] += other > key[m];
+  }
+#pragma unroll
+  for (int m = 0; m < M; ++m)
+    if (i + m * step < n) f(key[m], rank[m]);
+}
+
+constexpr int kMaxTop = 32;
 struct LogprobFwdParams {
   const void* z;
   int64_t ldz, rows, vocab;
@@ -96,6 +116,9 @@ struct LogprobFwdParams {
   int top;
   int32_t* top_id;
   float* top_logp;
+  int segments;                // that a row is cut into, one to a block; > 1: what they find goes to `parts`, [row][segment] of 4 + 2 top floats
+  int64_t segment;             // elements
+  float* parts;
 };
 
 // Three numbers of a set of logits: maximum, S and sum of e^d d (base 2) against it.
@@ -108,40 +131,110 @@ __device__ __forceinline__ Soft rebase(const Soft& a, float m, float bound, floa
   return {m, a.s * f, f * __builtin_fmaf(d, a.s, a.t)};
 }
 
-template <class T, int NT, int U>
-__global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) {
-  constexpr int E = Vec<T>::E, kWaves = NT / 64;
-  constexpr int64_t kChunk = (int64_t)NT * U * E;
-  __shared__ float group_max[64];
-  __shared__ Soft wave_soft[2][kWaves];
-  __shared__ uint64_t list[kCap + kMaxTop], wave_key[2][kWaves];
-  __shared__ int count;
+// The logit of a row's given token, for one thread: asked for before anything else, as one load waits for the other.
+struct Given { bool is; float z; };
+template <class T> __device__ __forceinline__ Given given_of(const LogprobFwdParams& p, int64_t row) {
+  if (!p.targets || !p.logp) return {false, 0.f};
+  const int target = p.targets[row];
+  if (target < 0 || target >= p.vocab) return {false, 0.f};
+  return {true, to_f32((reinterpret_cast<const T*>(p.z) + row * p.ldz)[target])};
+}
+
+// What becomes of a row when its parts are together: `all` of the fast sums, the list of n keys that hold the best (LDS, behind a barrier).
+// The whole block calls; `given` is its first thread's.
+template <class T, int NT>
+__device__ __forceinline__ void finish_row(const LogprobFwdParams& p, int64_t row, Soft all, const uint64_t* list, int n, Soft* wave_soft,
+                                           const Given& given) {
+  constexpr int kWaves = NT / 64;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, top = p.top;
-  const int64_t row = blockIdx.x, V = p.vocab;
   const T* const z = reinterpret_cast<const T*>(p.z) + row * p.ldz;
   const float k = p.k, bound = safe_bound(k);
-  const int target = p.targets ? p.targets[row] : -1;
-  const bool given = target >= 0 && target < V;
-  float zt = 0.f;
-  if (given && t == 0 && p.logp) zt = to_f32(z[target]);
-  if (t == 0) count = 0;
+  const bool extreme = !(fabsf(all.m) <= bound);
+  if (extreme && fabsf(all.m) < INFINITY) {              // once more, with z - max first
+    float s = 0.f, st = 0.f;
+    for (int64_t c = t; c < p.vocab; c += NT) {
+      const float d = larger((to_f32(z[c]) - all.m) * k, kFloor), x = __builtin_amdgcn_exp2f(d);
+      s += x;
+      st = __builtin_fmaf(x, d, st);
+    }
+    s = lanes_sum(s);
+    st = lanes_sum(st);
+    if (lane == 0) wave_soft[wave] = Soft{0.f, s, st};
+    __syncthreads();
+    all.s = all.t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      all.s += wave_soft[w].s;
+      all.t += wave_soft[w].t;
+    }
+  }
+  const bool none = all.m == -INFINITY && all.s == 0.f;  // (a NaN beside makes S one)
+  const float nan = __builtin_nanf("");
+  if (all.m == INFINITY || (all.m == -INFINITY && !none)) all.s = nan;
+  const float log2s = __builtin_amdgcn_logf(all.s), lse = (log2s - (extreme ? 0.f : shift_error(all.m, bound, k))) * kLn2;
+  auto log_p = [&](float x) { return none ? -INFINITY : (x - all.m) * p.scale - lse; };    // only what is out of range itself overflows
+  if (t == 0) {
+    if (p.logp) p.logp[row] = given.is ? log_p(given.z) : 0.f;
+    if (p.entropy) p.entropy[row] = none ? 0.f : (log2s - all.t / all.s) * kLn2;
+    if (p.stats) *reinterpret_cast<float2*>(p.stats + 2 * row) = make_float2(all.m, none ? 0.f : lse);
+  }
+  if (top > 0) {
+    const bool bad = !(all.s == all.s);
+    if (bad) n = 0;
+    auto put = [&](uint64_t key, int rank) {
+      if (rank < top) {
+        p.top_id[row * top + rank] = (int32_t)index_of(key);
+        p.top_logp[row * top + rank] = log_p(value_of(key));
+      }
+    };
+    for (int i = t; i < n; i += NT) ranks<1>(list, n, i, NT, put);
+    for (int i = n + t; i < top; i += NT) {
+      p.top_id[row * top + i] = -1;
+      p.top_logp[row * top + i] = bad ? nan : -INFINITY;
+    }
+  }
+}
+
+// LDS of one wave: what its lanes wrote is there for the others.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// NT threads of a block, U vectors of 16 bytes to one in a chunk; a wave's list has kPlaces places, and kMaxTop more for a k best of a chunk.
+constexpr int kPlaces = 256;
+template <class T, int NT, int U, bool TOP>
+__global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) {
+  constexpr int E = Vec<T>::E, kWaves = NT / 64;
+  constexpr uint32_t kChunk = NT * U * E;
+  __shared__ Soft wave_soft[2][kWaves];
+  __shared__ uint64_t lists[TOP ? kWaves : 1][TOP ? kPlaces + kMaxTop : 1], best_keys[TOP ? kWaves * kMaxTop : 1];
+  __shared__ int counts[kWaves];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), top = TOP ? p.top : 0;
+  const int64_t row = p.segments > 1 ? blockIdx.x / p.segments : blockIdx.x;
+  const int seg = p.segments > 1 ? (int)(blockIdx.x - row * p.segments) : 0;
+  const uint32_t from = seg * (uint32_t)p.segment, V = (uint32_t)(from + p.segment < p.vocab ? from + p.segment : p.vocab);   // of this block: from .. V - 1
+  const T* const z = reinterpret_cast<const T*>(p.z) + row * p.ldz;
+  const float k = p.k, bound = safe_bound(k);
+  uint64_t* const list = lists[TOP ? wave : 0];
+  Given given = {};
+  if (t == 0 && p.segments == 1) given = given_of<T>(p, row);
+  int n = 0;                                             // keys in it
 
   u32x4 v[U], nx[U];
-  auto fetch = [&](int64_t c0) {
+  auto fetch = [&](uint32_t c0) {
+    const uint32_t c = c0 + (uint32_t)t * E;
 #pragma unroll
-    for (int u = 0; u < U; ++u) nx[u] = load_vec(z, c0 + ((int64_t)u * NT + t) * E, V);
+    for (int u = 0; u < U; ++u) nx[u] = load_vec(z, c + u * NT * E, V);
   };
   Soft mine = {-INFINITY, 0.f, 0.f};
   float thr = -__FLT_MAX__;                              // finite: -infinity is no alternative
   float vec_max[U], chunk_max;
 
-  // A bound that the k best of the chunk reach: upper bits of the k-th largest of 64 groups' maxima.  All waves find the same.  Two of the
-  // block's barriers lie between two writes of group_max.
-  auto bound_of_chunk = [&] {
-    const float g = lanes_max<NT / 64>(chunk_max);
-    if (t % (NT / 64) == 0) group_max[t / (NT / 64)] = g;
-    __syncthreads();
-    const uint32_t mine16 = (uint32_t)(key_of(group_max[lane], 0) >> 48);
+  // A bound that the k best of the wave reach: upper bits of the k-th largest of its lanes' maxima, of the chunk or of all so far.
+  auto bound_of = [&](float lane_max) {
+    const uint32_t mine16 = (uint32_t)(key_of(lane_max, 0) >> 48);
     uint32_t best = 0;
 #pragma unroll
     for (int b = 15; b >= 0; --b) {
@@ -150,58 +243,48 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
     }
     return value_of((uint64_t)best << 48);               // NaN's bits are never reached: maxima leave NaN out
   };
-  auto push = [&](int64_t c0) {
+  auto push = [&](uint32_t c0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (!__any(vec_max[u] >= thr)) continue;
-      if (vec_max[u] >= thr) {
+      uint32_t col = c0 + (uint32_t)(u * NT + t) * E;
+      asm volatile("" : "+v"(col));                      // not kept for every u across the loop
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float x = Vec<T>::get(v[u], e);
-          if (x >= thr) {
-            const int at = atomicAdd(&count, 1);
-            if (at < kCap) list[at] = key_of(x, (uint32_t)(c0 + ((int64_t)u * NT + t) * E + e));
-          }
-        }
+      for (int e = 0; e < E; ++e) {
+        const float x = Vec<T>::get(v[u], e);
+        const uint64_t who = __ballot(x >= thr);
+        if (who == 0) continue;
+        const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+        if (x >= thr && at < kPlaces) list[at] = key_of(x, col + e);
+        n += __popcll(who);
       }
     }
   };
-  // Ranks of what is in the list, of which n at most kCap + kMaxTop; f(rank, key).
-  auto ranked = [&](int n, auto&& f) {
-    for (int i = t; i < n; i += NT) {
-      const uint64_t key = list[i];
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += list[j] > key;
-      f(rank, key);
-    }
+  // The k best of the list alone stay in it, in order.
+  auto compact = [&] {
+    wave_sync();
+    auto put = [&](uint64_t key, int rank) {
+      if (rank < top) best_keys[wave * kMaxTop + rank] = key;
+    };
+#pragma unroll 1
+    for (int i = 0; i < n; i += 128) ranks<2>(list, n, i + lane, 64, put);
+    wave_sync();
+    n = n < top ? n : top;
+    if (lane < n) list[lane] = best_keys[wave * kMaxTop + lane];
+    wave_sync();
   };
-  // The k best of the list alone stay in it.  Called by all, behind a barrier; ends with one.
-  auto compact = [&](int n) {
-    constexpr int kPer = (kCap + kMaxTop + NT - 1) / NT;
-    int to[kPer], m = 0;
-    uint64_t keys[kPer];
-    ranked(n, [&](int rank, uint64_t key) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (i == m) to[i] = rank, keys[i] = key;
-      ++m;
-    });
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (i < m && to[i] < top) list[to[i]] = keys[i];
-    if (t == 0) count = n < top ? n : top;
-    __syncthreads();
-  };
-  // The k best of the chunk to the end of a list of n, one by one, from memory: rows that come here are odd ones.
-  auto extract = [&](int n, int64_t c0) {
+  // The k best of the wave's part of the chunk to the end of the list, one by one, from memory: rows that come here are odd ones.
+  auto extract = [&](uint32_t c0) {
     uint64_t last = ~0ull;
-    int found = 0;
-    for (; found < top; ++found) {
+#pragma unroll 1
+    for (int found = 0; found < top; ++found) {
       uint64_t best = 0;
-      for (int64_t c = c0 + t; c < V && c < c0 + kChunk; c += NT) {
+#pragma unroll 1
+      for (int i = 0; i < U * E; ++i) {
+        const uint32_t c = c0 + (uint32_t)((i / E) * NT + t) * E + i % E;
+        if (c >= V) continue;
         const float x = to_f32(z[c]);
-        const uint64_t key = x >= -__FLT_MAX__ ? key_of(x, (uint32_t)c) : 0;
+        const uint64_t key = x >= -__FLT_MAX__ ? key_of(x, c) : 0;
         if (key < last && key > best) best = key;
       }
 #pragma unroll
@@ -209,21 +292,16 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
         const uint64_t other = __shfl_xor((unsigned long long)best, o, 64);
         best = other > best ? other : best;
       }
-      if (lane == 0) wave_key[found & 1][wave] = best;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) best = wave_key[found & 1][w] > best ? wave_key[found & 1][w] : best;
       if (best == 0) break;
       last = best;
-      if (t == 0) list[n + found] = best;
+      if (lane == 0) list[n] = best;
+      ++n;
     }
-    if (t == 0) count = n + found;
-    __syncthreads();
-    return n + found;
   };
 
-  fetch(0);
-  for (int64_t c0 = 0; c0 < V; c0 += kChunk) {
+  fetch(from);
+#pragma unroll 1
+  for (uint32_t c0 = from; c0 < V; c0 += kChunk) {
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = nx[u];
     if (c0 + kChunk < V) fetch(c0 + kChunk);             // travels while this one is reduced
@@ -247,34 +325,27 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
         mine.t = __builtin_fmaf(x, d, mine.t);
         if (e == E - 1) __builtin_amdgcn_sched_barrier(0);
       }
-    if (top > 0) {
-      if (c0 == 0) thr = fmaxf(thr, bound_of_chunk());   // (its barrier is behind the one write of count, too)
-      const int before = c0 == 0 ? 0 : count;            // nobody writes it between the last barrier and the next
-      if (c0 > 0) __syncthreads();
+    if constexpr (TOP) {                                 // uniform over the wave
+      thr = fmaxf(thr, bound_of(mine.m));
+      const int before = n;
       push(c0);
-      __syncthreads();
-      int n = count;
-      if (n > kCap) {                                    // uniform, as everything below
-        thr = fmaxf(thr, bound_of_chunk());              // (a barrier: everybody has read count)
-        if (t == 0) count = before;
-        __syncthreads();
+      if (n > kPlaces) {
+        n = before;
+        thr = fmaxf(thr, bound_of(chunk_max));
         push(c0);
-        __syncthreads();
-        n = count;
-        if (n > kCap) {
-          __syncthreads();
-          n = extract(before, c0);
+        if (n > kPlaces) {
+          n = before;
+          extract(c0);
         }
       }
-      if (n > kCap / 2) {
-        __syncthreads();
-        compact(n);
-        if (count == top) thr = fmaxf(thr, value_of(list[top - 1]));
+      if (n > kPlaces / 2) {
+        compact();
+        if (n == top) thr = fmaxf(thr, value_of(list[top - 1]));
       }
     }
   }
 
-  // All of the row: within a wave, then between waves.
+  // All of the segment: within a wave, then between waves.
   {
     const float m = lanes_max(mine.m);
     Soft a = rebase(mine, m, bound, k);
@@ -282,7 +353,22 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
     a.t = lanes_sum(a.t);
     if (lane == 0) wave_soft[0][wave] = a;
   }
+  if constexpr (TOP) {
+    compact();
+    if (lane == 0) counts[wave] = n;
+  }
   __syncthreads();
+  int keys = 0;                                          // of all waves
+  if constexpr (TOP) {
+    int first = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) first += counts[w];
+      keys += counts[w];
+    }
+    if (lane < n) best_keys[first + lane] = list[lane];
+    __syncthreads();
+  }
   Soft all = {-INFINITY, 0.f, 0.f};
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) all.m = fmaxf(all.m, wave_soft[0][w].m);
@@ -292,49 +378,70 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
     all.s += a.s;
     all.t += a.t;
   }
-  const bool extreme = !(fabsf(all.m) <= bound);
-  if (extreme && fabsf(all.m) < INFINITY) {              // once more, with z - max first
-    float s = 0.f, st = 0.f;
-    for (int64_t c = t; c < V; c += NT) {
-      const float d = larger((to_f32(z[c]) - all.m) * k, kFloor), x = __builtin_amdgcn_exp2f(d);
-      s += x;
-      st = __builtin_fmaf(x, d, st);
-    }
-    s = lanes_sum(s);
-    st = lanes_sum(st);
-    if (lane == 0) wave_soft[1][wave] = Soft{0.f, s, st};
-    __syncthreads();
-    all.s = all.t = 0.f;
+  if (p.segments == 1) {
+    finish_row<T, NT>(p, row, all, best_keys, keys, wave_soft[1], given);
+    return;
+  }
+  float* const out = p.parts + (int64_t)blockIdx.x * (4 + 2 * p.top);
+  if (t == 0) *reinterpret_cast<float2*>(out) = make_float2(all.m, all.s), out[2] = all.t;
+  if constexpr (TOP) {
+    uint64_t* const to = reinterpret_cast<uint64_t*>(out + 4);
+    for (int i = t; i < keys; i += NT)
+      ranks<1>(best_keys, keys, i, NT, [&](uint64_t key, int rank) {
+        if (rank < top) to[rank] = key;
+      });
+    for (int i = keys + t; i < top; i += NT) to[i] = 0;    // no key
+  }
+}
+
+// The segments of a row together, at most kSegments of at most kMaxTop keys each, by one wave: of the keys those are ranked that reach the k-th largest of
+// the lanes' maxima.
+constexpr int kSegments = 32, kJoin = 64;
+template <class T>
+__global__ __launch_bounds__(kJoin) void logprob_join_kernel(LogprobFwdParams p) {
+  constexpr int kPer = kSegments * kMaxTop / kJoin;
+  __shared__ uint64_t list[kSegments * kMaxTop];
+  __shared__ Soft wave_soft[1];
+  const int lane = threadIdx.x, top = p.top;
+  const int64_t row = blockIdx.x;
+  const float* const in = p.parts + row * p.segments * (4 + 2 * top);
+  const float k = p.k, bound = safe_bound(k);
+  Given given = {};
+  if (lane == 0) given = given_of<T>(p, row);
+  Soft all = {-INFINITY, 0.f, 0.f};
+  if (lane < p.segments) {
+    const float* const q = in + lane * (4 + 2 * top);
+    all = Soft{q[0], q[1], q[2]};
+  }
+  uint64_t key[kPer], best = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      all.s += wave_soft[1][w].s;
-      all.t += wave_soft[1][w].t;
-    }
+  for (int m = 0; m < kPer; ++m) {
+    const int i = m * kJoin + lane, s = top > 0 ? i / top : 0;
+    key[m] = i < p.segments * top ? *reinterpret_cast<const uint64_t*>(in + s * (4 + 2 * top) + 4 + 2 * (i - s * top)) : 0;
+    best = key[m] > best ? key[m] : best;
   }
-  const bool none = all.m == -INFINITY && all.s == 0.f;  // (a NaN beside makes S one)
-  const float nan = __builtin_nanf("");
-  if (all.m == INFINITY || (all.m == -INFINITY && !none)) all.s = nan;
-  const float log2s = __builtin_amdgcn_logf(all.s), lse = (log2s - (extreme ? 0.f : shift_error(all.m, bound, k))) * kLn2;
-  auto log_p = [&](float x) { return none ? -INFINITY : (x - all.m) * p.scale - lse; };    // only what is out of range itself overflows
-  if (t == 0) {
-    if (p.logp) p.logp[row] = given ? log_p(zt) : 0.f;
-    if (p.entropy) p.entropy[row] = none ? 0.f : (log2s - all.t / all.s) * kLn2;
-    if (p.stats) *reinterpret_cast<float2*>(p.stats + 2 * row) = make_float2(all.m, none ? 0.f : lse);
-  }
+  all = rebase(all, lanes_max(all.m), bound, k);
+  all.s = lanes_sum(all.s);
+  all.t = lanes_sum(all.t);
+  int n = 0;
   if (top > 0) {
-    const bool bad = !(all.s == all.s);
-    const int n = bad ? 0 : count;                       // (barriers lie behind the last write)
-    ranked(n, [&](int rank, uint64_t key) {
-      if (rank < top) {
-        p.top_id[row * top + rank] = (int32_t)index_of(key);
-        p.top_logp[row * top + rank] = log_p(value_of(key));
-      }
-    });
-    for (int i = n + t; i < top; i += NT) {
-      p.top_id[row * top + i] = -1;
-      p.top_logp[row * top + i] = bad ? nan : -INFINITY;
+    const uint32_t mine16 = (uint32_t)(best >> 48);
+    uint32_t least = 0;
+#pragma unroll
+    for (int b = 15; b >= 0; --b) {
+      const uint32_t tryit = least | 1u << b;
+      if (__popcll(__ballot(mine16 >= tryit)) >= top) least = tryit;
     }
+#pragma unroll
+    for (int m = 0; m < kPer; ++m) {
+      const bool take = key[m] != 0 && (uint32_t)(key[m] >> 48) >= least;
+      const uint64_t who = __ballot(take);
+      if (take) list[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = key[m];
+      n += __popcll(who);
+    }
+    __syncthreads();
   }
+  finish_row<T, kJoin>(p, row, all, list, n, wave_soft, given);
 }
 
 // ---- backward ----------------------------------------------------------------------------------------------------
@@ -413,9 +520,17 @@ hipError_t check(const LogprobArgs& a) {
 
 }  // namespace
 
+// How many segments rows are cut into: where there are too few rows for the chip, as many as keep 4096 elements each.
+static int segments_of(int64_t rows, int64_t vocab) {
+  if (rows >= 512 || vocab < 8192) return 1;
+  int64_t n = 1024 / (rows < 1 ? 1 : rows);
+  if (n > vocab / 4096) n = vocab / 4096;
+  return (int)(n < kSegments ? n : kSegments);
+}
 int64_t logprob_ws_floats(int64_t rows, int64_t vocab, int k) {
   if (rows < 0 || rows > (1LL << 31) - 1 || vocab < 1 || vocab > (1LL << 28) || k < 0 || k > kMaxTop) return -1;
-  return 0;
+  const int n = segments_of(rows, vocab);
+  return n > 1 ? rows * n * (4 + 2 * k) : 0;
 }
 
 hipError_t launch_logprob_fwd(hipStream_t s, const LogprobArgs& a, float* logp, float* entropy, float* stats, int k, int32_t* top_id, float* top_logp,
@@ -424,16 +539,25 @@ hipError_t launch_logprob_fwd(hipStream_t s, const LogprobArgs& a, float* logp, 
       (logp && !a.targets) || (!logp && !entropy && !stats && k == 0))
     return hipErrorInvalidValue;
   if (((uintptr_t)logp | (uintptr_t)entropy | (uintptr_t)top_id | (uintptr_t)top_logp) & 3 || (uintptr_t)stats & 7) return hipErrorInvalidValue;
-  (void)ws;
+  if (logprob_ws_floats(a.rows, a.vocab, k) > 0 && (!ws || ((uintptr_t)ws & 7))) return hipErrorInvalidValue;
   if (a.rows == 0) return hipSuccess;
-  const LogprobFwdParams p{a.z, a.ldz, a.rows, a.vocab, a.targets, a.scale, a.scale * kLog2e, logp, entropy, stats, k, top_id, top_logp};
-  auto run = [&](auto t) {
+  const int n = segments_of(a.rows, a.vocab);
+  const LogprobFwdParams p{a.z, a.ldz, a.rows, a.vocab, a.targets, a.scale, a.scale * kLog2e, logp, entropy, stats, k, top_id, top_logp, n,
+                           (a.vocab + n - 1) / n, ws};
+  auto run = [&](auto t, auto with_top) {
     using T = decltype(t);
-    if (a.rows <= 256 && a.vocab > 8192) logprob_fwd_kernel<T, 1024, 4><<<(unsigned)a.rows, 1024, 0, s>>>(p);
-    else logprob_fwd_kernel<T, 256, 8><<<(unsigned)a.rows, 256, 0, s>>>(p);
+    constexpr bool TOP = decltype(with_top)::value;
+    const unsigned blocks = (unsigned)(a.rows * n);
+    if (a.vocab <= 2048) logprob_fwd_kernel<T, 64, 4, TOP><<<blocks, 64, 0, s>>>(p);
+    else logprob_fwd_kernel<T, 256, 4, TOP><<<blocks, 256, 0, s>>>(p);
+    if (n > 1) logprob_join_kernel<T><<<(unsigned)a.rows, kJoin, 0, s>>>(p);
   };
-  if (a.dtype == kF32) run(float{});
-  else run(bf16{});
+  auto type = [&](auto t) {
+    if (k > 0) run(t, std::true_type{});
+    else run(t, std::false_type{});
+  };
+  if (a.dtype == kF32) type(float{});
+  else type(bf16{});
   return hipGetLastError();
 }
 

@@ -199,7 +199,8 @@ template <class F> void by_size(int64_t rows, int64_t d, F&& f) {
   else if (d <= 1024) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
   else if (d <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
   else if (d <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-  else if (d <= 8192) f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+  else if (d <= 8192 && many) f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+  else if (d <= 8192) f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
   else f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
 }
 constexpr int64_t kMaxCols = 16384, kMaxRows = (1LL << 31) - 1;
@@ -331,7 +332,7 @@ int bwd_rows(int64_t d) {
 }
 int64_t bwd_teams(int64_t rows, int64_t d) {
   const int per = bwd_rows(d);
-  const int64_t teams = (rows + per - 1) / per, most = d <= 512 ? 4 * kBwdTeams : kBwdTeams;
+  const int64_t teams = (rows + per - 1) / per, most = d <= 512 ? 4 * kBwdTeams : d <= 1024 ? 2 * kBwdTeams : kBwdTeams;
   return teams < most ? teams : most;
 }
 
