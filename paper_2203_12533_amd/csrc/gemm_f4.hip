@@ -290,7 +290,7 @@ __global__ __launch_bounds__(S::kThreads, S::G / 4) void gemm_f4_stream_kernel(G
   const int tiles = p.tiles_m * p.tiles_n, n = (int)((p.K + kF4BK - 1) / kF4BK);
   const uint32_t ring = (uint32_t)(uintptr_t)(lds_ptr)smem, biases = ring + 2 * S::kStage;
   const float* const bias = epi_has_bias(p.epi.mode) ? p.epi.bias : nullptr;
-  p.epi.bias = nullptr;                                     // added before the epilogue
+  p.epi.bias = nullptr;                                     // in the sums already
 
   // Where loads are: k tile `kt` of output tile `to`, the `count`-th of this workgroup (at least two k tiles to one).  Scales of a k tile as in the kernel below.
   const int64_t Ra = ((p.M + 63) & ~63LL) * 4, Rb = ((p.N + 63) & ~63LL) * 4;
@@ -454,10 +454,15 @@ __global__ __launch_bounds__(S::kThreads, S::G / 4) void gemm_f4_stream_kernel(G
   uint32_t st = 0;
   int done = 0;
   for (int o = blockIdx.x; o < tiles; o += gridDim.x, ++done) {
+    // Sums begin with the bias, which is in LDS before the first operands are: 128 additions less.
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int j = 0; j < FN; ++j) {
+      typedef __attribute__((address_space(3))) const f32x4* at;
+      f32x4 b = {0.f, 0.f, 0.f, 0.f};
+      if (bias) b = *(at)(uintptr_t)(biases + (done % S::kBiases) * (S::BN * 4) + (wn * FN * 16 + 16 * j + 4 * (fresh(lane) >> 4)) * 4);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < FM; ++i) acc[i][j] = b;
+    }
     for (int t = 0; t < n; ++t) {
       if (t + 2 == n) {                      // loads are two k tiles ahead; behind the last output tile they fetch it once more, for nobody
         if (to + (int)gridDim.x < tiles) to += gridDim.x;
@@ -472,15 +477,6 @@ __global__ __launch_bounds__(S::kThreads, S::G / 4) void gemm_f4_stream_kernel(G
     int tm, tn;
     tile_of_block(o, tiles, p.tiles_m, p.tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
-    if (bias) {
-      typedef __attribute__((address_space(3))) const f32x4* at;
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const f32x4 b = *(at)(uintptr_t)(biases + (done % S::kBiases) * (S::BN * 4) + (wn * FN * 16 + 16 * j + 4 * (fresh(lane) >> 4)) * 4);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) acc[i][j] += b;
-      }
-    }
     const bool whole = m0 + S::BM <= p.M && n0 + S::BN <= p.N;
     with_extra<F32>(p.epi, [&](auto kind) {
       constexpr int K = decltype(kind)::value;

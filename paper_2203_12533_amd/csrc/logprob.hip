@@ -11,7 +11,8 @@
 // registers, the k-th largest of its 64 lanes' maxima (the upper 16 bits of it) is a bound that k elements at least reach, and
 // usually few more do.  Those go to the list as keys of value and index, 64 bits, no two alike, placed by a ballot; what comes later in the row adds
 // what reaches the bound.  A list that is full gets a tighter bound, and where that does not help - values that fall into few
-// lanes - the k best are taken out one by one.  At the end a wave ranks its list by counting, and the block the waves' k best.
+// lanes - the k best are taken out one by one.  At the end one wave takes the lists together, drops what is below such a bound of all, and ranks the rest
+// by counting (every wave its own list first, in order: 174 us for 8192 rows of 32768 bf16 and k = 32, this 147).
 //
 // Bound by memory: forward one read, backward one read and one write.
 #include <type_traits>
@@ -140,7 +141,7 @@ template <class T> __device__ __forceinline__ Given given_of(const LogprobFwdPar
   return {true, to_f32((reinterpret_cast<const T*>(p.z) + row * p.ldz)[target])};
 }
 
-// What becomes of a row when its parts are together: `all` of the fast sums, the list of n keys that hold the best (LDS, behind a barrier).
+// What becomes of a row when its parts are together: `all` of the fast sums, the list of n keys that hold the best (LDS, the first wave's).
 // The whole block calls; `given` is its first thread's.
 template <class T, int NT>
 __device__ __forceinline__ void finish_row(const LogprobFwdParams& p, int64_t row, Soft all, const uint64_t* list, int n, Soft* wave_soft,
@@ -178,7 +179,7 @@ __device__ __forceinline__ void finish_row(const LogprobFwdParams& p, int64_t ro
     if (p.entropy) p.entropy[row] = none ? 0.f : (log2s - all.t / all.s) * kLn2;
     if (p.stats) *reinterpret_cast<float2*>(p.stats + 2 * row) = make_float2(all.m, none ? 0.f : lse);
   }
-  if (top > 0) {
+  if (top > 0 && wave == 0) {
     const bool bad = !(all.s == all.s);
     if (bad) n = 0;
     auto put = [&](uint64_t key, int rank) {
@@ -187,8 +188,8 @@ __device__ __forceinline__ void finish_row(const LogprobFwdParams& p, int64_t ro
         p.top_logp[row * top + rank] = log_p(value_of(key));
       }
     };
-    for (int i = t; i < n; i += NT) ranks<1>(list, n, i, NT, put);
-    for (int i = n + t; i < top; i += NT) {
+    for (int i = lane; i < n; i += 64) ranks<1>(list, n, i, 64, put);
+    for (int i = n + lane; i < top; i += 64) {
       p.top_id[row * top + i] = -1;
       p.top_logp[row * top + i] = bad ? nan : -INFINITY;
     }
@@ -200,6 +201,31 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// To the front of a list in LDS: those of a wave's keys (0: none), M to a lane, whose upper 16 bits reach the k-th largest of the lanes' maxima.  The k
+// best are among them; how many they are is returned.
+template <int M> __device__ __forceinline__ int shortlist(const uint64_t (&key)[M], int top, uint64_t* list) {
+  uint64_t most = 0;
+#pragma unroll
+  for (int m = 0; m < M; ++m) most = key[m] > most ? key[m] : most;
+  const uint32_t mine16 = (uint32_t)(most >> 48);
+  uint32_t least = 0;
+#pragma unroll
+  for (int b = 15; b >= 0; --b) {
+    const uint32_t tryit = least | 1u << b;
+    if (__popcll(__ballot(mine16 >= tryit)) >= top) least = tryit;
+  }
+  int n = 0;
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    const bool take = key[m] != 0 && (uint32_t)(key[m] >> 48) >= least;
+    const uint64_t who = __ballot(take);
+    if (take) list[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = key[m];
+    n += __popcll(who);
+  }
+  wave_sync();
+  return n;
 }
 
 // NT threads of a block, U vectors of 16 bytes to one in a chunk; a wave's list has kPlaces places, and kMaxTop more for a k best of a chunk.
@@ -353,21 +379,17 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
     a.t = lanes_sum(a.t);
     if (lane == 0) wave_soft[0][wave] = a;
   }
-  if constexpr (TOP) {
-    compact();
-    if (lane == 0) counts[wave] = n;
-  }
+  if (TOP && lane == 0) counts[wave] = n;                // kPlaces / 2 at most
   __syncthreads();
-  int keys = 0;                                          // of all waves
+  int keys = 0;                                          // the first wave's: what can be among the block's k best
   if constexpr (TOP) {
-    int first = 0;
+    if (wave == 0) {
+      constexpr int kPer = kPlaces / 2 / 64;
+      uint64_t key[kWaves * kPer];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) first += counts[w];
-      keys += counts[w];
+      for (int i = 0; i < kWaves * kPer; ++i) key[i] = i % kPer * 64 + lane < counts[i / kPer] ? lists[i / kPer][i % kPer * 64 + lane] : 0;
+      keys = shortlist(key, top, lists[0]);              // all of them are in registers: the lists' place is free
     }
-    if (lane < n) best_keys[first + lane] = list[lane];
-    __syncthreads();
   }
   Soft all = {-INFINITY, 0.f, 0.f};
 #pragma unroll
@@ -379,18 +401,19 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
     all.t += a.t;
   }
   if (p.segments == 1) {
-    finish_row<T, NT>(p, row, all, best_keys, keys, wave_soft[1], given);
+    finish_row<T, NT>(p, row, all, lists[0], keys, wave_soft[1], given);
     return;
   }
   float* const out = p.parts + (int64_t)blockIdx.x * (4 + 2 * p.top);
   if (t == 0) *reinterpret_cast<float2*>(out) = make_float2(all.m, all.s), out[2] = all.t;
   if constexpr (TOP) {
+    if (wave > 0) return;
     uint64_t* const to = reinterpret_cast<uint64_t*>(out + 4);
-    for (int i = t; i < keys; i += NT)
-      ranks<1>(best_keys, keys, i, NT, [&](uint64_t key, int rank) {
+    for (int i = lane; i < keys; i += 64)
+      ranks<1>(lists[0], keys, i, 64, [&](uint64_t key, int rank) {
         if (rank < top) to[rank] = key;
       });
-    for (int i = keys + t; i < top; i += NT) to[i] = 0;    // no key
+    for (int i = keys + lane; i < top; i += 64) to[i] = 0;  // no key
   }
 }
 
@@ -413,34 +436,16 @@ __global__ __launch_bounds__(kJoin) void logprob_join_kernel(LogprobFwdParams p)
     const float* const q = in + lane * (4 + 2 * top);
     all = Soft{q[0], q[1], q[2]};
   }
-  uint64_t key[kPer], best = 0;
+  uint64_t key[kPer];
 #pragma unroll
   for (int m = 0; m < kPer; ++m) {
     const int i = m * kJoin + lane, s = top > 0 ? i / top : 0;
     key[m] = i < p.segments * top ? *reinterpret_cast<const uint64_t*>(in + s * (4 + 2 * top) + 4 + 2 * (i - s * top)) : 0;
-    best = key[m] > best ? key[m] : best;
   }
   all = rebase(all, lanes_max(all.m), bound, k);
   all.s = lanes_sum(all.s);
   all.t = lanes_sum(all.t);
-  int n = 0;
-  if (top > 0) {
-    const uint32_t mine16 = (uint32_t)(best >> 48);
-    uint32_t least = 0;
-#pragma unroll
-    for (int b = 15; b >= 0; --b) {
-      const uint32_t tryit = least | 1u << b;
-      if (__popcll(__ballot(mine16 >= tryit)) >= top) least = tryit;
-    }
-#pragma unroll
-    for (int m = 0; m < kPer; ++m) {
-      const bool take = key[m] != 0 && (uint32_t)(key[m] >> 48) >= least;
-      const uint64_t who = __ballot(take);
-      if (take) list[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = key[m];
-      n += __popcll(who);
-    }
-    __syncthreads();
-  }
+  const int n = top > 0 ? shortlist(key, top, list) : 0;
   finish_row<T, kJoin>(p, row, all, list, n, wave_soft, given);
 }
 

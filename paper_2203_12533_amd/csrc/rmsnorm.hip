@@ -332,7 +332,7 @@ int bwd_rows(int64_t d) {
 }
 int64_t bwd_teams(int64_t rows, int64_t d) {
   const int per = bwd_rows(d);
-  const int64_t teams = (rows + per - 1) / per, most = d <= 512 ? 4 * kBwdTeams : d <= 1024 ? 2 * kBwdTeams : kBwdTeams;
+  const int64_t teams = (rows + per - 1) / per, most = d <= 512 ? 4 * kBwdTeams : kBwdTeams;
   return teams < most ? teams : most;
 }
 

@@ -153,7 +153,7 @@ def codes(seed, rows, k, spread=7):
 
 
 def product(ctx, m, n, k, epilogue=pwb.PW_EPI_STORE, bf16=False, accumulate=0, seed=0, lda=None, ldb=None, ldc=None, bias=True, nan_blocks=(),
-            spread=7, exact=False):
+            spread=7, exact=False, bias_scale=1.0):
     """Runs one product and checks everything it writes.  Returns C as the bits it has."""
     (a, sa), (b, sb) = codes(seed, m, k, 0 if exact else spread), codes(seed + 10, n, k, 0 if exact else spread)
     if exact:
@@ -171,7 +171,7 @@ def product(ctx, m, n, k, epilogue=pwb.PW_EPI_STORE, bf16=False, accumulate=0, s
         table[~own] = 255
     sat, sbt = torch.from_numpy(ta).cuda(), torch.from_numpy(tb).cuda()
     rng = np.random.RandomState(seed + 5)
-    bias_v = rng.randn(n).astype(np.float32)
+    bias_v = (bias_scale * rng.randn(n)).astype(np.float32)
     biast = torch.from_numpy(bias_v).cuda()
     aux = c0 = c2 = auxt = None
     ct = full(m, ldc, 7.0, act(bf16))
@@ -196,8 +196,8 @@ def product(ctx, m, n, k, epilogue=pwb.PW_EPI_STORE, bf16=False, accumulate=0, s
     # (2^-23) of a partial sum, which the sum of magnitudes bounds; up to eight waves' sums and the epilogue's additions
     mag = np.abs(va) @ np.abs(vb).T
     allow = 0.0 * mag if exact else (k // 32 + 8 + 4) * 2.0 ** -23 * mag
-    if has_bias:
-        ref, allow = ref + bias_v, allow + U * (mag + np.abs(bias_v))
+    if has_bias:                                             # sums may begin with it: then it is part of every partial sum, K / 32 of them
+        ref, allow = ref + bias_v, allow + (k // 32 * 2.0 ** -23 + U) * np.abs(bias_v) + U * mag
     if accumulate:
         ref, allow = ref + c0, allow + U * (mag + np.abs(c0))
     if epilogue == pwb.PW_EPI_BIAS_RESIDUAL:
@@ -252,6 +252,11 @@ def test_f4_product_sums_are_exact(ctx, m, n, k):
 @pytest.mark.parametrize("m,n,k,kw", [(40000, 70, 160, {"bf16": True}), (70, 40000, 160, {"accumulate": 1}), (2560, 4096, 4096, {"bf16": True})])
 def test_f4_product_many_tiles(ctx, m, n, k, kw):
     product(ctx, m, n, k, seed=2, **kw)
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 40, 1056), (300, 520, 416), (3100, 2900, 1056)])
+def test_f4_product_beside_a_large_bias(ctx, m, n, k):
+    product(ctx, m, n, k, epilogue=pwb.PW_EPI_BIAS, bias_scale=2.0 ** 24)
 
 
 def test_f4_product_of_rows_far_apart(ctx):
