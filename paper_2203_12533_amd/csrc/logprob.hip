@@ -14,7 +14,12 @@
 // lanes - the k best are taken out one by one.  At the end one wave takes the lists together, drops what is below such a bound of all, and ranks the rest
 // by counting (every wave its own list first, in order: 174 us for 8192 rows of 32768 bf16 and k = 32, this 147).
 //
-// Bound by memory: forward one read, backward one read and one write.
+// Bound by memory: forward one read, backward one read and one write, the forward one nearly as much by its 40 or so cycles per element and lane (exp2 takes
+// four slots of ten).  The last 256 MB of logits, what the large cache holds, are read so that they stay there, and the backward call goes backwards and
+// finds them; all else is read, and the gradient written, past the caches.  8192 rows of 32768 bf16: forward 95 us without alternatives (5.7 TB/s),
+// 121 with 8, 147 with 32; forward with 8 and backward 310, with every access an ordinary one, forwards, 338.  4096 rows of fp32: 95 and 277, so 321.
+// Few rows are cut into segments, a block each, and joined by a second launch (4 rows of 32768 fp32, 20 alternatives: 10.6 us; as one block of 1024
+// threads 15.6); a call of one launch is bound by latency (1 x 4000: 6.3 us).
 #include <type_traits>
 
 #include "common.hpp"
@@ -39,8 +44,7 @@ template <class T> struct Vec;
 template <> struct Vec<float> {
   static constexpr int E = 4;
   static constexpr uint32_t kFill = 0xff800000u;                                // -infinity
-  static __device__ __forceinline__ u32x4 load(const float* p) { return *reinterpret_cast<const u32x4u4*>(p); }
-  static __device__ __forceinline__ void store(float* p, const u32x4& v) { *reinterpret_cast<u32x4u4*>(p) = v; }
+  typedef u32x4u4 At;
   static __device__ __forceinline__ float get(const u32x4& v, int e) { return __uint_as_float(v[e]); }
   static __device__ __forceinline__ void put(u32x4& v, int e, float x) { v[e] = __float_as_uint(x); }
   static __device__ __forceinline__ void fill(u32x4& v, int e, float x) { v[e] = __float_as_uint(x); }
@@ -48,14 +52,17 @@ template <> struct Vec<float> {
 template <> struct Vec<bf16> {
   static constexpr int E = 8;
   static constexpr uint32_t kFill = 0xff80ff80u;
-  static __device__ __forceinline__ u32x4 load(const bf16* p) { return *reinterpret_cast<const u32x4u2*>(p); }
-  static __device__ __forceinline__ void store(bf16* p, const u32x4& v) { *reinterpret_cast<u32x4u2*>(p) = v; }
+  typedef u32x4u2 At;
   static __device__ __forceinline__ float get(const u32x4& v, int e) { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
 };
 // Columns c .. of a row of n (2^28 at most: offsets of bytes are 32 bits beside a uniform address); -infinity behind its end.
-template <class T> __device__ __forceinline__ u32x4 load_vec(const T* row, uint32_t c, uint32_t n) {
+// KEEP: to stay in the caches.
+template <bool KEEP, class T> __device__ __forceinline__ u32x4 load_vec(const T* row, uint32_t c, uint32_t n) {
   constexpr int E = Vec<T>::E;
-  if (c + E <= n) return Vec<T>::load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + c * (uint32_t)sizeof(T)));
+  if (c + E <= n) {
+    const auto p = reinterpret_cast<const typename Vec<T>::At*>(reinterpret_cast<const char*>(row) + c * (uint32_t)sizeof(T));
+    return KEEP ? *p : __builtin_nontemporal_load(p);
+  }
   u32x4 v = {Vec<T>::kFill, Vec<T>::kFill, Vec<T>::kFill, Vec<T>::kFill};
 #pragma unroll
   for (int e = 0; e < E - 1; ++e)
@@ -73,8 +80,9 @@ template <class T> __device__ __forceinline__ u32x4 load_vec(const T* row, uint3
 // The larger; NaN where there is one.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// Where s z overflows, or comes near it, z - max is formed first; a maximum within these bounds leaves room for every product.
-__device__ __forceinline__ float safe_bound(float k) { return 1e38f / fmaxf(k, 1.f); }
+// Rows whose maximum is further from 0 are read again, with z - max formed first: up to 2^22 the rounding of max k shifts d by 1/4 at most, beyond it the sums
+// would lose their bits and overflow.
+__device__ __forceinline__ float safe_bound(float k) { return fminf(4194304.f / k, 1e38f); }
 
 // Order of values and, among equals, of indices from the lowest on, as integers.
 __device__ __forceinline__ uint64_t key_of(float v, uint32_t index) {
@@ -120,6 +128,7 @@ struct LogprobFwdParams {
   int segments;                // that a row is cut into, one to a block; > 1: what they find goes to `parts`, [row][segment] of 4 + 2 top floats
   int64_t segment;             // elements
   float* parts;
+  int64_t kept;                // rows from this one on are left in the caches
 };
 
 // Three numbers of a set of logits: maximum, S and sum of e^d d (base 2) against it.
@@ -243,6 +252,7 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
   const uint32_t from = seg * (uint32_t)p.segment, V = (uint32_t)(from + p.segment < p.vocab ? from + p.segment : p.vocab);   // of this block: from .. V - 1
   const T* const z = reinterpret_cast<const T*>(p.z) + row * p.ldz;
   const float k = p.k, bound = safe_bound(k);
+  const bool keep = row >= p.kept;
   uint64_t* const list = lists[TOP ? wave : 0];
   Given given = {};
   if (t == 0 && p.segments == 1) given = given_of<T>(p, row);
@@ -252,7 +262,7 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
   auto fetch = [&](uint32_t c0) {
     const uint32_t c = c0 + (uint32_t)t * E;
 #pragma unroll
-    for (int u = 0; u < U; ++u) nx[u] = load_vec(z, c + u * NT * E, V);
+    for (int u = 0; u < U; ++u) nx[u] = keep ? load_vec<true>(z, c + u * NT * E, V) : load_vec<false>(z, c + u * NT * E, V);
   };
   Soft mine = {-INFINITY, 0.f, 0.f};
   float thr = -__FLT_MAX__;                              // finite: -infinity is no alternative
@@ -457,6 +467,7 @@ struct LogprobBwdParams {
   const int32_t* targets;
   float scale, k;
   const float *stats, *entropy, *dlogp, *dentropy;
+  int64_t kept;                // rows from this one on may be in a cache
 };
 constexpr int kBwdThreads = 256, kBwdVecs = 4;
 template <class T>
@@ -464,7 +475,8 @@ __global__ __launch_bounds__(kBwdThreads) void logprob_bwd_kernel(LogprobBwdPara
   constexpr int E = Vec<T>::E, U = kBwdVecs;
   constexpr int64_t kSeg = (int64_t)kBwdThreads * U * E;
   const float k = p.k, bound = safe_bound(k);
-  for (int64_t b = blockIdx.x; b < p.rows * p.segments; b += gridDim.x) {
+  // Backwards: the last rows may be in a cache.
+  for (int64_t b = p.rows * p.segments - 1 - blockIdx.x; b >= 0; b -= gridDim.x) {
     const int64_t row = b / p.segments, c0 = (b - row * p.segments) * kSeg + (int64_t)threadIdx.x * E, V = p.vocab;
     const T* const z = reinterpret_cast<const T*>(p.z) + row * p.ldz;
     T* const dz = reinterpret_cast<T*>(p.dz) + row * p.lddz;
@@ -472,7 +484,7 @@ __global__ __launch_bounds__(kBwdThreads) void logprob_bwd_kernel(LogprobBwdPara
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t c = c0 + (int64_t)u * kBwdThreads * E;
-      if (c < V) v[u] = load_vec(z, c, V);
+      if (c < V) v[u] = row >= p.kept ? load_vec<true>(z, c, V) : load_vec<false>(z, c, V);
     }
     const float2 st = *reinterpret_cast<const float2*>(p.stats + 2 * row);
     const int target = p.targets ? p.targets[row] : -1;
@@ -480,18 +492,28 @@ __global__ __launch_bounds__(kBwdThreads) void logprob_bwd_kernel(LogprobBwdPara
     const float dl = given ? p.dlogp[row] * p.scale : 0.f, de = p.dentropy ? p.dentropy[row] * p.scale : 0.f;
     const bool none = st.x == -INFINITY && st.y == 0.f, extreme = !(fabsf(st.x) <= bound);
     const float mk = shift_of(st.x, bound, k), log2s = st.y * kLog2e + (extreme ? 0.f : shift_error(st.x, bound, k));
-    // dz = p (a0 + a1 log2 p) + [v = t] dl
+    // dz = p (a0 + a1 log2 p) + [v = t] dl.  A row like any other takes one multiply-add for log2 p, against c1 = max k + log2 S rounded to 32 bits: what
+    // that leaves, c2, goes into a0 and a1.
     const float a0 = -(dl + (p.dentropy ? de * p.entropy[row] : 0.f)), a1 = -de * kLn2;
+    const float c1 = mk + log2s, b1 = c1 - mk, c2 = (mk - (c1 - b1)) + (log2s - b1), f = __builtin_amdgcn_exp2f(-c2);
+    const float f0 = f * (a0 - a1 * c2), f1 = f * a1;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t c = c0 + (int64_t)u * kBwdThreads * E;
       if (c >= V) break;
       float o[E];
+      if (!(none || extreme)) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float x = Vec<T>::get(v[u], e);
-        const float d = larger((extreme ? (x - st.x) * k : __builtin_fmaf(x, k, -mk)) - log2s, kFloor), q = __builtin_amdgcn_exp2f(d);
-        o[e] = none ? 0.f : q * __builtin_fmaf(a1, d, a0);
+        for (int e = 0; e < E; ++e) {
+          const float d = larger(__builtin_fmaf(Vec<T>::get(v[u], e), k, -c1), kFloor);
+          o[e] = __builtin_amdgcn_exp2f(d) * __builtin_fmaf(f1, d, f0);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float d = larger((Vec<T>::get(v[u], e) - st.x) * k - log2s, kFloor);
+          o[e] = none ? 0.f : __builtin_amdgcn_exp2f(d) * __builtin_fmaf(a1, d, a0);
+        }
       }
       if (given && !none && target >= c && target < c + E) {
 #pragma unroll
@@ -506,7 +528,7 @@ __global__ __launch_bounds__(kBwdThreads) void logprob_bwd_kernel(LogprobBwdPara
         for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(o[i]);
       }
       if (c + E <= V) {
-        Vec<T>::store(dz + c, w);
+        __builtin_nontemporal_store((typename Vec<T>::At)w, reinterpret_cast<typename Vec<T>::At*>(dz + c));
       } else {
 #pragma unroll
         for (int e = 0; e < E - 1; ++e)
@@ -525,7 +547,14 @@ hipError_t check(const LogprobArgs& a) {
 
 }  // namespace
 
+// The first row of the last 256 MB, which is what the large cache holds.
+static int64_t kept_from(const LogprobArgs& a) {
+  const int64_t rows = (256LL << 20) / (a.vocab * (a.dtype == kBF16 ? 2 : 4));
+  return rows < a.rows ? a.rows - rows : 0;
+}
 // How many segments rows are cut into: where there are too few rows for the chip, as many as keep 4096 elements each.
+// In us, cut and as one block of 1024 threads: 1 x 16384 bf16 11.7 and 13.4, 1 x 131072 11.9 and 25.5, 256 x 32768 15.4 and 14.5, 256 x 131072 29.8 and 28.2, 300 x
+// 32768 19.7 and 26.4, 511 x 32768 20.2 and 26.9; 600 rows are enough uncut (19.9).
 static int segments_of(int64_t rows, int64_t vocab) {
   if (rows >= 512 || vocab < 8192) return 1;
   int64_t n = 1024 / (rows < 1 ? 1 : rows);
@@ -548,7 +577,7 @@ hipError_t launch_logprob_fwd(hipStream_t s, const LogprobArgs& a, float* logp, 
   if (a.rows == 0) return hipSuccess;
   const int n = segments_of(a.rows, a.vocab);
   const LogprobFwdParams p{a.z, a.ldz, a.rows, a.vocab, a.targets, a.scale, a.scale * kLog2e, logp, entropy, stats, k, top_id, top_logp, n,
-                           (a.vocab + n - 1) / n, ws};
+                           (a.vocab + n - 1) / n, ws, kept_from(a)};
   auto run = [&](auto t, auto with_top) {
     using T = decltype(t);
     constexpr bool TOP = decltype(with_top)::value;
@@ -573,7 +602,7 @@ hipError_t launch_logprob_bwd(hipStream_t s, const LogprobArgs& a, const float* 
     return hipErrorInvalidValue;
   if (a.rows == 0) return hipSuccess;
   const int64_t seg = (int64_t)kBwdThreads * kBwdVecs * (a.dtype == kBF16 ? 8 : 4), segments = (a.vocab + seg - 1) / seg;
-  const LogprobBwdParams p{a.z, dz, a.ldz, lddz, a.rows, a.vocab, segments, a.targets, a.scale, a.scale * kLog2e, stats, entropy, dlogp, dentropy};
+  const LogprobBwdParams p{a.z, dz, a.ldz, lddz, a.rows, a.vocab, segments, a.targets, a.scale, a.scale * kLog2e, stats, entropy, dlogp, dentropy, kept_from(a)};
   const int64_t blocks = a.rows * segments, most = 1 << 20;
   const unsigned grid = (unsigned)(blocks < most ? blocks : most);
   if (a.dtype == kF32) logprob_bwd_kernel<float><<<grid, kBwdThreads, 0, s>>>(p);

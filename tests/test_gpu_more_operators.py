@@ -531,10 +531,11 @@ def logprob(ctx, z, targets, scale=1.0, k=0, bf16=False, ldz=None, offset=0, bac
     lpv = np.where(np.isfinite(lpv), lpv, 0.0)
     dl, de = np.abs(np.where(given, dl, 0.0))[:, None], np.abs(de)[:, None]
     h = np.abs(np.where(np.isfinite(rh), rh, 0.0))[:, None]
-    # an error of log p is one of p, relative; the products and additions of the formula on top; p below 2^-126 may be 0
+    # an error of log p is one of p, relative; the products and additions of the formula on top; p below 2^-126 may be 0, whatever it is multiplied
+    # with then, s (dl + de (|log p| + H)), and so may the result
     hot = np.zeros_like(ref)
     hot[np.arange(rows)[given], t[given]] = 1.0
-    allow = s * (pr * (dl * (elp + 8 * U) + de * (elp * (np.abs(lpv) + h + 1) + eh[:, None] + 8 * U * (np.abs(lpv) + h))) + 4 * U * dl * hot) + TINY
+    allow = s * (pr * (dl * (elp + 8 * U) + de * (elp * (np.abs(lpv) + h + 1) + eh[:, None] + 8 * U * (np.abs(lpv) + h))) + 4 * U * dl * hot) + TINY + 2.0 ** -125 * s * (dl + de * (np.abs(lpv) + h))
     allow = np.where(np.isfinite(allow), allow, 0.0)
     within(back(out)[:, :vocab], ref, allow, "dz", EPS[bf16])
     if not in_place:
@@ -621,6 +622,20 @@ def test_log_probabilities_of_masked_rows_and_special_values(ctx, bf16):
     logprob(ctx, z, t, 2.0, 7, bf16, backward=False)
     t[[0, 7, 11]] = [200, 41, 100]                              # a masked token is the given one
     logprob(ctx, z, t, 0.5, 0, bf16)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("vocab", [300, 9000])
+def test_log_probabilities_of_rows_far_from_zero(ctx, vocab, bf16):
+    """Maxima of any size, several of them in a row, and logits a few steps of the type below: differences are what counts."""
+    tops = np.array([s * m for m in (1000.0, 2.0 ** 21, 4.1e6, 5e6, 3e7, 2.0 ** 28, 1e10, 3e14, 1e20, 1e30, 5e37) for s in (1, -1)])
+    step = np.exp2(np.floor(np.log2(np.abs(tops))) - (7 if bf16 else 23))
+    back_by = np.random.RandomState(3).randint(0, 30, (tops.size, vocab))
+    z = low(tops, bf16)[:, None] - np.where(tops < 0, 1, 0.5)[:, None] * step[:, None] * back_by
+    t = np.arange(tops.size) * 7
+    for k, scale in ((5, 1.0), (0, 0.7), (0, 1e-7), (3, 37.0)):
+        z[:, [11, vocab - 1]] = low(tops, bf16)[:, None]
+        logprob(ctx, z, t, scale, k, bf16)
 
 
 def test_log_probabilities_write_what_is_asked_for_and_repeat_their_bits(ctx):
