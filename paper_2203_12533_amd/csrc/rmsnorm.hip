@@ -5,7 +5,7 @@
 //
 // Bound by memory: a row is read once into registers (a wave to a row of up to 2048 columns, a block beyond), four consecutive columns to a
 // lane, so that every load and store of 4, 2 or 1 byte an element covers whole lines; 32 lanes hold a block of 128 columns, whose largest
-// magnitude takes five moves between lanes.  8192 x 2048 bf16 with x' and 8 bits, nothing of it cached: forward 44.7 us (4.9 TB/s), backward 50.4 (5.3); rows
+// magnitude takes five moves between lanes.  8192 x 2048 bf16 with x' and 8 bits, nothing of it cached: forward 43.4 us (5.0 TB/s), backward 51 (5.3); rows
 // read like everything else 51 and 53.  One row: 4.7 us, a launch.  What the separate passes would move besides: x' once more for the norm, h once more for the
 // quantisation.  Sums, r and h are fp32; q rounds h once, and so does h in bf16.
 #include <type_traits>
@@ -21,45 +21,54 @@ namespace {
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));        // wherever an element may be
 typedef unsigned short u16x4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
 
-// Columns c .. c + 3 of a row of d; zeros behind its end.  ONCE: nothing reads them again, and they leave the caches to what is written.
-template <bool ONCE> __device__ __forceinline__ f32x4 load4(const float* p, int c, int d) {
-  if (c + 4 <= d) {
-    const f32x4u* const at = reinterpret_cast<const f32x4u*>(p + c);
+// Columns c .. c + 3 of a row of d: four elements as they are stored, asked for without a question, from the row's last four columns where those wanted are
+// not all there, and put in their place, zeros behind the row, when they are used: a branch at each load makes it wait for the one before (8192 x 1000
+// backward 48 us, this 29; forward 21 and 25, of 2001 columns 24.7 and 21.6).  ONCE: nothing reads them again, and they leave the caches to what is written.
+// Rows that are a team's vectors exactly need none of it; rows of fewer than four columns are one lane's.
+enum Edge { kWhole, kAny, kTiny };
+__device__ __forceinline__ int last4(int c, int d) { return c + 4 <= d ? c : d - 4; }
+template <class T, Edge EDGE> struct Stored;
+template <Edge EDGE> struct Stored<float, EDGE> {
+  typedef f32x4u type;
+  template <bool ONCE> static __device__ __forceinline__ type load(const float* p, int c, int d) {
+    if constexpr (EDGE == kTiny) return type{p[0], d > 1 ? p[1] : 0.f, d > 2 ? p[2] : 0.f, 0.f};
+    const type* const at = reinterpret_cast<const type*>(p + (EDGE == kWhole ? c : last4(c, d)));
     return ONCE ? __builtin_nontemporal_load(at) : *at;
   }
-  f32x4 v = {};
+  static __device__ __forceinline__ f32x4 wide(const type& w, int c, int d) {
+    f32x4 v = w;
+    const int off = EDGE == kWhole ? 0 : EDGE == kTiny ? c : c - last4(c, d);
+    if (off > 0) {
 #pragma unroll
-  for (int e = 0; e < 3; ++e)
-    if (c + e < d) v[e] = p[c + e];
-  return v;
-}
-struct Bf4 { u16x4u v; };
-template <class T> struct Stored;            // four elements as they are stored, read once
-template <> struct Stored<float> {
-  typedef f32x4 type;
-  static __device__ __forceinline__ type load(const float* p, int c, int d) { return load4<true>(p, c, d); }
-  static __device__ __forceinline__ f32x4 wide(type v) { return v; }
-};
-template <> struct Stored<bf16> {
-  typedef uint2 type;
-  static __device__ __forceinline__ type load(const bf16* p, int c, int d) {
-    u16x4u v = {};
-    if (c + 4 <= d) {
-      v = __builtin_nontemporal_load(reinterpret_cast<const u16x4u*>(p + c));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 3; ++e)
-        if (c + e < d) v[e] = __builtin_bit_cast(unsigned short, p[c + e]);
+      for (int e = 0; e < 4; ++e) v[e] = off == 1 && e < 3 ? w[(e + 1) & 3] : off == 2 && e < 2 ? w[(e + 2) & 3] : off == 3 && e < 1 ? w[3] : 0.f;
     }
-    return make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
-  }
-  static __device__ __forceinline__ f32x4 wide(type v) {
-    return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
+    return v;
   }
 };
-__device__ __forceinline__ void store4(float* p, int c, int d, const f32x4& v) {
-  if (c + 4 <= d) {
+template <Edge EDGE> struct Stored<bf16, EDGE> {
+  typedef u32x2u type;
+  template <bool ONCE> static __device__ __forceinline__ type load(const bf16* p, int c, int d) {
+    if constexpr (EDGE == kTiny) {
+      auto at = [&](int e) { return e < d ? (uint32_t)__builtin_bit_cast(unsigned short, p[e]) : 0u; };
+      return type{at(0) | at(1) << 16, at(2)};
+    }
+    const type* const at = reinterpret_cast<const type*>(p + (EDGE == kWhole ? c : last4(c, d)));
+    return ONCE ? __builtin_nontemporal_load(at) : *at;
+  }
+  static __device__ __forceinline__ f32x4 wide(const type& w, int c, int d) {
+    type v = w;
+    const int off = EDGE == kWhole ? 0 : EDGE == kTiny ? c : c - last4(c, d);
+    if (off > 0) {
+      const uint64_t x = off < 4 ? ((uint64_t)w[1] << 32 | w[0]) >> (16 * off) : 0;
+      v = type{(uint32_t)x, (uint32_t)(x >> 32)};
+    }
+    return f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xffff0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xffff0000u)};
+  }
+};
+template <Edge EDGE> __device__ __forceinline__ void store4(float* p, int c, int d, const f32x4& v) {
+  if (EDGE == kWhole || c + 4 <= d) {
     *reinterpret_cast<f32x4u*>(p + c) = v;
   } else {
 #pragma unroll
@@ -67,9 +76,9 @@ __device__ __forceinline__ void store4(float* p, int c, int d, const f32x4& v) {
       if (c + e < d) p[c + e] = v[e];
   }
 }
-__device__ __forceinline__ void store4(bf16* p, int c, int d, const f32x4& v) {
+template <Edge EDGE> __device__ __forceinline__ void store4(bf16* p, int c, int d, const f32x4& v) {
   const bf16x4 o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
-  if (c + 4 <= d) {
+  if (EDGE == kWhole || c + 4 <= d) {
     *reinterpret_cast<u16x4u*>(p + c) = __builtin_bit_cast(u16x4u, o);
   } else {
 #pragma unroll
@@ -93,24 +102,27 @@ struct RmsFwdParams {
 
 // NT threads to a row, VEC times four columns to a thread; a block of 64 threads per row has four rows.  F8: 0 no 8-bit output, 1 e4m3, 2 e5m2.
 template <int NT> constexpr int kBlock = NT < 256 ? 256 : NT;
-template <class T, int NT, int VEC, int F8>
+template <class T, int NT, int VEC, int F8, Edge EDGE>
 __global__ __launch_bounds__(kBlock<NT>) void rmsnorm_fwd_kernel(RmsFwdParams p) {
+  typedef Stored<float, EDGE> Wide;
+  typedef Stored<T, EDGE> Narrow;
   constexpr int kTeams = kBlock<NT> / NT, kWaves = NT / 64;
   __shared__ float red[3][NT > 64 ? kWaves : 1];
   const int team = NT < 256 ? threadIdx.x / NT : 0, t = threadIdx.x % NT, d = p.d;
   const int64_t step = (int64_t)gridDim.x * kTeams;
   const float inv_d = 1.f / (float)d;
-  f32x4 v[VEC], nx[VEC];
-  typename Stored<T>::type ny[VEC];
+  f32x4 v[VEC];
+  typename Wide::type nx[VEC];
+  typename Narrow::type ny[VEC];
   // The next row of this team travels while the current one is reduced and stored.
   auto fetch = [&](int64_t n) {
     const float* const xr = p.x + n * p.ldx;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) nx[i] = load4<true>(xr, 4 * (t + i * NT), d);
+    for (int i = 0; i < VEC; ++i) nx[i] = Wide::template load<true>(xr, 4 * (t + i * NT), d);
     if (p.y) {
       const T* const yr = reinterpret_cast<const T*>(p.y) + n * p.ldh;
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) ny[i] = Stored<T>::load(yr, 4 * (t + i * NT), d);
+      for (int i = 0; i < VEC; ++i) ny[i] = Narrow::template load<true>(yr, 4 * (t + i * NT), d);
     }
   };
   // Over the team; the sums of two calls in turn lie apart, so that one barrier is enough.
@@ -133,8 +145,8 @@ __global__ __launch_bounds__(kBlock<NT>) void rmsnorm_fwd_kernel(RmsFwdParams p)
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-      v[i] = nx[i];
-      if (p.y) v[i] += Stored<T>::wide(ny[i]);
+      v[i] = Wide::wide(nx[i], 4 * (t + i * NT), d);
+      if (p.y) v[i] += Narrow::wide(ny[i], 4 * (t + i * NT), d);
     }
     if (n + step < p.rows) fetch(n + step);
 #pragma unroll
@@ -156,18 +168,18 @@ __global__ __launch_bounds__(kBlock<NT>) void rmsnorm_fwd_kernel(RmsFwdParams p)
     if (p.rstd && t == 0) p.rstd[n] = r;
     if (p.x_out) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) store4(p.x_out + n * p.ldx, 4 * (t + i * NT), d, v[i]);
+      for (int i = 0; i < VEC; ++i) store4<EDGE>(p.x_out + n * p.ldx, 4 * (t + i * NT), d, v[i]);
     }
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       const int c = 4 * (t + i * NT);
       f32x4 h = v[i] * r;
-      if (c < d) h *= load4<false>(p.g, c, d);
-      if (p.h) store4(reinterpret_cast<T*>(p.h) + n * p.ldh, c, d, h);
+      h *= Wide::wide(Wide::template load<false>(p.g, c, d), c, d);
+      if (p.h) store4<EDGE>(reinterpret_cast<T*>(p.h) + n * p.ldh, c, d, h);
       if constexpr (F8 != 0) {
         constexpr bool E5M2 = F8 == 2;
         uint32_t m = 0;
-        if (c + 4 > d) {                     // zeros behind the row, also where r is NaN
+        if (EDGE != kWhole && c + 4 > d) {   // zeros behind the row, also where r is NaN
 #pragma unroll
           for (int e = 0; e < 4; ++e) h[e] = c + e < d ? h[e] : 0.f;
         }
@@ -207,6 +219,13 @@ template <class F> void by_size(int64_t rows, int64_t d, F&& f) {
   else if (d <= 8192) f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
   else f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
 }
+template <int NT, int VEC, class F> void by_edge(int64_t d, F&& f) {
+  using std::integral_constant;
+  if (d == 4 * NT * VEC) return f(integral_constant<Edge, kWhole>{});
+  if constexpr (NT == 64 && VEC == 1)
+    if (d < 4) return f(integral_constant<Edge, kTiny>{});
+  f(integral_constant<Edge, kAny>{});
+}
 constexpr int64_t kMaxCols = 16384, kMaxRows = (1LL << 31) - 1;
 
 // ---- backward ----------------------------------------------------------------------------------------------------
@@ -221,19 +240,22 @@ struct RmsBwdParams {
   int64_t rows, ldx, ldh, stride;
   int d, accumulate;                         // accumulate: one team adds into dg
 };
-template <class T, int NT, int VEC, int ROWS>
+template <class T, int NT, int VEC, int ROWS, Edge EDGE>
 __global__ __launch_bounds__(NT) void rmsnorm_bwd_kernel(RmsBwdParams p) {
+  typedef Stored<float, EDGE> Wide;
+  typedef Stored<T, EDGE> Narrow;
   constexpr int kWaves = NT / 64;
   __shared__ float red[2][ROWS][kWaves];
   const int t = threadIdx.x, d = p.d;
   const int64_t step = (int64_t)gridDim.x * ROWS;
   const float inv_d = 1.f / (float)d;
-  f32x4 gv[VEC], acc[VEC], xv[ROWS][VEC], rv[ROWS][VEC];
-  typename Stored<T>::type dv[ROWS][VEC];
+  f32x4 gv[VEC], acc[VEC];
+  typename Wide::type xv[ROWS][VEC], rv[ROWS][VEC];
+  typename Narrow::type dv[ROWS][VEC];
   float rs[ROWS];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
-    gv[i] = load4<false>(p.g, 4 * (t + i * NT), d);
+    gv[i] = Wide::wide(Wide::template load<false>(p.g, 4 * (t + i * NT), d), 4 * (t + i * NT), d);
     acc[i] = f32x4{};
   }
   auto fetch = [&](int64_t n0) {
@@ -245,9 +267,9 @@ __global__ __launch_bounds__(NT) void rmsnorm_bwd_kernel(RmsBwdParams p) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         const int c = 4 * (t + i * NT);
-        xv[r][i] = load4<true>(p.x + n * p.ldx, c, d);
-        dv[r][i] = Stored<T>::load(reinterpret_cast<const T*>(p.dh) + n * p.ldh, c, d);
-        if (p.dres) rv[r][i] = load4<true>(p.dres + n * p.ldx, c, d);
+        xv[r][i] = Wide::template load<true>(p.x + n * p.ldx, c, d);
+        dv[r][i] = Narrow::template load<true>(reinterpret_cast<const T*>(p.dh) + n * p.ldh, c, d);
+        if (p.dres) rv[r][i] = Wide::template load<true>(p.dres + n * p.ldx, c, d);
       }
     }
   };
@@ -266,9 +288,10 @@ __global__ __launch_bounds__(NT) void rmsnorm_bwd_kernel(RmsBwdParams p) {
       if (n0 + r >= p.rows) continue;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const f32x4 dh = Stored<T>::wide(dv[r][i]);
-        xh[r][i] = xv[r][i] * rr[r];
-        if (p.dres) dr[r][i] = rv[r][i];
+        const int c = 4 * (t + i * NT);
+        const f32x4 dh = Narrow::wide(dv[r][i], c, d);
+        xh[r][i] = Wide::wide(xv[r][i], c, d) * rr[r];
+        if (p.dres) dr[r][i] = Wide::wide(rv[r][i], c, d);
         acc[i] += dh * xh[r][i];
         dg[r][i] = dh * gv[i];
         const f32x4 m = dg[r][i] * xh[r][i];
@@ -301,8 +324,8 @@ __global__ __launch_bounds__(NT) void rmsnorm_bwd_kernel(RmsBwdParams p) {
         const int c = 4 * (t + i * NT);
         f32x4 o = (dg[r][i] - xh[r][i] * m) * rr[r];
         if (p.dres) o += dr[r][i];
-        store4(p.dx + n * p.ldx, c, d, o);
-        if (p.dy) store4(reinterpret_cast<T*>(p.dy) + n * p.ldh, c, d, o);
+        store4<EDGE>(p.dx + n * p.ldx, c, d, o);
+        if (p.dy) store4<EDGE>(reinterpret_cast<T*>(p.dy) + n * p.ldh, c, d, o);
       }
     }
   }
@@ -311,8 +334,8 @@ __global__ __launch_bounds__(NT) void rmsnorm_bwd_kernel(RmsBwdParams p) {
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
     const int c = 4 * (t + i * NT);
-    if (p.accumulate) acc[i] += load4<false>(out, c, d);
-    store4(out, c, d, acc[i]);
+    if (p.accumulate) acc[i] += Wide::wide(Wide::template load<false>(out, c, d), c, d);
+    store4<EDGE>(out, c, d, acc[i]);
   }
 }
 constexpr int kBwdTeams = 512;
@@ -363,7 +386,10 @@ hipError_t launch_rmsnorm_fwd(hipStream_t s, const RmsnormArgs& a, const float* 
     by_size(a.rows, a.cols, [&](auto nt, auto vec) {
       constexpr int NT = decltype(nt)::value, VEC = decltype(vec)::value, kTeams = kBlock<NT> / NT;
       const int64_t blocks = (a.rows + kTeams - 1) / kTeams, most = NT == 1024 ? 512 : NT == 256 ? 2048 : 1024;
-      rmsnorm_fwd_kernel<decltype(t), NT, VEC, decltype(f8)::value><<<(unsigned)(blocks < most ? blocks : most), kBlock<NT>, 0, s>>>(p);
+      const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+      by_edge<NT, VEC>(a.cols, [&](auto edge) {
+        rmsnorm_fwd_kernel<decltype(t), NT, VEC, decltype(f8)::value, decltype(edge)::value><<<grid, kBlock<NT>, 0, s>>>(p);
+      });
     });
   };
   auto format = [&](auto t) {
@@ -398,7 +424,9 @@ hipError_t launch_rmsnorm_bwd(hipStream_t s, const RmsnormArgs& a, const void* d
   auto run = [&](auto t) {
     by_width_bwd(a.cols, [&](auto nt, auto vec) {
       constexpr int NT = decltype(nt)::value, VEC = decltype(vec)::value;
-      rmsnorm_bwd_kernel<decltype(t), NT, VEC, kBwdRows<NT, VEC>><<<(unsigned)teams, NT, 0, s>>>(p);
+      by_edge<NT, VEC>(a.cols, [&](auto edge) {
+        rmsnorm_bwd_kernel<decltype(t), NT, VEC, kBwdRows<NT, VEC>, decltype(edge)::value><<<(unsigned)teams, NT, 0, s>>>(p);
+      });
     });
   };
   if (a.dtype == kF32) run(float{});
