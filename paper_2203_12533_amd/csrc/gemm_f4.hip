@@ -278,6 +278,14 @@ __device__ __forceinline__ int fresh(int v) {
   return v;
 }
 
+// The order of tiles, with the columns of each group of eight rows of tiles turned by an eighth of them (by four where that is less): what is written at one time is spread over
+// whole rows of C.  Else the eight XCDs write the same few columns of rows that are a power of two apart, which share memory channels.  Into arrays that no cache holds, bf16, us, unturned and turned:
+// 8192 x 8192 x 2048 92 and 83, 8192 x 8192 x 8192 251 and 237, 16384 x 16384 x 512 219 and 143, 8192 x 7168 x 2048 79.7 and 79.1.
+__device__ __forceinline__ void stream_tile(int o, int tiles, int tiles_m, int tiles_n, int& tm, int& tn) {
+  tile_of_block(o, tiles, tiles_m, tiles_n, tm, tn);
+  tn += tm / 8 * (tiles_n > 32 ? tiles_n / 8 : 4) % tiles_n;
+  if (tn >= tiles_n) tn -= tiles_n;
+}
 template <class S, bool F32>
 __global__ __launch_bounds__(S::kThreads, S::G / 4) void gemm_f4_stream_kernel(GemmF4Params p) {
   constexpr int FM = S::FM, FN = S::FN, G = S::G, WN = S::WN;
@@ -305,7 +313,7 @@ __global__ __launch_bounds__(S::kThreads, S::G / 4) void gemm_f4_stream_kernel(G
   const bool partial = p.K % kF4BK != 0;
   auto begin = [&] {                                        // the loads of output tile `to`
     int tm, tn;
-    tile_of_block(to, tiles, p.tiles_m, p.tiles_n, tm, tn);
+    stream_tile(to, tiles, p.tiles_m, p.tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
     const int mine = fresh(lane);
     oa.init(p.A, p.lda, m0, p.M, 0, wave, mine);
@@ -475,7 +483,7 @@ __global__ __launch_bounds__(S::kThreads, S::G / 4) void gemm_f4_stream_kernel(G
       st = S::kStage - st;
     }
     int tm, tn;
-    tile_of_block(o, tiles, p.tiles_m, p.tiles_n, tm, tn);
+    stream_tile(o, tiles, p.tiles_m, p.tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
     const bool whole = m0 + S::BM <= p.M && n0 + S::BN <= p.N;
     with_extra<F32>(p.epi, [&](auto kind) {
