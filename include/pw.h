@@ -754,8 +754,8 @@ typedef struct {
 /* logp, entropy: fp32 [rows], or null (logp needs targets).  stats: fp32 [rows][2], 8-byte aligned, for the backward call, or null: the largest z and the log of sum
  * exp(s (z - that)).  top_id: int32 [rows][k] and top_logp: fp32 [rows][k], the k tokens of largest z in descending order, the lowest index first among
  * equals, and their log probabilities; k at most 32 (0: both null); places that no token is left for hold -1 and -infinity.
- * ws: workspace of pw_logprob_ws_floats(rows, vocab, k) floats, 8-byte aligned (may be null where that is 0); nothing in it outlasts the call, and calls that can run at the
- * same time need one each.  The outputs overlap nothing else. */
+ * ws: workspace of pw_logprob_ws_floats(rows, vocab, k) floats, 8-byte aligned (may be null where that is 0); nothing in it outlasts the
+ * call, and calls that can run at the same time need one each.  The outputs overlap nothing else. */
 pw_status pw_op_logprob_fwd(pw_ctx* ctx, const pw_logprob_args* args, float* logp, float* entropy, float* stats, int k, int32_t* top_id,
                             float* top_logp, float* ws);
 int64_t pw_logprob_ws_floats(int64_t rows, int64_t vocab, int k);   /* -1 for impossible sizes */
@@ -773,9 +773,9 @@ typedef struct {
   int64_t n;                 /* elements */
   int32_t dtype;             /* PW_F32 or PW_BF16 */
 } pw_grad_tensor;
-/* tensors: host array of `count`, read during the call; count at most 2^20, elements at most 2^40 altogether.  max_norm >= 0 (infinity: factor is 1).  result: device, fp32 [2], receives norm and
- * factor.  ws: workspace of pw_grad_clip_ws_floats() floats, 8-byte aligned; nothing in it outlasts the call, and calls that can run at the same time need one each.
- * An output overlaps nothing but its own g (as a whole).  If one tensor is refused nothing is enqueued. */
+/* tensors: host array of `count`, read during the call; count at most 2^20, elements at most 2^40 altogether.  max_norm >= 0 (infinity:
+ * factor is 1).  result: device, fp32 [2], receives norm and factor.  ws: workspace of pw_grad_clip_ws_floats() floats, 8-byte aligned;
+ * nothing in it outlasts the call, and calls that can run at the same time need one each.  An output overlaps nothing but its own g (as a whole).  If one tensor is refused nothing is enqueued. */
 pw_status pw_op_grad_clip(pw_ctx* ctx, const pw_grad_tensor* tensors, int count, float max_norm, float* result, float* ws);
 int64_t pw_grad_clip_ws_floats(void);
 

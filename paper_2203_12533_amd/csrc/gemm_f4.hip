@@ -278,9 +278,10 @@ __device__ __forceinline__ int fresh(int v) {
   return v;
 }
 
-// The order of tiles, with the columns of each group of eight rows of tiles turned by an eighth of them (by four where that is less): what is written at one time is spread over
-// whole rows of C.  Else the eight XCDs write the same few columns of rows that are a power of two apart, which share memory channels.  Into arrays that no cache holds, bf16, us, unturned and turned:
-// 8192 x 8192 x 2048 92 and 83, 8192 x 8192 x 8192 251 and 237, 16384 x 16384 x 512 219 and 143, 8192 x 7168 x 2048 79.7 and 79.1.
+// The order of tiles, with the columns of each group of eight rows of tiles turned by an eighth of them (by four where that is less): what is written
+// at one time is spread over whole rows of C.  Else the eight XCDs write the same few columns of rows that are a power of two apart, which share
+// memory channels.  Into arrays that no cache holds, bf16, us, unturned and turned: 8192 x 8192 x 2048 92 and 83, 8192 x 8192 x 8192 251 and 237,
+// 16384 x 16384 x 512 219 and 143, 8192 x 7168 x 2048 79.7 and 79.1.
 __device__ __forceinline__ void stream_tile(int o, int tiles, int tiles_m, int tiles_n, int& tm, int& tn) {
   tile_of_block(o, tiles, tiles_m, tiles_n, tm, tn);
   tn += tm / 8 * (tiles_n > 32 ? tiles_n / 8 : 4) % tiles_n;

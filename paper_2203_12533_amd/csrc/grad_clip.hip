@@ -7,10 +7,10 @@
 // take chunks of tensors in turn and leave a sum each, then every block of the second adds those sums in the same order (16 KB or
 // less, from the cache) and scales its chunks.
 //
-// Bound by memory: two reads and a write of 4 (2) bytes.  The last 256 MB, what the large cache holds, are read so that they stay there, and the second launch
-// goes backwards and finds them; all else is read and written past the caches.  336e6 fp32 elements: norm 193 us (6.9 TB/s), all 610 (6.6 TB/s of
-// three passes over memory); with every access an ordinary one 247 and 765, forwards through the second too and on 1024 blocks.
-// 67e6 elements 117 us, with nothing kept 132, with ordinary stores 164.  A small set is two launches: 24 tensors of 139e3 elements 9.3 us.
+// Bound by memory: two reads and a write of 4 (2) bytes.  The last 256 MB, what the large cache holds, are read so that they stay there, and the
+// second launch goes backwards and finds them; all else is read and written past the caches.  336e6 fp32 elements: norm 193 us (6.9 TB/s), all 610
+// (6.6 TB/s of three passes over memory); with every access an ordinary one 247 and 765, forwards through the second too and on 1024 blocks. 67e6
+// elements 117 us, with nothing kept 132, with ordinary stores 164.  A small set is two launches: 24 tensors of 139e3 elements 9.3 us.
 #include "common.hpp"
 #include "kernels.hpp"
 

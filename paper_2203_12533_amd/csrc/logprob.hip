@@ -3,9 +3,9 @@
 //   d_v = s (z_v - max z),  S = sum e^d,  logp = d_t - log S,  H = log S - (sum e^d d) / S          (both terms of H are >= 0: nothing cancels)
 //   dz_v = s [dlogp ([v = t] - p_v) - dentropy p_v (log p_v + H)],  p_v = e^(d_v - log S)
 //
-// In base 2: d = z k - max k with k = s log2 e, one fused multiply-add, whose product is exact; that max k is rounded shifts all of a row
-// alike, by an amount that is known and taken off log S.  Every thread keeps a running maximum, S and sum of its own; they meet once per row.  Sums are fp32, of at most
-// vocab / threads terms before they meet in a tree.
+// In base 2: d = z k - max k with k = s log2 e, one fused multiply-add, whose product is exact; that max k is rounded shifts all of a row alike, by
+// an amount that is known and taken off log S.  Every thread keeps a running maximum, S and sum of its own; they meet once per row.  Sums are fp32,
+// of at most vocab / threads terms before they meet in a tree.
 //
 // Alternatives.  Every wave keeps a list in LDS of what can be among the k best of its columns, without a word to the others: with a part of the row in
 // registers, the k-th largest of its 64 lanes' maxima (the upper 16 bits of it) is a bound that k elements at least reach, and
@@ -14,12 +14,12 @@
 // lanes - the k best are taken out one by one.  At the end one wave takes the lists together, drops what is below such a bound of all, and ranks the rest
 // by counting (every wave its own list first, in order: 174 us for 8192 rows of 32768 bf16 and k = 32, this 147).
 //
-// Bound by memory: forward one read, backward one read and one write, the forward one nearly as much by its 40 or so cycles per element and lane (exp2 takes
-// four slots of ten).  The last 256 MB of logits, what the large cache holds, are read so that they stay there, and the backward call goes backwards and
-// finds them; all else is read, and the gradient written, past the caches.  8192 rows of 32768 bf16: forward 95 us without alternatives (5.7 TB/s),
-// 121 with 8, 147 with 32; forward with 8 and backward 310, with every access an ordinary one, forwards, 338.  4096 rows of fp32: 95 and 277, so 321.
-// Few rows are cut into segments, a block each, and joined by a second launch (4 rows of 32768 fp32, 20 alternatives: 10.6 us; as one block of 1024
-// threads 15.6); a call of one launch is bound by latency (1 x 4000: 6.3 us).
+// Bound by memory: forward one read, backward one read and one write, the forward one nearly as much by its 40 or so cycles per element and lane
+// (exp2 takes four slots of ten).  The last 256 MB of logits, what the large cache holds, are read so that they stay there, and the backward call
+// goes backwards and finds them; all else is read, and the gradient written, past the caches.  8192 rows of 32768 bf16: forward 95 us without
+// alternatives (5.7 TB/s), 121 with 8, 147 with 32; forward with 8 and backward 310, with every access an ordinary one, forwards, 338.  4096 rows of
+// fp32: 95 and 277, so 321. Few rows are cut into segments, a block each, and joined by a second launch (4 rows of 32768 fp32, 20 alternatives: 10.6
+// us; as one block of 1024 threads 12.2); a call of one launch is bound by latency (1 x 4000: 6.3 us).
 #include <type_traits>
 
 #include "common.hpp"
@@ -80,8 +80,8 @@ template <bool KEEP, class T> __device__ __forceinline__ u32x4 load_vec(const T*
 // The larger; NaN where there is one.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// Rows whose maximum is further from 0 are read again, with z - max formed first: up to 2^22 the rounding of max k shifts d by 1/4 at most, beyond it the sums
-// would lose their bits and overflow.
+// Rows whose maximum is further from 0 are read again, with z - max formed first: up to 2^22 the rounding of max k shifts d by 1/4 at most, beyond it
+// the sums would lose their bits and overflow.
 __device__ __forceinline__ float safe_bound(float k) { return fminf(4194304.f / k, 1e38f); }
 
 // Order of values and, among equals, of indices from the lowest on, as integers.
@@ -552,18 +552,23 @@ static int64_t kept_from(const LogprobArgs& a) {
   const int64_t rows = (256LL << 20) / (a.vocab * (a.dtype == kBF16 ? 2 : 4));
   return rows < a.rows ? a.rows - rows : 0;
 }
-// How many segments rows are cut into: where there are too few rows for the chip, as many as keep 4096 elements each.
-// In us, cut and as one block of 1024 threads: 1 x 16384 bf16 11.7 and 13.4, 1 x 131072 11.9 and 25.5, 256 x 32768 15.4 and 14.5, 256 x 131072 29.8 and 28.2, 300 x
-// 32768 19.7 and 26.4, 511 x 32768 20.2 and 26.9; 600 rows are enough uncut (19.9).
-static int segments_of(int64_t rows, int64_t vocab) {
-  if (rows >= 512 || vocab < 8192) return 1;
-  int64_t n = 1024 / (rows < 1 ? 1 : rows);
+// How many segments rows are cut into: where there are too few for the chip and a row is more than 64 KB, as many as keep 4096 elements each, a block of 256 threads to one.
+// Up to two blocks of 512 threads to a unit, whole rows of more than 16 KB are one block's of 512 threads, else of 256, of 64 up to 2048 elements.  In us, 20 alternatives:
+//                      cut   512   256 threads                            cut   512   256 threads
+//   4 x 32768 bf16    11.4  10.3                   64 x 131072 bf16      14.3  24.9
+//   4 x 32768 fp32    10.9  12.2                   256 x 131072 bf16     27.8  26.7
+//   4 x 131072 fp32   11.2  29.3                   511 x 131072 bf16     40.7  36.7
+//   4 x 16384 bf16    11.4   7.9                   511 x 32768 bf16      18.5  14.3
+//   4 x 4000 fp32            6.8   6.0             511 x 5000 bf16             10.2   7.7        (600 x 32768 with 256: 19.9)
+static int segments_of(int64_t rows, int64_t vocab, int bytes) {
+  if (rows < 1 || rows >= 256 || vocab * bytes <= 65536) return 1;
+  int64_t n = 1024 / rows;
   if (n > vocab / 4096) n = vocab / 4096;
   return (int)(n < kSegments ? n : kSegments);
 }
 int64_t logprob_ws_floats(int64_t rows, int64_t vocab, int k) {
   if (rows < 0 || rows > (1LL << 31) - 1 || vocab < 1 || vocab > (1LL << 28) || k < 0 || k > kMaxTop) return -1;
-  const int n = segments_of(rows, vocab);
+  const int n = segments_of(rows, vocab, 4);             // of either type: bf16 rows are cut in as many or not at all
   return n > 1 ? rows * n * (4 + 2 * k) : 0;
 }
 
@@ -575,7 +580,7 @@ hipError_t launch_logprob_fwd(hipStream_t s, const LogprobArgs& a, float* logp, 
   if (((uintptr_t)logp | (uintptr_t)entropy | (uintptr_t)top_id | (uintptr_t)top_logp) & 3 || (uintptr_t)stats & 7) return hipErrorInvalidValue;
   if (logprob_ws_floats(a.rows, a.vocab, k) > 0 && (!ws || ((uintptr_t)ws & 7))) return hipErrorInvalidValue;
   if (a.rows == 0) return hipSuccess;
-  const int n = segments_of(a.rows, a.vocab);
+  const int bytes = a.dtype == kBF16 ? 2 : 4, n = segments_of(a.rows, a.vocab, bytes);
   const LogprobFwdParams p{a.z, a.ldz, a.rows, a.vocab, a.targets, a.scale, a.scale * kLog2e, logp, entropy, stats, k, top_id, top_logp, n,
                            (a.vocab + n - 1) / n, ws, kept_from(a)};
   auto run = [&](auto t, auto with_top) {
@@ -583,6 +588,7 @@ hipError_t launch_logprob_fwd(hipStream_t s, const LogprobArgs& a, float* logp, 
     constexpr bool TOP = decltype(with_top)::value;
     const unsigned blocks = (unsigned)(a.rows * n);
     if (a.vocab <= 2048) logprob_fwd_kernel<T, 64, 4, TOP><<<blocks, 64, 0, s>>>(p);
+    else if (n == 1 && a.rows <= 512 && a.vocab * bytes > 16384) logprob_fwd_kernel<T, 512, 4, TOP><<<blocks, 512, 0, s>>>(p);
     else logprob_fwd_kernel<T, 256, 4, TOP><<<blocks, 256, 0, s>>>(p);
     if (n > 1) logprob_join_kernel<T><<<(unsigned)a.rows, kJoin, 0, s>>>(p);
   };

@@ -23,10 +23,10 @@ typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));        // 
 typedef unsigned short u16x4u __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
 
-// Columns c .. c + 3 of a row of d: four elements as they are stored, asked for without a question, from the row's last four columns where those wanted are
-// not all there, and put in their place, zeros behind the row, when they are used: a branch at each load makes it wait for the one before (8192 x 1000
-// backward 48 us, this 29; forward 21 and 25, of 2001 columns 24.7 and 21.6).  ONCE: nothing reads them again, and they leave the caches to what is written.
-// Rows that are a team's vectors exactly need none of it; rows of fewer than four columns are one lane's.
+// Columns c .. c + 3 of a row of d: four elements as they are stored, asked for without a question, from the row's last four columns where those
+// wanted are not all there, and put in their place, zeros behind the row, when they are used: a branch at each load makes it wait for the one before
+// (8192 x 1000 backward 48 us, this 29; forward 21 and 25, of 2001 columns 24.7 and 21.6).  ONCE: nothing reads them again, and they leave the caches
+// to what is written. Rows that are a team's vectors exactly need none of it; rows of fewer than four columns are one lane's.
 enum Edge { kWhole, kAny, kTiny };
 __device__ __forceinline__ int last4(int c, int d) { return c + 4 <= d ? c : d - 4; }
 template <class T, Edge EDGE> struct Stored;
