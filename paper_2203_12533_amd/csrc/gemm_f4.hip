@@ -785,9 +785,9 @@ hipError_t launch_direct(hipStream_t s, GemmF4Params p, bool f32) {
 }
 // Which shape: the largest whose tiles give every compute unit one, as a launch of up to one round takes as long as one tile.  Measured in us on both
 // sides of each step (k = 2048 unless it says so, bf16):
-//   few rows and columns straight from memory up to 512 blocks of 16 x 16 (1 x 8192 3.8 against 4.4 as tiles of 32 x 64, 16 x 8192 4.5 and 4.5;
-//     beyond, 1 x 16384 5.0 and 4.5, 3 x 32768 9.1 and 8.0); eight waves share a long k (16 x 4096 x 8192 7.2, four 7.7), four where it is short
-//     (3 x 32768 9.1, eight 11.6);
+//   few rows and columns straight from memory, up to 512 blocks of 16 x 16 (1 x 8192 3.8, as tiles of 32 x 64 4.4, 16 x 8192 4.5 and 4.5; beyond, 1 x 16384
+//     5.0 and 4.5, 3 x 32768 9.1 and 8.0), up to 256 if k is long (16 x 4096 x 4096 4.5 and 5.2, x 8192 7.2 and 6.8; beyond, 16 x 8192 x 4096 6.6 and 5.2,
+//     128 x 1024 x 16384 19.8 and 10.0); eight waves share a long k (16 x 4096 x 8192 7.2, four 7.7), four a short one (3 x 32768 9.1, eight 11.6);
 //   32 x 64 up to 256 tiles (256 x 2048 4.6, as 64 x 64 5.6; 1024 x 1024 7.6 and 5.8), 64 x 64 up to 256 (1024 x 1024 5.8, as 128 x 64 6.8; 1024 x 2048
 //     10.0 and 7.2), 128 x 64 up to 256 (1024 x 2048 7.2, as 128 x 128 8.5; 2048 x 2048 10.5 and 9.3);
 //   128 x 128 is there twice on a unit, so up to 128 tiles of 256 x 256 it needs one round (2816 x 2816, 121 of them, 14.7, as 256 x 256 19.3; 2816 x 3000,
@@ -797,7 +797,8 @@ hipError_t launch_direct(hipStream_t s, GemmF4Params p, bool f32) {
 //     131072 x 100, whose rows of C do not end with a tile, 39.6 and 46.9), and of 128 x 128 (131072 x 60 45.3, as 128 x 64 35.1).
 hipError_t choose(hipStream_t s, const GemmF4Params& p, bool f32) {
   auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
-  if (tiles(16, 16) <= 512 || p.lda > kMaxLd || p.ldb > kMaxLd) return p.K >= 4096 ? launch_direct<8>(s, p, f32) : launch_direct<4>(s, p, f32);
+  const bool deep = p.K >= 4096;
+  if (tiles(16, 16) <= (deep ? 256 : 512) || p.lda > kMaxLd || p.ldb > kMaxLd) return deep ? launch_direct<8>(s, p, f32) : launch_direct<4>(s, p, f32);
   if (tiles(Few::BM, Few::BN) <= 256) return launch<Few>(s, p, f32);
   if (tiles(Split::BM, Split::BN) <= 256) return launch<Split>(s, p, f32);
   if (tiles(Half::BM, Half::BN) <= 256 || p.N <= Half::BN) return launch<Half>(s, p, f32);

@@ -581,16 +581,22 @@ hipError_t launch_logprob_fwd(hipStream_t s, const LogprobArgs& a, float* logp, 
   if (logprob_ws_floats(a.rows, a.vocab, k) > 0 && (!ws || ((uintptr_t)ws & 7))) return hipErrorInvalidValue;
   if (a.rows == 0) return hipSuccess;
   const int bytes = a.dtype == kBF16 ? 2 : 4, n = segments_of(a.rows, a.vocab, bytes);
-  const LogprobFwdParams p{a.z, a.ldz, a.rows, a.vocab, a.targets, a.scale, a.scale * kLog2e, logp, entropy, stats, k, top_id, top_logp, n,
-                           (a.vocab + n - 1) / n, ws, kept_from(a)};
   auto run = [&](auto t, auto with_top) {
     using T = decltype(t);
     constexpr bool TOP = decltype(with_top)::value;
-    const unsigned blocks = (unsigned)(a.rows * n);
-    if (a.vocab <= 2048) logprob_fwd_kernel<T, 64, 4, TOP><<<blocks, 64, 0, s>>>(p);
-    else if (n == 1 && a.rows <= 512 && a.vocab * bytes > 16384) logprob_fwd_kernel<T, 512, 4, TOP><<<blocks, 512, 0, s>>>(p);
-    else logprob_fwd_kernel<T, 256, 4, TOP><<<blocks, 256, 0, s>>>(p);
-    if (n > 1) logprob_join_kernel<T><<<(unsigned)a.rows, kJoin, 0, s>>>(p);
+    const int64_t most = 1LL << 22;                        // rows of a launch, which takes less than 2^32 threads
+    for (int64_t r = 0; r < a.rows; r += most) {
+      auto from = [&](auto* p, int64_t per) { return p ? p + r * per : nullptr; };
+      const int64_t rows = a.rows - r < most ? a.rows - r : most;
+      const LogprobFwdParams p{reinterpret_cast<const T*>(a.z) + r * a.ldz, a.ldz, rows, a.vocab, from(a.targets, 1), a.scale, a.scale * kLog2e,
+                               from(logp, 1), from(entropy, 1), from(stats, 2), k, from(top_id, k), from(top_logp, k), n, (a.vocab + n - 1) / n, ws,
+                               kept_from(a) - r};
+      const unsigned blocks = (unsigned)(rows * n);
+      if (a.vocab <= 2048) logprob_fwd_kernel<T, 64, 4, TOP><<<blocks, 64, 0, s>>>(p);
+      else if (n == 1 && a.rows <= 512 && a.vocab * bytes > 16384) logprob_fwd_kernel<T, 512, 4, TOP><<<blocks, 512, 0, s>>>(p);
+      else logprob_fwd_kernel<T, 256, 4, TOP><<<blocks, 256, 0, s>>>(p);
+      if (n > 1) logprob_join_kernel<T><<<(unsigned)rows, kJoin, 0, s>>>(p);
+    }
   };
   auto type = [&](auto t) {
     if (k > 0) run(t, std::true_type{});

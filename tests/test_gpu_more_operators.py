@@ -563,6 +563,32 @@ def test_log_probabilities_of_many_rows(ctx, rows, vocab, k, bf16):
     logprob(ctx, 2 * rnd(rows, rows, vocab), np.random.RandomState(2).randint(-1, vocab, rows), 1.0, k, bf16)
 
 
+def test_log_probabilities_of_more_rows_than_a_launch_has_threads_for(ctx):
+    rows, vocab = (1 << 26) + 5, 3
+    z = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1, (1 << 22) - 1, 1 << 22, (1 << 22) + 1, 1 << 25, (1 << 26) - 1, 1 << 26, rows - 1], device="cuda")
+    z[at] = torch.arange(at.numel() * vocab, device="cuda").reshape(-1, vocab).remainder(7).to(torch.bfloat16)
+    t = torch.ones(rows, dtype=torch.int32, device="cuda")
+    lp, en, st = (torch.full((rows, n), 7.0, device="cuda") for n in (1, 1, 2))
+    ids, tl = torch.zeros(rows, 1, dtype=torch.int32, device="cuda"), torch.zeros(rows, 1, device="cuda")
+    torch.cuda.synchronize()
+    a = pwb.LogprobArgs(dtype=pwb.PW_BF16, z=p(z), ldz=vocab, rows=rows, vocab=vocab, targets=p(t), scale=1.0)
+    ctx.logprob_fwd(a, p(lp), p(en), p(st), 1, p(ids), p(tl), None)
+    ctx.logprob_bwd(a, p(st), p(en), p(st), None, p(z), vocab)             # dlogp: any array of that length
+    ctx.synchronize()
+    v = np.arange(at.numel() * vocab).reshape(-1, vocab) % 7
+    rlp, rh, rid, rtl = M.logprob_fwd(v.astype(np.float64), np.ones(at.numel(), np.int64), 1.0, 1)
+    elp, eh, _, _ = logp_bounds(v.astype(np.float64), 1.0)
+    within(back(lp[at])[:, 0], rlp, elp[:, 1], "logp", U)
+    within(back(en[at])[:, 0], rh, eh, "entropy", U)
+    assert np.array_equal(ids[at].cpu().numpy(), rid)
+    within(back(tl[at]), rtl, np.take_along_axis(elp, rid, 1), "top", U)
+    zeros = torch.ones(rows, dtype=torch.bool, device="cuda")
+    zeros[at] = False
+    assert torch.isclose(lp[zeros], torch.tensor(-np.log(3.0), dtype=torch.float32, device="cuda"), rtol=1e-5).all()
+    assert (ids[zeros] == 0).all() and (st[zeros, 0] == 0).all()
+
+
 @pytest.mark.parametrize("parts", ["logp", "entropy"])
 def test_log_probabilities_with_one_gradient_only(ctx, parts):
     logprob(ctx, 2 * rnd(3, 7, 700), np.arange(7) * 90, 1.3, 0, True, parts=parts)
