@@ -12,7 +12,8 @@
 // those of the rows l, l + 16, l + 32, l + 48, and the 64 words of 64 rows and four blocks are neighbours.
 //
 // Bound by memory: a block of 256 threads takes 128 x 128 elements, 8 x 8 to a thread.  A wave has 32 rows of the tile, which is the
-// block length, so that the maxima of both orientations are four exchanges between lanes and meet nowhere else.
+// block length, so that the maxima of both orientations are four exchanges between lanes and meet nowhere else.  8192 x 2048 bf16 into both 11.1 us
+// (4.6 TB/s), 333 x 500 fp32 4.0, a launch.
 #include <type_traits>
 
 #include "common.hpp"

@@ -378,7 +378,7 @@ def test_rms_norm_of_any_width(ctx, cols, bf16):
 
 @pytest.mark.parametrize("rows,cols,kw", [(1, 2048, {}), (6000, 64, {}), (9000, 48, {"x_out": "same"}), (300, 2048, {"h": False}),
                                           (70, 640, {"h": False, "y": False, "x_out": None}), (5000, 1000, {"x_out": "same", "eps": 0.0}),
-                                          (2100, 4100, {"y": False})])
+                                          (2100, 4100, {"y": False}), (3000, 1999, {"x_out": "same"}), (600, 1999, {"x_out": "same"})])
 @pytest.mark.parametrize("bf16", [False, True])
 def test_rms_norm_of_many_rows(ctx, rows, cols, kw, bf16):
     rms_forward(ctx, rows, cols, bf16, fmt="e4m3", seed=3, **kw)
@@ -443,7 +443,8 @@ def test_rms_norm_gradients_of_any_width(ctx, cols, bf16):
 
 
 @pytest.mark.parametrize("rows,cols,kw", [(9000, 64, {}), (3000, 500, {"dres": "same"}), (2500, 2048, {"dy": False}), (2500, 1000, {"dg": False}),
-                                          (700, 5000, {"accumulate": 1}), (3, 2048, {"accumulate": 1, "dres": None}), (4, 2048, {}), (5, 2048, {})])
+                                          (700, 5000, {"accumulate": 1}), (3, 2048, {"accumulate": 1, "dres": None}), (4, 2048, {}), (5, 2048, {}),
+                                          (3000, 1999, {"dres": "same"}), (2500, 301, {"dres": "same"}), (300, 9001, {"dres": "same"})])
 @pytest.mark.parametrize("bf16", [False, True])
 def test_rms_norm_gradients_of_many_rows(ctx, rows, cols, kw, bf16):
     rms_backward(ctx, rows, cols, bf16, seed=1, **kw)
