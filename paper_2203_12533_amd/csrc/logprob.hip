@@ -17,8 +17,8 @@
 // Bound by memory: forward one read, backward one read and one write, the forward one nearly as much by its 40 or so cycles per element and lane
 // (exp2 takes four slots of ten).  The last 256 MB of logits, what the large cache holds, are read so that they stay there, and the backward call
 // goes backwards and finds them; all else is read, and the gradient written, past the caches.  8192 rows of 32768 bf16: forward 95 us without
-// alternatives (5.7 TB/s), 121 with 8, 147 with 32; forward with 8 and backward 310, with every access an ordinary one, forwards, 338.  4096 rows of
-// fp32: 95 and 277, so 321. Few rows are cut into segments, a block each, and joined by a second launch (4 rows of 32768 fp32, 20 alternatives: 10.6
+// alternatives (5.7 TB/s), 121 with 8, 147 with 32; forward with 8 and backward 280, with every access an ordinary one, forwards, 338.  4096 rows of
+// fp32: 94 and 253, so 321. Few rows are cut into segments, a block each, and joined by a second launch (4 rows of 32768 fp32, 20 alternatives: 10.6
 // us; as one block of 1024 threads 12.2); a call of one launch is bound by latency (1 x 4000: 6.3 us).
 #include <type_traits>
 
@@ -469,9 +469,11 @@ struct LogprobBwdParams {
   const float *stats, *entropy, *dlogp, *dentropy;
   int64_t kept;                // rows from this one on may be in a cache
 };
+// A block takes one part of a row after the other, four of them where there are many: 8192 x 32768 bf16 157 us behind the forward pass, a block to each part
+// 190, 4096 rows of fp32 159 and 181; eight waves to a SIMD by holding registers down (fp32 with five 190 in parts).
 constexpr int kBwdThreads = 256, kBwdVecs = 4;
 template <class T>
-__global__ __launch_bounds__(kBwdThreads) void logprob_bwd_kernel(LogprobBwdParams p) {
+__global__ __launch_bounds__(kBwdThreads, 8) void logprob_bwd_kernel(LogprobBwdParams p) {
   constexpr int E = Vec<T>::E, U = kBwdVecs;
   constexpr int64_t kSeg = (int64_t)kBwdThreads * U * E;
   const float k = p.k, bound = safe_bound(k);
@@ -615,7 +617,7 @@ hipError_t launch_logprob_bwd(hipStream_t s, const LogprobArgs& a, const float* 
   if (a.rows == 0) return hipSuccess;
   const int64_t seg = (int64_t)kBwdThreads * kBwdVecs * (a.dtype == kBF16 ? 8 : 4), segments = (a.vocab + seg - 1) / seg;
   const LogprobBwdParams p{a.z, dz, a.ldz, lddz, a.rows, a.vocab, segments, a.targets, a.scale, a.scale * kLog2e, stats, entropy, dlogp, dentropy, kept_from(a)};
-  const int64_t blocks = a.rows * segments, most = 1 << 20;
+  const int64_t blocks = a.rows * segments, most = 4 * 2048;            // 2048 are on the chip at a time
   const unsigned grid = (unsigned)(blocks < most ? blocks : most);
   if (a.dtype == kF32) logprob_bwd_kernel<float><<<grid, kBwdThreads, 0, s>>>(p);
   else logprob_bwd_kernel<bf16><<<grid, kBwdThreads, 0, s>>>(p);
