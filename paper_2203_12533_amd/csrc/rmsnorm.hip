@@ -339,8 +339,11 @@ __global__ __launch_bounds__(NT) void rmsnorm_bwd_kernel(RmsBwdParams p) {
   }
 }
 constexpr int kBwdTeams = 512;
-// Rows that a team takes at a time: what its registers hold twice over.
-template <int NT, int VEC> constexpr int kBwdRows = VEC <= 2 ? 4 : NT == 256 ? 2 : 1;
+// Rows that a team takes at a time: what its registers hold twice over, with two waves to a SIMD; fewer where rows do not fill the vectors, which takes registers
+// too (us with 4 or 2 rows and with 2 or 1: 3000 x 2001 bf16 28.4 and 25.2, 8192 x 1500 53.4 and 44.8, 3000 x 2500 42.5 and 33.3; 8192 x 2048, whole, 50.3 with
+// 4 and 51.5 with 2).
+template <int NT, int VEC, Edge EDGE> constexpr int kBwdRows =
+    NT != 256 ? (VEC <= 2 ? 4 : 1) : EDGE == kWhole || VEC == 1 ? (VEC <= 2 ? 4 : 2) : VEC == 2 ? 2 : 1;
 // Threads to a row, vectors to a thread: registers are shared among more threads than in the forward pass, which holds less of a row.
 template <class F> void by_width_bwd(int64_t d, F&& f) {
   using std::integral_constant;
@@ -354,7 +357,10 @@ template <class F> void by_width_bwd(int64_t d, F&& f) {
 }
 int bwd_rows(int64_t d) {
   int rows = 0;
-  by_width_bwd(d, [&](auto nt, auto vec) { rows = kBwdRows<decltype(nt)::value, decltype(vec)::value>; });
+  by_width_bwd(d, [&](auto nt, auto vec) {
+    constexpr int NT = decltype(nt)::value, VEC = decltype(vec)::value;
+    by_edge<NT, VEC>(d, [&](auto edge) { rows = kBwdRows<NT, VEC, decltype(edge)::value>; });
+  });
   return rows;
 }
 int64_t bwd_teams(int64_t rows, int64_t d) {
@@ -425,7 +431,7 @@ hipError_t launch_rmsnorm_bwd(hipStream_t s, const RmsnormArgs& a, const void* d
     by_width_bwd(a.cols, [&](auto nt, auto vec) {
       constexpr int NT = decltype(nt)::value, VEC = decltype(vec)::value;
       by_edge<NT, VEC>(a.cols, [&](auto edge) {
-        rmsnorm_bwd_kernel<decltype(t), NT, VEC, kBwdRows<NT, VEC>, decltype(edge)::value><<<(unsigned)teams, NT, 0, s>>>(p);
+        rmsnorm_bwd_kernel<decltype(t), NT, VEC, kBwdRows<NT, VEC, decltype(edge)::value>, decltype(edge)::value><<<(unsigned)teams, NT, 0, s>>>(p);
       });
     });
   };
