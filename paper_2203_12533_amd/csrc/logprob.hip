@@ -12,14 +12,15 @@
 // usually few more do.  Those go to the list as keys of value and index, 64 bits, no two alike, placed by a ballot; what comes later in the row adds
 // what reaches the bound.  A list that is full gets a tighter bound, and where that does not help - values that fall into few
 // lanes - the k best are taken out one by one.  At the end one wave takes the lists together, drops what is below such a bound of all, and ranks the rest
-// by counting (every wave its own list first, in order: 174 us for 8192 rows of 32768 bf16 and k = 32, this 147).
+// by counting (every wave its own list first, in order: 174 us for 8192 rows of 32768 bf16 and k = 32, this then 147).
 //
 // Bound by memory: forward one read, backward one read and one write, the forward one nearly as much by its 40 or so cycles per element and lane
-// (exp2 takes four slots of ten).  The last 256 MB of logits, what the large cache holds, are read so that they stay there, and the backward call
-// goes backwards and finds them; all else is read, and the gradient written, past the caches.  8192 rows of 32768 bf16: forward 95 us without
-// alternatives (5.7 TB/s), 121 with 8, 147 with 32; forward with 8 and backward 280, with every access an ordinary one, forwards, 338.  4096 rows of
-// fp32: 94 and 253, so 321. Few rows are cut into segments, a block each, and joined by a second launch (4 rows of 32768 fp32, 20 alternatives: 10.6
-// us; as one block of 1024 threads 12.2); a call of one launch is bound by latency (1 x 4000: 6.3 us).
+// (exp2 takes four slots of ten); vectors that lie behind the row as a whole are left out (8192 x 9000 bf16, 8 alternatives, 74 us with them, 55
+// without).  The last 256 MB of logits, what the large cache holds, are read so that they stay there, and the backward call goes backwards and finds
+// them; all else is read, and the gradient written, past the caches.  8192 rows of 32768 bf16: forward 93 us without alternatives (5.8 TB/s), 111
+// with 8, 128 with 32; forward with 8 and backward 266, with every access an ordinary one, forwards, 338.  4096 rows of fp32: 93 and 253, so 321.
+// Few rows are cut into segments, a block each, and joined by a second launch (4 rows of 32768 fp32, 20 alternatives: 10.7 us; as one block of 1024
+// threads 12.2); a call of one launch is bound by latency (1 x 4000: 5.1 us).
 #include <type_traits>
 
 #include "common.hpp"
@@ -237,10 +238,11 @@ template <int M> __device__ __forceinline__ int shortlist(const uint64_t (&key)[
   return n;
 }
 
-// NT threads of a block, U vectors of 16 bytes to one in a chunk; a wave's list has kPlaces places, and kMaxTop more for a k best of a chunk.
+// NT threads of a block, U vectors of 16 bytes to one in a chunk; a wave's list has kPlaces places, and kMaxTop more for a k best of a chunk.  Six blocks of 256
+// to a unit, two registers spilled for it (8192 x 32768 bf16, 8 alternatives, 103 us; five 106).
 constexpr int kPlaces = 256;
 template <class T, int NT, int U, bool TOP>
-__global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) {
+__global__ __launch_bounds__(NT, NT == 256 ? 6 : 4) void logprob_fwd_kernel(LogprobFwdParams p) {
   constexpr int E = Vec<T>::E, kWaves = NT / 64;
   constexpr uint32_t kChunk = NT * U * E;
   __shared__ Soft wave_soft[2][kWaves];
@@ -353,7 +355,8 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
     mine = rebase(mine, fmaxf(mine.m, chunk_max), bound, k);
     const float mk = shift_of(mine.m, bound, k);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      if (u > 0 && c0 + u * NT * E >= V) break;          // uniform: the row's last chunk
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float d = larger(__builtin_fmaf(Vec<T>::get(v[u], e), k, -mk), kFloor), x = __builtin_amdgcn_exp2f(d);
@@ -361,6 +364,7 @@ __global__ __launch_bounds__(NT, 4) void logprob_fwd_kernel(LogprobFwdParams p) 
         mine.t = __builtin_fmaf(x, d, mine.t);
         if (e == E - 1) __builtin_amdgcn_sched_barrier(0);
       }
+    }
     if constexpr (TOP) {                                 // uniform over the wave
       thr = fmaxf(thr, bound_of(mine.m));
       const int before = n;
@@ -555,7 +559,8 @@ static int64_t kept_from(const LogprobArgs& a) {
   return rows < a.rows ? a.rows - rows : 0;
 }
 // How many segments rows are cut into: where there are too few for the chip and a row is more than 64 KB, as many as keep 4096 elements each, a block of 256 threads to one.
-// Up to two blocks of 512 threads to a unit, whole rows of more than 16 KB are one block's of 512 threads, else of 256, of 64 up to 2048 elements.  In us, 20 alternatives:
+// Up to two blocks of 512 threads to a unit, whole rows of more than 16 KB are one block's of 512 threads, else of 256, of 64 up to 2048 elements, and a thread's vectors in a chunk
+// are no more than the row needs (8192 x 4000 bf16, 4 alternatives, 47 with four, 29 with two; 8192 x 100 15.5 with four, 10.0 with one).  In us, 20 alternatives:
 //                      cut   512   256 threads                            cut   512   256 threads
 //   4 x 32768 bf16    11.4  10.3                   64 x 131072 bf16      14.3  24.9
 //   4 x 32768 fp32    10.9  12.2                   256 x 131072 bf16     27.8  26.7
@@ -594,8 +599,12 @@ hipError_t launch_logprob_fwd(hipStream_t s, const LogprobArgs& a, float* logp, 
                                from(logp, 1), from(entropy, 1), from(stats, 2), k, from(top_id, k), from(top_logp, k), n, (a.vocab + n - 1) / n, ws,
                                kept_from(a) - r};
       const unsigned blocks = (unsigned)(rows * n);
-      if (a.vocab <= 2048) logprob_fwd_kernel<T, 64, 4, TOP><<<blocks, 64, 0, s>>>(p);
+      constexpr int E = Vec<T>::E;
+      if (a.vocab <= 64 * E) logprob_fwd_kernel<T, 64, 1, TOP><<<blocks, 64, 0, s>>>(p);
+      else if (a.vocab <= 128 * E) logprob_fwd_kernel<T, 64, 2, TOP><<<blocks, 64, 0, s>>>(p);
+      else if (a.vocab <= 2048) logprob_fwd_kernel<T, 64, 4, TOP><<<blocks, 64, 0, s>>>(p);
       else if (n == 1 && a.rows <= 512 && a.vocab * bytes > 16384) logprob_fwd_kernel<T, 512, 4, TOP><<<blocks, 512, 0, s>>>(p);
+      else if (a.vocab <= 512 * E) logprob_fwd_kernel<T, 256, 2, TOP><<<blocks, 256, 0, s>>>(p);
       else logprob_fwd_kernel<T, 256, 4, TOP><<<blocks, 256, 0, s>>>(p);
       if (n > 1) logprob_join_kernel<T><<<(unsigned)rows, kJoin, 0, s>>>(p);
     }
