@@ -559,6 +559,15 @@ def test_log_probabilities_of_any_vocabulary(ctx, vocab, bf16):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("vocab", [256, 257, 512, 513, 1024, 1025, 2048, 2049, 4096, 4097, 16385, 32769])
+def test_log_probabilities_where_one_kernel_takes_over_from_another(ctx, vocab, bf16):
+    z = 3 * rnd(vocab, 3, vocab)
+    z[1, 0], z[2, vocab - 1] = 40.0, 40.0                     # the likeliest is the first, the last
+    logprob(ctx, z, [0, vocab - 1, vocab // 2], 1.0, 9, bf16, seed=vocab)
+    logprob(ctx, np.tile(z, (200, 1))[:520], np.arange(520) % vocab, 1.0, 3, bf16, seed=vocab)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("rows,vocab,k", [(300, 500, 4), (600, 9000, 32), (300, 40000, 20), (257, 8200, 0), (1000, 61, 32)])
 def test_log_probabilities_of_many_rows(ctx, rows, vocab, k, bf16):
     logprob(ctx, 2 * rnd(rows, rows, vocab), np.random.RandomState(2).randint(-1, vocab, rows), 1.0, k, bf16)
