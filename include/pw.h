@@ -742,7 +742,8 @@ int64_t pw_rmsnorm_bwd_ws_floats(int64_t rows, int64_t cols);   /* -1 for imposs
  * Of rows of logits z, times a scale s (1 / temperature): p = softmax(s z), the log probability of one given token per row, the entropy
  * H = -sum p log p and the k likeliest tokens; and the gradient of the logits from gradients of the first two.  A logit of -infinity is a
  * token that cannot occur: p = 0, and it adds nothing to H.  A row of them only has no distribution: its logp is -infinity, H is 0, it has no alternatives
- * and no gradient.  A row that holds a NaN or +infinity has none either: its logp, H, top_logp and gradients are NaN, its top_id -1. */
+ * and no gradient.  A row that holds a NaN or +infinity has none either: its logp, H, top_logp and gradients are NaN, its top_id -1.
+ * No log probability is above 0 and no H below it, however they round. */
 typedef struct {
   int32_t dtype;             /* of z and dz: PW_F32 or PW_BF16 */
   const void* z;

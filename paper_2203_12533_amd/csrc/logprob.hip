@@ -4,7 +4,8 @@
 //   dz_v = s [dlogp ([v = t] - p_v) - dentropy p_v (log p_v + H)],  p_v = e^(d_v - log S)
 //
 // In base 2: d = z k - max k with k = s log2 e, one fused multiply-add, whose product is exact; that max k is rounded shifts all of a row alike, by
-// an amount that is known and taken off log S.  Every thread keeps a running maximum, S and sum of its own; they meet once per row.  Sums are fp32,
+// an amount of at most 1/4 that is known and taken off log S (in H it cancels).  What rounding then leaves of log S and H below 0 becomes 0, so that no
+// probability is above 1.  Every thread keeps a running maximum, S and sum of its own; they meet once per row.  Sums are fp32,
 // of at most vocab / threads terms before they meet in a tree.
 //
 // Alternatives.  Every wave keeps a list in LDS of what can be among the k best of its columns, without a word to the others: with a part of the row in
@@ -182,11 +183,12 @@ __device__ __forceinline__ void finish_row(const LogprobFwdParams& p, int64_t ro
   const bool none = all.m == -INFINITY && all.s == 0.f;  // (a NaN beside makes S one)
   const float nan = __builtin_nanf("");
   if (all.m == INFINITY || (all.m == -INFINITY && !none)) all.s = nan;
-  const float log2s = __builtin_amdgcn_logf(all.s), lse = (log2s - (extreme ? 0.f : shift_error(all.m, bound, k))) * kLn2;
-  auto log_p = [&](float x) { return none ? -INFINITY : (x - all.m) * p.scale - lse; };    // only what is out of range itself overflows
+  // S has a term of 1, so that log S >= 0 (and H); larger() keeps a NaN.
+  const float log2s = __builtin_amdgcn_logf(all.s), lse = larger((log2s - (extreme ? 0.f : shift_error(all.m, bound, k))) * kLn2, 0.f);
+  auto log_p = [&](float x) { return none ? -INFINITY : __builtin_fmaf(x - all.m, p.scale, -lse); };    // only what is out of range itself overflows
   if (t == 0) {
     if (p.logp) p.logp[row] = given.is ? log_p(given.z) : 0.f;
-    if (p.entropy) p.entropy[row] = none ? 0.f : (log2s - all.t / all.s) * kLn2;
+    if (p.entropy) p.entropy[row] = none ? 0.f : larger((log2s - all.t / all.s) * kLn2, 0.f);
     if (p.stats) *reinterpret_cast<float2*>(p.stats + 2 * row) = make_float2(all.m, none ? 0.f : lse);
   }
   if (top > 0 && wave == 0) {
