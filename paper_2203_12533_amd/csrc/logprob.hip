@@ -5,8 +5,9 @@
 //
 // In base 2: d = z k - max k with k = s log2 e, one fused multiply-add, whose product is exact; that max k is rounded shifts all of a row alike, by
 // an amount of at most 1/4 that is known and taken off log S (in H it cancels).  What rounding then leaves of log S and H below 0 becomes 0, so that no
-// probability is above 1.  Every thread keeps a running maximum, S and sum of its own; they meet once per row.  Sums are fp32,
-// of at most vocab / threads terms before they meet in a tree.
+// probability is above 1.  Every thread keeps a running maximum, S and sum of its own; they meet once per row, in a tree.  A
+// part of a row (32 terms of a thread) is summed in fp32 and joins the running pair in 64 bits: equal terms, as logits in few bits give, round the same way every
+// time, and log S of a chain of 16384 fp32 additions was off by 8e-5.
 //
 // Alternatives.  Every wave keeps a list in LDS of what can be among the k best of its columns, without a word to the others: with a part of the row in
 // registers, the k-th largest of its 64 lanes' maxima (the upper 16 bits of it) is a bound that k elements at least reach, and
@@ -84,7 +85,7 @@ __device__ __forceinline__ float larger(float a, float b) { return __builtin_ele
 
 // Rows whose maximum is further from 0 are read again, with z - max formed first: up to 2^22 the rounding of max k shifts d by 1/4 at most, beyond it
 // the sums would lose their bits and overflow.
-__device__ __forceinline__ float safe_bound(float k) { return fminf(4194304.f / k, 1e38f); }
+float safe_bound(float k) { return fminf(4194304.f / k, 1e38f); }
 
 // Order of values and, among equals, of indices from the lowest on, as integers.
 __device__ __forceinline__ uint64_t key_of(float v, uint32_t index) {
@@ -122,7 +123,7 @@ struct LogprobFwdParams {
   const void* z;
   int64_t ldz, rows, vocab;
   const int32_t* targets;
-  float scale, k;              // k = scale * log2 e
+  float scale, k, bound;       // k = scale * log2 e, bound = safe_bound(k)
   float *logp, *entropy, *stats;
   int top;
   int32_t* top_id;
@@ -142,6 +143,12 @@ __device__ __forceinline__ Soft rebase(const Soft& a, float m, float bound, floa
   const float d = larger(shift_of(a.m, bound, k) - shift_of(m, bound, k), kFloor), f = __builtin_amdgcn_exp2f(d);
   return {m, a.s * f, f * __builtin_fmaf(d, a.s, a.t)};
 }
+// S and sum of a thread over as many parts as there are, against a maximum that moved by d.
+struct Long { double s, t; };
+__device__ __forceinline__ Long rebase(const Long& a, float d) {
+  const double f = __builtin_amdgcn_exp2f(d);
+  return {f * a.s, f * __builtin_fma((double)d, a.s, a.t)};
+}
 
 // The logit of a row's given token, for one thread: asked for before anything else, as one load waits for the other.
 struct Given { bool is; float z; };
@@ -160,17 +167,16 @@ __device__ __forceinline__ void finish_row(const LogprobFwdParams& p, int64_t ro
   constexpr int kWaves = NT / 64;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, top = p.top;
   const T* const z = reinterpret_cast<const T*>(p.z) + row * p.ldz;
-  const float k = p.k, bound = safe_bound(k);
+  const float k = p.k, bound = p.bound;
   const bool extreme = !(fabsf(all.m) <= bound);
   if (extreme && fabsf(all.m) < INFINITY) {              // once more, with z - max first
-    float s = 0.f, st = 0.f;
+    double own = 0.0, own_t = 0.0;
     for (int64_t c = t; c < p.vocab; c += NT) {
       const float d = larger((to_f32(z[c]) - all.m) * k, kFloor), x = __builtin_amdgcn_exp2f(d);
-      s += x;
-      st = __builtin_fmaf(x, d, st);
+      own += x;
+      own_t = __builtin_fma((double)x, (double)d, own_t);
     }
-    s = lanes_sum(s);
-    st = lanes_sum(st);
+    const float s = lanes_sum((float)own), st = lanes_sum((float)own_t);
     if (lane == 0) wave_soft[wave] = Soft{0.f, s, st};
     __syncthreads();
     all.s = all.t = 0.f;
@@ -251,11 +257,13 @@ __global__ __launch_bounds__(NT, NT == 256 ? 6 : 4) void logprob_fwd_kernel(Logp
   __shared__ uint64_t lists[TOP ? kWaves : 1][TOP ? kPlaces + kMaxTop : 1], best_keys[TOP ? kWaves * kMaxTop : 1];
   __shared__ int counts[kWaves];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), top = TOP ? p.top : 0;
-  const int64_t row = p.segments > 1 ? blockIdx.x / p.segments : blockIdx.x;
-  const int seg = p.segments > 1 ? (int)(blockIdx.x - row * p.segments) : 0;
+  // A division's result is in vector registers, which are short here.
+  const uint32_t in_row = __builtin_amdgcn_readfirstlane(p.segments > 1 ? blockIdx.x / (uint32_t)p.segments : blockIdx.x);
+  const int64_t row = in_row;
+  const uint32_t seg = blockIdx.x - in_row * (uint32_t)p.segments;
   const uint32_t from = seg * (uint32_t)p.segment, V = (uint32_t)(from + p.segment < p.vocab ? from + p.segment : p.vocab);   // of this block: from .. V - 1
   const T* const z = reinterpret_cast<const T*>(p.z) + row * p.ldz;
-  const float k = p.k, bound = safe_bound(k);
+  const float k = p.k, bound = p.bound;
   const bool keep = row >= p.kept;
   uint64_t* const list = lists[TOP ? wave : 0];
   Given given = {};
@@ -268,7 +276,8 @@ __global__ __launch_bounds__(NT, NT == 256 ? 6 : 4) void logprob_fwd_kernel(Logp
 #pragma unroll
     for (int u = 0; u < U; ++u) nx[u] = keep ? load_vec<true>(z, c + u * NT * E, V) : load_vec<false>(z, c + u * NT * E, V);
   };
-  Soft mine = {-INFINITY, 0.f, 0.f};
+  Long mine = {0.0, 0.0};
+  float so_far = -INFINITY;                              // the maximum
   float thr = -__FLT_MAX__;                              // finite: -infinity is no alternative
   float vec_max[U], chunk_max;
 
@@ -354,21 +363,24 @@ __global__ __launch_bounds__(NT, NT == 256 ? 6 : 4) void logprob_fwd_kernel(Logp
       chunk_max = fmaxf(chunk_max, vec_max[u]);
       __builtin_amdgcn_sched_barrier(0);
     }
-    mine = rebase(mine, fmaxf(mine.m, chunk_max), bound, k);
-    const float mk = shift_of(mine.m, bound, k);
+    const float most = fmaxf(so_far, chunk_max), mk = shift_of(most, bound, k), change = larger(shift_of(so_far, bound, k) - mk, kFloor);
+    so_far = most;
+    mine = rebase(mine, change);
+    float s = 0.f, st = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (u > 0 && c0 + u * NT * E >= V) break;          // uniform: the row's last chunk
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float d = larger(__builtin_fmaf(Vec<T>::get(v[u], e), k, -mk), kFloor), x = __builtin_amdgcn_exp2f(d);
-        mine.s += x;
-        mine.t = __builtin_fmaf(x, d, mine.t);
+        s += x;
+        st = __builtin_fmaf(x, d, st);
         if (e == E - 1) __builtin_amdgcn_sched_barrier(0);
       }
     }
+    mine = {mine.s + s, mine.t + st};
     if constexpr (TOP) {                                 // uniform over the wave
-      thr = fmaxf(thr, bound_of(mine.m));
+      thr = fmaxf(thr, bound_of(so_far));
       const int before = n;
       push(c0);
       if (n > kPlaces) {
@@ -389,8 +401,8 @@ __global__ __launch_bounds__(NT, NT == 256 ? 6 : 4) void logprob_fwd_kernel(Logp
 
   // All of the segment: within a wave, then between waves.
   {
-    const float m = lanes_max(mine.m);
-    Soft a = rebase(mine, m, bound, k);
+    const float m = lanes_max(so_far);
+    Soft a = rebase(Soft{so_far, (float)mine.s, (float)mine.t}, m, bound, k);
     a.s = lanes_sum(a.s);
     a.t = lanes_sum(a.t);
     if (lane == 0) wave_soft[0][wave] = a;
@@ -444,7 +456,7 @@ __global__ __launch_bounds__(kJoin) void logprob_join_kernel(LogprobFwdParams p)
   const int lane = threadIdx.x, top = p.top;
   const int64_t row = blockIdx.x;
   const float* const in = p.parts + row * p.segments * (4 + 2 * top);
-  const float k = p.k, bound = safe_bound(k);
+  const float k = p.k, bound = p.bound;
   Given given = {};
   if (lane == 0) given = given_of<T>(p, row);
   Soft all = {-INFINITY, 0.f, 0.f};
@@ -471,7 +483,7 @@ struct LogprobBwdParams {
   void* dz;
   int64_t ldz, lddz, rows, vocab, segments;
   const int32_t* targets;
-  float scale, k;
+  float scale, k, bound;
   const float *stats, *entropy, *dlogp, *dentropy;
   int64_t kept;                // rows from this one on may be in a cache
 };
@@ -482,7 +494,7 @@ template <class T>
 __global__ __launch_bounds__(kBwdThreads, 8) void logprob_bwd_kernel(LogprobBwdParams p) {
   constexpr int E = Vec<T>::E, U = kBwdVecs;
   constexpr int64_t kSeg = (int64_t)kBwdThreads * U * E;
-  const float k = p.k, bound = safe_bound(k);
+  const float k = p.k, bound = p.bound;
   // Backwards: the last rows may be in a cache.
   for (int64_t b = p.rows * p.segments - 1 - blockIdx.x; b >= 0; b -= gridDim.x) {
     const int64_t row = b / p.segments, c0 = (b - row * p.segments) * kSeg + (int64_t)threadIdx.x * E, V = p.vocab;
@@ -593,11 +605,12 @@ hipError_t launch_logprob_fwd(hipStream_t s, const LogprobArgs& a, float* logp, 
   auto run = [&](auto t, auto with_top) {
     using T = decltype(t);
     constexpr bool TOP = decltype(with_top)::value;
+    const float k2 = a.scale * kLog2e;
     const int64_t most = 1LL << 22;                        // rows of a launch, which takes less than 2^32 threads
     for (int64_t r = 0; r < a.rows; r += most) {
       auto from = [&](auto* p, int64_t per) { return p ? p + r * per : nullptr; };
       const int64_t rows = a.rows - r < most ? a.rows - r : most;
-      const LogprobFwdParams p{reinterpret_cast<const T*>(a.z) + r * a.ldz, a.ldz, rows, a.vocab, from(a.targets, 1), a.scale, a.scale * kLog2e,
+      const LogprobFwdParams p{reinterpret_cast<const T*>(a.z) + r * a.ldz, a.ldz, rows, a.vocab, from(a.targets, 1), a.scale, k2, safe_bound(k2),
                                from(logp, 1), from(entropy, 1), from(stats, 2), k, from(top_id, k), from(top_logp, k), n, (a.vocab + n - 1) / n, ws,
                                kept_from(a) - r};
       const unsigned blocks = (unsigned)(rows * n);
@@ -627,7 +640,8 @@ hipError_t launch_logprob_bwd(hipStream_t s, const LogprobArgs& a, const float* 
     return hipErrorInvalidValue;
   if (a.rows == 0) return hipSuccess;
   const int64_t seg = (int64_t)kBwdThreads * kBwdVecs * (a.dtype == kBF16 ? 8 : 4), segments = (a.vocab + seg - 1) / seg;
-  const LogprobBwdParams p{a.z, dz, a.ldz, lddz, a.rows, a.vocab, segments, a.targets, a.scale, a.scale * kLog2e, stats, entropy, dlogp, dentropy, kept_from(a)};
+  const float k2 = a.scale * kLog2e;
+  const LogprobBwdParams p{a.z, dz, a.ldz, lddz, a.rows, a.vocab, segments, a.targets, a.scale, k2, safe_bound(k2), stats, entropy, dlogp, dentropy, kept_from(a)};
   const int64_t blocks = a.rows * segments, most = 4 * 2048;            // 2048 are on the chip at a time
   const unsigned grid = (unsigned)(blocks < most ? blocks : most);
   if (a.dtype == kF32) logprob_bwd_kernel<float><<<grid, kBwdThreads, 0, s>>>(p);

@@ -1,13 +1,19 @@
-"""Ends of the ranges that the header promises for log probabilities: the signs of log probabilities and entropies.
+"""Ends of the ranges that the header promises for log probabilities: the signs of log probabilities and
+entropies, sums over long rows.
 
 Tolerances are derived, not measured.  A rounding is off by half a step (relative 2^-24 in fp32, 2^-8 in bf16)."""
 import numpy as np
 import pytest
+import torch
 
 import test_gpu_more_operators as G
+from gpu_util import DT
 from paper_2203_12533_amd import binding as pwb
 
 pytestmark = pytest.mark.gpu
+
+U = G.U
+p = G.p
 
 
 @pytest.fixture(scope="module")
@@ -37,3 +43,54 @@ def test_log_probabilities_are_at_most_zero_and_entropies_at_least(ctx, rows, vo
     assert (lp[ok] <= 0).all() and (tl[ok] <= 0).all(), (lp[ok].max(), tl[ok].max())
     assert (en[ok] >= 0).all() and (st[ok, 1] >= 0).all(), (en[ok].min(), st[ok, 1].min())
     assert np.isnan(lp[7]) and np.isnan(en[7]) and np.isnan(tl[7]).all() and np.isnan(st[7, 1])
+
+
+# ---- log probabilities: long rows ------------------------------------------------------------------------------
+
+def check_long_rows(ctx, levels, at, scale, bf16):
+    """Rows of `levels` [rows, L] in the order that `at` [vocab] tells: sums over the L values are the reference."""
+    rows, vocab = levels.shape[0], at.size
+    levels = G.low(levels, bf16)
+    dt = G.act(bf16)
+    where = torch.from_numpy(at).cuda()
+    z = torch.empty(rows, vocab, dtype=dt, device="cuda")
+    for r in range(rows):
+        z[r] = torch.from_numpy(levels[r]).to(dt).cuda()[where]
+    del where
+    n = np.bincount(at, minlength=levels.shape[1]).astype(np.float64)
+    s = float(np.float32(scale))
+    d = s * (levels - levels.max(1, keepdims=True))
+    e = n * np.exp(d)
+    S, T = e.sum(1), (e * d).sum(1)
+    first = [int(np.argmax(at == level)) for level in range(levels.shape[1])]
+    targets = np.array([first[r % len(first)] for r in range(rows)])
+    dt_target = d[np.arange(rows), np.arange(rows) % len(first)]
+    tt = torch.from_numpy(targets.astype(np.int32)).cuda()
+    lp, en, st = G.full(1, rows, 7.0), G.full(1, rows, 7.0), G.full(rows, 2, 7.0)
+    ws = G.full(1, pwb.logprob_ws_floats(rows, vocab, 0) + 1, float("nan"))
+    a = pwb.LogprobArgs(dtype=DT[bf16], z=p(z), ldz=vocab, rows=rows, vocab=vocab, targets=p(tt), scale=scale)
+    torch.cuda.synchronize()
+    ctx.logprob_fwd(a, p(lp), p(en), p(st), 0, None, None, p(ws))
+    ctx.synchronize()
+    # as test_gpu_more_operators.logp_bounds has them, but the chain does not grow with the row: 32 additions in a part of it, and where
+    # parts, threads and segments meet 32 more
+    e1, e2 = -T / S, (e * d * d).sum(1) / S
+    big, chain = np.log(vocab) + 1, 64
+    G.within(G.back(lp)[0], dt_target - np.log(S), U * (4 * np.abs(dt_target) + 3 * e1 + chain + 8 + 4 * big), "logp", U)
+    G.within(G.back(en)[0], np.log(S) - T / S, U * ((chain + 8) * (2 + e1) + 4 * e2 + 8 * e1 + 4 * big), "entropy", U)
+
+
+@pytest.mark.parametrize("bf16,rows,vocab", [(True, 256, 1 << 22), (False, 256, 1 << 21), (True, 3, (1 << 27) + 5), (False, 3, 1 << 26), (False, 300, 50001)])
+def test_log_probabilities_of_long_rows_of_few_values(ctx, bf16, rows, vocab):
+    """Equal terms round the same way again and again, as logits in few bits do."""
+    rng = np.random.RandomState(1)
+    levels = 3 * rng.randn(rows, 1) - np.arange(8) * rng.uniform(0.01, 0.6, (rows, 1))
+    check_long_rows(ctx, levels, rng.randint(0, 8, vocab).astype(np.uint8).astype(np.int64), 1.0, bf16)
+
+
+@pytest.mark.parametrize("rows,vocab", [(256, 1 << 20), (2, 1 << 24)])
+def test_log_probabilities_of_long_rows_far_from_zero(ctx, rows, vocab):
+    """Rows that are read again with differences from their largest value."""
+    rng = np.random.RandomState(2)
+    levels = 1e11 - 8192.0 * np.arange(8) * (1 + np.arange(rows) % 5)[:, None]
+    check_long_rows(ctx, levels, rng.randint(0, 8, vocab), 1e-4, False)
