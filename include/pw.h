@@ -760,8 +760,8 @@ typedef struct {
 pw_status pw_op_logprob_fwd(pw_ctx* ctx, const pw_logprob_args* args, float* logp, float* entropy, float* stats, int k, int32_t* top_id,
                             float* top_logp, float* ws);
 int64_t pw_logprob_ws_floats(int64_t rows, int64_t vocab, int k);   /* -1 for impossible sizes */
-/* dz = s [dlogp (onehot(target) - p) - dentropy p (log p + H)], rows lddz apart; it may be the same array as z.  stats and entropy: what the
- * forward call wrote (entropy may be null where dentropy is).  dlogp, dentropy: fp32 [rows]; either may be null (dlogp needs targets). */
+/* dz = s [dlogp (onehot(target) - p) - dentropy p (log p + H)], rows lddz apart; it may be the same array as z if lddz = ldz, and overlaps
+ * nothing else.  stats and entropy: what the forward call wrote (entropy may be null where dentropy is).  dlogp, dentropy: fp32 [rows]; either may be null (dlogp needs targets). */
 pw_status pw_op_logprob_bwd(pw_ctx* ctx, const pw_logprob_args* args, const float* stats, const float* entropy, const float* dlogp,
                             const float* dentropy, void* dz, int64_t lddz);
 

@@ -638,6 +638,7 @@ hipError_t launch_logprob_bwd(hipStream_t s, const LogprobArgs& a, const float* 
   if (check(a) != hipSuccess || !stats || !dz || lddz < a.vocab || (dlogp && !a.targets) || (dentropy && !entropy)) return hipErrorInvalidValue;
   if (((uintptr_t)dlogp | (uintptr_t)entropy | (uintptr_t)dentropy) & 3 || (uintptr_t)stats & 7 || (uintptr_t)dz & (a.dtype == kBF16 ? 1 : 3))
     return hipErrorInvalidValue;
+  if (dz == a.z && lddz != a.ldz && a.rows > 1) return hipErrorInvalidValue;   // a row's gradient would lie on other rows' logits
   if (a.rows == 0) return hipSuccess;
   const int64_t seg = (int64_t)kBwdThreads * kBwdVecs * (a.dtype == kBF16 ? 8 : 4), segments = (a.vocab + seg - 1) / seg;
   const float k2 = a.scale * kLog2e;

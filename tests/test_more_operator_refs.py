@@ -229,6 +229,28 @@ def test_what_the_launchers_refuse(tmp_path):
     assert r.returncode == 0, r.stdout + r.stderr
 
 
+def run_on_the_host(tmp_path, body):
+    """A program over the launchers; `expect` as in REFUSALS."""
+    src, exe = tmp_path / "more.cpp", tmp_path / "more"
+    src.write_text(REFUSALS[:REFUSALS.index("  // quantisation")] + body + '  std::printf("%d\\n", bad);\n  return bad != 0;\n}\n')
+    here = os.path.dirname(pwb.LIB_PATH)
+    subprocess.check_call(["g++", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", os.path.join(here, "csrc"), str(src),
+                           "-L", here, "-lpw", "-L/opt/rocm/lib", "-lamdhip64", "-Wl,-rpath," + here, "-Wl,-rpath,/opt/rocm/lib", "-o", str(exe)])
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
+def test_a_gradient_in_place_has_the_rows_of_the_logits(tmp_path):
+    """With another stride a row of the gradient would lie on logits that another workgroup has still to read."""
+    run_on_the_host(tmp_path, r'''
+  const LogprobArgs a{kBF16, P, 12, 4, 10, I, 1.f};
+  expect("closer", launch_logprob_bwd(nullptr, a, F, F, F, F, P, 10), no);
+  expect("further apart", launch_logprob_bwd(nullptr, a, F, F, F, F, P, 16), no);
+  LogprobArgs none = a; none.rows = 0;
+  expect("the same", launch_logprob_bwd(nullptr, none, F, F, F, F, P, 12), ok);
+''')
+
+
 def test_calls_without_a_context_or_arguments_are_refused():
     lib = pwb.lib()
     for name, args in (("f4_quantize", [None]), ("f4_gemm", [None]), ("rmsnorm_fwd", [None] * 7), ("rmsnorm_bwd", [None] * 9 + [0]),
