@@ -750,7 +750,7 @@ typedef struct {
   int64_t ldz;               /* elements from row to row */
   int64_t rows, vocab;       /* rows at most 2^31 - 1, vocab 1 .. 2^28 */
   const int32_t* targets;    /* device, [rows], or null.  A token outside [0, vocab) is none: the row's logp is 0 and dlogp is not looked at */
-  float scale;               /* s: positive and finite */
+  float scale;               /* s: positive, at most 2^127 */
 } pw_logprob_args;
 /* logp, entropy: fp32 [rows], or null (logp needs targets).  stats: fp32 [rows][2], 8-byte aligned, for the backward call, or null: the largest z and the log of sum
  * exp(s (z - that)).  top_id: int32 [rows][k] and top_logp: fp32 [rows][k], the k tokens of largest z in descending order, the lowest index first among

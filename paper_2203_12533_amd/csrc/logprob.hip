@@ -560,7 +560,7 @@ __global__ __launch_bounds__(kBwdThreads, 8) void logprob_bwd_kernel(LogprobBwdP
 
 hipError_t check(const LogprobArgs& a) {
   if ((a.dtype != kF32 && a.dtype != kBF16) || !a.z || a.rows < 0 || a.rows > (1LL << 31) - 1 || a.vocab < 1 || a.vocab > (1LL << 28) ||
-      a.ldz < a.vocab || !(a.scale > 0.f && a.scale < INFINITY) || ((uintptr_t)a.z & (a.dtype == kBF16 ? 1 : 3)) || ((uintptr_t)a.targets & 3))
+      a.ldz < a.vocab || !(a.scale > 0.f && a.scale <= 0x1p127f) || ((uintptr_t)a.z & (a.dtype == kBF16 ? 1 : 3)) || ((uintptr_t)a.targets & 3))
     return hipErrorInvalidValue;
   return hipSuccess;
 }

@@ -1,5 +1,5 @@
 """Ends of the ranges that the header promises for log probabilities: the signs of log probabilities and
-entropies, sums over long rows.
+entropies, sums over long rows, the largest and smallest scales.
 
 Tolerances are derived, not measured.  A rounding is off by half a step (relative 2^-24 in fp32, 2^-8 in bf16)."""
 import numpy as np
@@ -94,3 +94,12 @@ def test_log_probabilities_of_long_rows_far_from_zero(ctx, rows, vocab):
     rng = np.random.RandomState(2)
     levels = 1e11 - 8192.0 * np.arange(8) * (1 + np.arange(rows) % 5)[:, None]
     check_long_rows(ctx, levels, rng.randint(0, 8, vocab), 1e-4, False)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("scale", [2.0 ** 127, 1e30, 1e-30, 2.0 ** -126, 1e-44])
+def test_log_probabilities_at_the_ends_of_the_scale(ctx, scale, bf16):
+    z = 3 * G.rnd(5, 20, 700)
+    z[3:6] = 0.0
+    z[4, 10] = -1.0
+    G.logprob(ctx, z, np.arange(20) * 30, scale, 4, bf16, backward=False)

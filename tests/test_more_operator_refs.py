@@ -251,6 +251,18 @@ def test_a_gradient_in_place_has_the_rows_of_the_logits(tmp_path):
 ''')
 
 
+def test_a_scale_whose_base_2_form_overflows_is_refused(tmp_path):
+    """s log2 e has to be a number: 0 times infinity would make the likeliest token's shift NaN."""
+    run_on_the_host(tmp_path, r'''
+  LogprobArgs a{kBF16, P, 10, 4, 10, I, 3e38f};
+  expect("forward", launch_logprob_fwd(nullptr, a, F, F, F, 3, I, F, F), no);
+  expect("backward", launch_logprob_bwd(nullptr, a, F, F, F, F, P, 10), no);
+  a.scale = 0x1.000002p127f; expect("just above", launch_logprob_fwd(nullptr, a, F, F, F, 3, I, F, F), no);
+  a.scale = 0x1p127f; a.rows = 0; expect("the largest", launch_logprob_fwd(nullptr, a, F, F, F, 3, I, F, F), ok);
+  a.scale = 1e-30f; expect("a small one", launch_logprob_fwd(nullptr, a, F, F, F, 3, I, F, F), ok);
+''')
+
+
 def test_calls_without_a_context_or_arguments_are_refused():
     lib = pwb.lib()
     for name, args in (("f4_quantize", [None]), ("f4_gemm", [None]), ("rmsnorm_fwd", [None] * 7), ("rmsnorm_bwd", [None] * 9 + [0]),
