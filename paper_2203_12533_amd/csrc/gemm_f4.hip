@@ -788,6 +788,7 @@ hipError_t launch_direct(hipStream_t s, GemmF4Params p, bool f32) {
   else gemm_f4_direct_kernel<W, false><<<(int)(tm * tn), 64 * W, 0, s>>>(p);
   return hipGetLastError();
 }
+enum Kernel { kDirect4, kDirect8, kFew, kSplit, kHalf, kMid, kBig };
 // Which shape: the largest whose tiles give every compute unit one, as a launch of up to one round takes as long as one tile.  Measured in us on both
 // sides of each step (k = 2048 unless it says so, bf16):
 //   few rows and columns straight from memory, up to 512 blocks of 16 x 16 (1 x 8192 3.8, as tiles of 32 x 64 4.4, 16 x 8192 4.5 and 4.5; beyond, 1 x 16384
@@ -800,17 +801,17 @@ hipError_t launch_direct(hipStream_t s, GemmF4Params p, bool f32) {
 //     4096 x 5376, 336, 35.4 and 36.3); from the third on it does not (8192 x 4608, 576, 56.0 and 56.1; 8192 x 8448, 1056, 92 and 100).
 //   Operands of one row or column of tiles: half of a tile of 256 x 256 would be empty (128 x 131072 45.4, as 128 x 128 33.9; 131072 x 128 43.4 and 32.9;
 //     131072 x 100, whose rows of C do not end with a tile, 39.6 and 46.9), and of 128 x 128 (131072 x 60 45.3, as 128 x 64 35.1).
-hipError_t choose(hipStream_t s, const GemmF4Params& p, bool f32) {
-  auto tiles = [&](int m, int n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
-  const bool deep = p.K >= 4096;
-  if (tiles(16, 16) <= (deep ? 256 : 512) || p.lda > kMaxLd || p.ldb > kMaxLd) return deep ? launch_direct<8>(s, p, f32) : launch_direct<4>(s, p, f32);
-  if (tiles(Few::BM, Few::BN) <= 256) return launch<Few>(s, p, f32);
-  if (tiles(Split::BM, Split::BN) <= 256) return launch<Split>(s, p, f32);
-  if (tiles(Half::BM, Half::BN) <= 256 || p.N <= Half::BN) return launch<Half>(s, p, f32);
+Kernel choose(int64_t M, int64_t N, int64_t K, bool far_apart) {
+  auto tiles = [&](int m, int n) { return ((M + m - 1) / m) * ((N + n - 1) / n); };
+  const bool deep = K >= 4096;
+  if (tiles(16, 16) <= (deep ? 256 : 512) || far_apart) return deep ? kDirect8 : kDirect4;
+  if (tiles(Few::BM, Few::BN) <= 256) return kFew;
+  if (tiles(Split::BM, Split::BN) <= 256) return kSplit;
+  if (tiles(Half::BM, Half::BN) <= 256 || N <= Half::BN) return kHalf;
   const int64_t big = tiles(Big::BM, Big::BN);
-  if (p.K > kF4BK && p.M > Mid::BM && p.N != Mid::BN && big > 128 && (big <= 256 || big >= 336)) return launch_big(s, p, f32);
-  return launch<Mid>(s, p, f32);
+  return K > kF4BK && M > Mid::BM && N != Mid::BN && big > 128 && (big <= 256 || big >= 336) ? kBig : kMid;
 }
+bool rows_far_apart(const GemmF4Args& a) { return a.lda / 2 > kMaxLd || a.ldb / 2 > kMaxLd; }
 
 }  // namespace
 
@@ -821,6 +822,11 @@ hipError_t gemm_f4_init() {
   if (e == hipSuccess) e = prepare<Split>();
   if (e == hipSuccess) e = prepare<Few>();
   return e;
+}
+
+const char* gemm_f4_kernel(const GemmF4Args& a) {
+  static const char* const names[] = {"direct, 4 waves", "direct, 8 waves", "32 x 64", "64 x 64", "128 x 64", "128 x 128", "256 x 256"};
+  return names[choose(a.M, a.N, a.K, rows_far_apart(a))];
 }
 
 hipError_t launch_gemm_f4(hipStream_t s, const GemmF4Args& a) {
@@ -841,7 +847,17 @@ hipError_t launch_gemm_f4(hipStream_t s, const GemmF4Args& a) {
   p.M = a.M; p.N = a.N; p.K = a.K; p.lda = a.lda / 2; p.ldb = a.ldb / 2;
   p.epi.mode = a.epilogue; p.epi.out_bf16 = a.out_dtype == kBF16; p.epi.accumulate = a.accumulate;
   p.epi.bias = a.bias; p.epi.aux = a.aux; p.epi.C = a.C; p.epi.C2 = a.C2; p.epi.ldc = a.ldc;
-  return choose(s, p, a.out_dtype == kF32);
+  const bool f32 = a.out_dtype == kF32;
+  switch (choose(a.M, a.N, a.K, rows_far_apart(a))) {
+    case kDirect4: return launch_direct<4>(s, p, f32);
+    case kDirect8: return launch_direct<8>(s, p, f32);
+    case kFew: return launch<Few>(s, p, f32);
+    case kSplit: return launch<Split>(s, p, f32);
+    case kHalf: return launch<Half>(s, p, f32);
+    case kMid: return launch<Mid>(s, p, f32);
+    case kBig: return launch_big(s, p, f32);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace pw

@@ -215,6 +215,7 @@ struct GemmF4Args {
   void* C2;
 };
 hipError_t launch_gemm_f4(hipStream_t s, const GemmF4Args& a);
+const char* gemm_f4_kernel(const GemmF4Args& a);   // that this product goes to: for tests, which have to reach all of them
 hipError_t gemm_f4_init();   // one-time set-up of kernel attributes (dynamic LDS); call once before any capture
 
 // rmsnorm.hip

@@ -1,5 +1,5 @@
-"""Ends of the ranges that the header promises for log probabilities: the signs of log probabilities and
-entropies, sums over long rows, the largest and smallest scales.
+"""Ends of the ranges that the header promises for the 4-bit products, log probabilities and clipping: the signs of log probabilities and
+entropies, sums over long rows, the largest and smallest scales, every epilogue of the product whose workgroups take tiles in turn.
 
 Tolerances are derived, not measured.  A rounding is off by half a step (relative 2^-24 in fp32, 2^-8 in bf16)."""
 import numpy as np
@@ -103,3 +103,34 @@ def test_log_probabilities_at_the_ends_of_the_scale(ctx, scale, bf16):
     z[3:6] = 0.0
     z[4, 10] = -1.0
     G.logprob(ctx, z, np.arange(20) * 30, scale, 4, bf16, backward=False)
+
+
+# ---- products whose workgroups take output tiles in turn -------------------------------------------------------
+
+# Whole tiles of 256 x 256 and ragged ones, one to a workgroup and several, two k tiles and more, the last of them whole or not.
+STREAM = [(2560, 4096, 288), (3100, 2900, 544), (5120, 4352, 288), (4900, 4700, 800)]
+
+
+@pytest.mark.parametrize("epilogue,bf16,accumulate", G.EPILOGUES)
+@pytest.mark.parametrize("m,n,k", STREAM)
+def test_f4_product_epilogues_of_tiles_in_turn(ctx, m, n, k, epilogue, bf16, accumulate):
+    G.product(ctx, m, n, k, epilogue=epilogue, bf16=bf16, accumulate=accumulate, seed=m)
+
+
+@pytest.mark.parametrize("m,n,k,bf16", [(2560, 4096, 512, True), (5120, 4352, 512, False), (4900, 4701, 544, True), (4900, 4701, 544, False), (9000, 4700, 288, False)])
+def test_f4_product_sums_of_tiles_in_turn_are_exact(ctx, m, n, k, bf16):
+    """fp32: every sum is a multiple of 1/4 below 2^22; bf16 rounds it once."""
+    G.product(ctx, m, n, k, exact=True, seed=7, bf16=bf16)
+
+
+def test_f4_product_of_tiles_in_turn_keeps_its_blocks_apart(ctx):
+    """Blocks without a number stay in their rows, rows and tables apart, no bias where none is given, and a bias that outweighs the sums."""
+    G.product(ctx, 4900, 4701, 288, nan_blocks=((0, 8), (255, 0), (256, 8), (4899, 7)), bf16=True)
+    G.product(ctx, 4900, 4700, 544, lda=576, ldb=640, ldc=4736, epilogue=pwb.PW_EPI_BIAS, bf16=True)
+    G.product(ctx, 4900, 4700, 288, epilogue=pwb.PW_EPI_BIAS_GELU, bf16=True, bias=False)
+    G.product(ctx, 4900, 4700, 800, epilogue=pwb.PW_EPI_BIAS, bias_scale=2.0 ** 24)
+
+
+@pytest.mark.parametrize("m,n,k", [(2560, 4096, 288), (3100, 2904, 288), (5120, 4352, 288), (4900, 4704, 800)])
+def test_f4_product_of_tiles_in_turn_takes_a_residual_in_place(ctx, m, n, k):
+    G.test_f4_product_takes_a_residual_in_place(ctx, m, n, k)

@@ -232,7 +232,7 @@ def test_what_the_launchers_refuse(tmp_path):
 def run_on_the_host(tmp_path, body):
     """A program over the launchers; `expect` as in REFUSALS."""
     src, exe = tmp_path / "more.cpp", tmp_path / "more"
-    src.write_text(REFUSALS[:REFUSALS.index("  // quantisation")] + body + '  std::printf("%d\\n", bad);\n  return bad != 0;\n}\n')
+    src.write_text("#include <string>" + REFUSALS[:REFUSALS.index("  // quantisation")] + body + '  std::printf("%d\\n", bad);\n  return bad != 0;\n}\n')
     here = os.path.dirname(pwb.LIB_PATH)
     subprocess.check_call(["g++", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", os.path.join(here, "csrc"), str(src),
                            "-L", here, "-lpw", "-L/opt/rocm/lib", "-lamdhip64", "-Wl,-rpath," + here, "-Wl,-rpath,/opt/rocm/lib", "-o", str(exe)])
@@ -261,6 +261,26 @@ def test_a_scale_whose_base_2_form_overflows_is_refused(tmp_path):
   a.scale = 0x1p127f; a.rows = 0; expect("the largest", launch_logprob_fwd(nullptr, a, F, F, F, 3, I, F, F), ok);
   a.scale = 1e-30f; expect("a small one", launch_logprob_fwd(nullptr, a, F, F, F, 3, I, F, F), ok);
 ''')
+
+
+def test_sizes_of_the_product_tests_reach_the_kernels_that_they_are_for(tmp_path):
+    """Where the choice of a kernel changes, sizes here and in the GPU tests have to follow."""
+    import test_gpu_more_operator_edges as edges
+    want = [(1, 200, 128, 0, "direct, 4 waves"), (3, 5000, 256, 0, "direct, 4 waves"), (33, 1000, 4096, 0, "direct, 8 waves"), (70, 5000, 96, 1 << 24, "32 x 64"),
+            (70, 5000, 96, (1 << 24) + 32, "direct, 4 waves"), (260, 300, 1056, 0, "direct, 4 waves"), (300, 520, 2080, 0, "32 x 64"), (500, 1300, 1056, 0, "64 x 64"),
+            (700, 900, 160, 0, "64 x 64"), (1030, 1100, 544, 0, "128 x 64"), (1300, 1100, 256, 0, "128 x 64"), (1500, 1420, 288, 0, "128 x 128"),
+            (1700, 1900, 1056, 0, "128 x 128"), (40000, 70, 160, 0, "128 x 128"), (70, 40000, 160, 0, "128 x 128"),
+            (2560, 4096, 256, 0, "128 x 128"), (3100, 2900, 256, 0, "128 x 128"), (3100, 2900, 416, 0, "256 x 256"), (2570, 4099, 288, 0, "256 x 256"),
+            (2560, 4096, 4096, 0, "256 x 256")]
+    want += [(m, n, k, 0, "256 x 256") for m, n, k in edges.STREAM] + [(4900, 4701, 288, 0, "256 x 256"), (9000, 4700, 288, 0, "256 x 256")]
+    lines = ["  struct { int64_t m, n, k, ld; const char* name; } const want[] = {"]
+    lines += ['    {%d, %d, %d, %d, "%s"},' % w for w in want]
+    lines += ["  };", "  for (const auto& w : want) {", "    GemmF4Args a{}; a.M = w.m; a.N = w.n; a.K = w.k; a.lda = w.ld ? w.ld : w.k; a.ldb = w.k;",
+              "    const char* got = gemm_f4_kernel(a);",
+              '    if (std::string(got) != w.name) { std::printf("%ld x %ld x %ld: %s, not %s\\n", (long)w.m, (long)w.n, (long)w.k, got, w.name); ++bad; }', "  }\n"]
+    run_on_the_host(tmp_path, "\n".join(lines))
+    tiles = [(m, n, -(-m // 256) * -(-n // 256)) for m, n, _ in edges.STREAM]
+    assert any(t > 256 and m % 256 == n % 256 == 0 for m, n, t in tiles) and any(t > 256 and m % 256 and n % 256 for m, n, t in tiles)   # several to a workgroup
 
 
 def test_calls_without_a_context_or_arguments_are_refused():
