@@ -1,5 +1,5 @@
 """Ends of the ranges that the header promises for the 4-bit products, log probabilities and clipping: the signs of log probabilities and
-entropies, sums over long rows, the largest and smallest scales, every epilogue of the product whose workgroups take tiles in turn.
+entropies, sums over long rows, the largest and smallest scales, every epilogue of the product whose workgroups take tiles in turn, and arrays that no cache holds.
 
 Tolerances are derived, not measured.  A rounding is off by half a step (relative 2^-24 in fp32, 2^-8 in bf16)."""
 import numpy as np
@@ -103,6 +103,74 @@ def test_log_probabilities_at_the_ends_of_the_scale(ctx, scale, bf16):
     z[3:6] = 0.0
     z[4, 10] = -1.0
     G.logprob(ctx, z, np.arange(20) * 30, scale, 4, bf16, backward=False)
+
+
+# ---- arrays that no cache holds --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("bf16,rows", [(True, 5000), (False, 2600)])
+def test_log_probabilities_past_the_caches_are_those_of_parts(ctx, bf16, rows):
+    """More than 256 MB of logits: rows read past the caches, rows left in them and the border between; the same bits as calls of fewer rows have."""
+    vocab, k, part = 33001, 5, 900                            # parts of more rows than a call has for which kernels are others
+    z = 2 * torch.randn(rows, vocab, device="cuda")
+    z = z.to(G.act(bf16))
+    t = torch.randint(0, vocab, (rows,), device="cuda", dtype=torch.int32)
+    dl, de = torch.randn(rows, device="cuda"), torch.randn(rows, device="cuda")
+    new = lambda *s, dt=torch.float32: torch.zeros(*s, dtype=dt, device="cuda")  # noqa: E731
+
+    def outputs():
+        return new(rows), new(rows), new(rows, 2), new(rows, k, dt=torch.int32), new(rows, k), torch.zeros_like(z)
+
+    def run(out, first, n, dz=None):
+        lp, en, st, ids, tl, own = out
+        dz = own if dz is None else dz
+        at = lambda x: x[first:].data_ptr()  # noqa: E731
+        a = pwb.LogprobArgs(dtype=DT[bf16], z=at(z), ldz=vocab, rows=n, vocab=vocab, targets=at(t), scale=1.25)
+        ctx.logprob_fwd(a, at(lp), at(en), at(st), k, at(ids), at(tl))
+        ctx.logprob_bwd(a, at(st), at(en), at(dl), at(de), at(dz), vocab)
+    whole, parts = outputs(), outputs()
+    torch.cuda.synchronize()
+    run(whole, 0, rows)
+    for first in range(0, rows, part):
+        run(parts, max(0, min(first, rows - part)), part)
+    ctx.synchronize()
+    for name, x, y in zip(("logp", "entropy", "stats", "ids", "top", "dz"), whole, parts):
+        assert torch.equal(x, y), name
+    zd = z[-3:].double()                                      # and they are the right ones
+    lsm = torch.log_softmax(1.25 * zd, 1)
+    assert torch.allclose(whole[0][-3:].double(), lsm.gather(1, t[-3:].long()[:, None])[:, 0], rtol=0, atol=1e-5)
+    run(whole, 0, rows, dz=z)
+    ctx.synchronize()
+    assert torch.equal(z, parts[5])
+
+
+def test_clipping_past_the_caches_and_of_many_groups(ctx):
+    """More chunks than blocks in both launches, more tensors than a launch takes, and 256 MB from the end inside of a tensor."""
+    sizes = [60000001, 40000003] + [1000 + 17 * i for i in range(100)] + [50000005, 100000007]
+    kinds = [torch.float32, torch.bfloat16] + [torch.bfloat16 if i % 2 else torch.float32 for i in range(100)] + [torch.float32, torch.bfloat16]
+    g = [(torch.randn(n, device="cuda") * (1 + i % 3)).to(dt) for i, (n, dt) in enumerate(zip(sizes, kinds))]
+    total = sum(float((x.double() ** 2).sum()) for x in g)
+    res, ws = G.full(1, 2, 0.0), G.full(1, pwb.grad_clip_ws_floats(), float("nan"))
+
+    def run(outs, max_norm):
+        ts = pwb.grad_tensors([(x.data_ptr(), o.data_ptr(), x.numel(), DT[x.dtype == torch.bfloat16]) for x, o in zip(g, outs)])
+        torch.cuda.synchronize()
+        ctx.grad_clip(ts, max_norm, p(res), p(ws))
+        ctx.synchronize()
+        norm, factor = G.back(res)[0]
+        assert abs(norm - total ** 0.5) <= (U + 2.0 ** -40) * norm
+        assert abs(factor - min(1.0, float(np.float32(max_norm)) / total ** 0.5)) <= (U + 2.0 ** -40) * factor
+        return factor
+    before = [x.clone() for x in g]
+    for max_norm in (100.0, 1e9):
+        outs = [torch.zeros_like(x) for x in g]
+        f = run(outs, max_norm)
+        for x, o in zip(g, outs):                             # one product in 32 bits, which bf16 rounds
+            assert torch.equal(o, (x.float() * f).to(x.dtype))
+        del outs
+    assert run(g, 1e9) == 1.0
+    assert all(torch.equal(x, b) for x, b in zip(g, before))
+    f = run(g, 100.0)
+    assert f < 1.0 and all(torch.equal(x, (b.float() * f).to(x.dtype)) for x, b in zip(g, before))
 
 
 # ---- products whose workgroups take output tiles in turn -------------------------------------------------------
