@@ -767,7 +767,8 @@ pw_status pw_op_logprob_bwd(pw_ctx* ctx, const pw_logprob_args* args, const floa
 
 /* ---- clipping by the norm of all gradients -----------------------------------------------------------
  * norm = sqrt(sum of the squares of all elements of all tensors), summed in 64 bits in a fixed order; factor = max_norm / norm where norm
- * exceeds max_norm, else 1 (NaN where the norm is NaN); out = g factor, rounded once. */
+ * exceeds max_norm, else 1 (NaN where the norm is NaN); out = g factor in fp32, which a bf16 output rounds once more.  Norm and factor are
+ * rounded to fp32 after they are formed in 64 bits. */
 typedef struct {
   const void* g;             /* device, aligned to its elements; may be null where n is 0 */
   void* out;                 /* like g; may be g itself; null: this tensor counts and is not scaled */

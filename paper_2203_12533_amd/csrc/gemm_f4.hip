@@ -55,7 +55,7 @@ __device__ __forceinline__ f32x4 mfma(const i32x4& b4, const i32x4& a4, f32x4 c,
 // Few rows, and rows too far apart for 32-bit offsets.  What bounds a product of few rows is reading B once, so nothing is
 // staged: a block owns 16 columns and 16 rows, its waves take every W-th 128 k, operands go from memory straight into
 // fragments (four lanes read 64 consecutive bytes of a row), kAhead steps at a time, and the waves' sums meet in LDS in wave order.
-// 1 x 8192 x 2048 3.8 us, a launch.
+// 1 x 8192 x 2048 4.9 us (3.8 to 4.3 where the operands of one call are those of the next), a launch.
 constexpr int kAhead = 4;
 template <int W, bool F32>
 __global__ __launch_bounds__(64 * W) void gemm_f4_direct_kernel(GemmF4Params p) {
@@ -153,8 +153,11 @@ __device__ __forceinline__ int read_scales(uint32_t at) {
 // leave from registers, in stores that nobody waits for.
 // What lies behind k in the last k tile is never made zero: scales of 0 (2^-127) on both sides make a product of any two e2m1 numbers vanish
 // (36 * 2^-254), so the lanes that would read behind the row read its beginning again, and one loop body serves every k tile.
-// Bound by power where k is long (8192^3 bf16 229 us, 4.8 PFLOP/s at 1.76 GHz), by LDS, whose reads take the time of the matrix instructions, in a k tile
-// (1.6 us, 64 instructions to a wave), and between output tiles by the way of the results out (8192 x 8192 x 2048 74 us, 78 to 83 where no cache holds C).
+// No single unit is full.  Where k is long (8192^3 bf16 229 us, 4.8 PFLOP/s) the matrix pipe is busy 61 % of the cycles, of which there are fewer (1.77 GHz,
+// against 2.1 to 2.3 in the shorter launches: power), and LDS 29 %; waves stand at waits for 26 % of theirs and wait for their turn 39 %.  A k tile takes 1.6 us
+// for 2048 cycles of matrix instructions on a SIMD.  8192 x 8192 x 2048, eight k tiles to an output tile, 74 us, 78 to 83 where no cache holds C: 38 % and 21 %;
+// of the 17 us of an output tile about 4 go to converting and storing it.  2048 x 8192 x 8192 fp32 66 to 70 us: 39 % and 24 %.  With a second output (GELU) 98
+// us at 8192 x 8192 x 2048, GELU backward 117, fp32 102 to 113, with a residual or an old value 162 to 166.  The fp32 form keeps 10 vector registers in memory.
 template <int WM_, int WN_, int FM_, int FN_>
 struct Stream {
   static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, G = WM * WN, kThreads = 64 * G;
@@ -503,8 +506,8 @@ __global__ __launch_bounds__(S::kThreads, S::G / 4) void gemm_f4_stream_kernel(G
 // Fragments are read one block of rows ahead of their use and MFMAs run across k tiles without a pause.  All of a k tile has been read from
 // LDS one unit (a block of rows against all columns of the wave) before its end; there (kTurn) the waves of a group meet, the next k
 // tile is there, and the stage of this one is free for k tile t + NS.  What bounds a launch of one round is a chain: loads, k tiles, the waves' sums where they
-// share a tile, epilogue (1000 x 760 x 1056 with a residual, 192 tiles of 64 x 64, 5.5 us); 2048 x 2048 x 8192, 256 tiles of 128 x 128, 25.3 us,
-// 2.7 PFLOP/s.
+// share a tile, epilogue (1000 x 760 x 1056 with a residual, 192 tiles of 64 x 64, 6.0 us); 2048 x 2048 x 8192, 256 tiles of 128 x 128, 25.4 us,
+// 2.7 PFLOP/s (fp32 29.0).
 template <class S, bool F32>
 __global__ __launch_bounds__(S::kThreads, S::kWavesPerSimd) void gemm_f4_tile_kernel(GemmF4Params p) {
   constexpr int FM = S::FM, FN = S::FN, G = S::G, WN = S::WN;
@@ -790,7 +793,8 @@ hipError_t launch_direct(hipStream_t s, GemmF4Params p, bool f32) {
 }
 enum Kernel { kDirect4, kDirect8, kFew, kSplit, kHalf, kMid, kBig };
 // Which shape: the largest whose tiles give every compute unit one, as a launch of up to one round takes as long as one tile.  Measured in us on both
-// sides of each step (k = 2048 unless it says so, bf16):
+// sides of each step, on one set of data (k = 2048 unless it says so, bf16; other k from 288 on and fp32 outputs follow the same steps, whose
+// places were not measured for them):
 //   few rows and columns straight from memory, up to 512 blocks of 16 x 16 (1 x 8192 3.8, as tiles of 32 x 64 4.4, 16 x 8192 4.5 and 4.5; beyond, 1 x 16384
 //     5.0 and 4.5, 3 x 32768 9.1 and 8.0), up to 256 if k is long (16 x 4096 x 4096 4.5 and 5.2, x 8192 7.2 and 6.8; beyond, 16 x 8192 x 4096 6.6 and 5.2,
 //     128 x 1024 x 16384 19.8 and 10.0); eight waves share a long k (16 x 4096 x 8192 7.2, four 7.7), four a short one (3 x 32768 9.1, eight 11.6);

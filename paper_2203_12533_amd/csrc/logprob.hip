@@ -6,23 +6,24 @@
 // In base 2: d = z k - max k with k = s log2 e, one fused multiply-add, whose product is exact; that max k is rounded shifts all of a row alike, by
 // an amount of at most 1/4 that is known and taken off log S (in H it cancels).  What rounding then leaves of log S and H below 0 becomes 0, so that no
 // probability is above 1.  Every thread keeps a running maximum, S and sum of its own; they meet once per row, in a tree.  A
-// part of a row (32 terms of a thread) is summed in fp32 and joins the running pair in 64 bits: equal terms, as logits in few bits give, round the same way every
-// time, and log S of a chain of 16384 fp32 additions was off by 8e-5.
+// part of a row (32 terms of a thread) is summed in fp32 and joins the running pair in 64 bits: equal terms, as logits in few bits give, round the same way
+// every time, and log S of a chain of 16384 fp32 additions was off by 8e-5.
 //
 // Alternatives.  Every wave keeps a list in LDS of what can be among the k best of its columns, without a word to the others: with a part of the row in
-// registers, the k-th largest of its 64 lanes' maxima (the upper 16 bits of it) is a bound that k elements at least reach, and
-// usually few more do.  Those go to the list as keys of value and index, 64 bits, no two alike, placed by a ballot; what comes later in the row adds
-// what reaches the bound.  A list that is full gets a tighter bound, and where that does not help - values that fall into few
-// lanes - the k best are taken out one by one.  At the end one wave takes the lists together, drops what is below such a bound of all, and ranks the rest
-// by counting (every wave its own list first, in order: 174 us for 8192 rows of 32768 bf16 and k = 32, this then 147).
+// registers, the k-th largest of its 64 lanes' maxima (the upper 16 bits of it) is a bound that k elements at least reach, and usually few more do.  Those go to
+// the list as keys of value and index, 64 bits, no two alike, placed by a ballot; what comes later in the row adds what reaches the bound.  A list that is full
+// gets a tighter bound, and where that does not help - values that fall into few lanes - the k best are taken out one by one, from memory: with 8 of them 2110
+// us for 8192 rows of 32768 bf16 of one value, and 1750 where a mask of the type's lowest value leaves 200 neighbours of each row (a mask of -infinity 85, since
+// that is no alternative; other rows 107).  At the end one wave takes the lists together, drops what is below such a bound of all, and ranks the rest by
+// counting (every wave its own list first, in order: 174 us for 8192 rows of 32768 bf16 and k = 32, this then 147).
 //
 // Bound by memory: forward one read, backward one read and one write, the forward one nearly as much by its 40 or so cycles per element and lane
 // (exp2 takes four slots of ten); vectors that lie behind the row as a whole are left out (8192 x 9000 bf16, 8 alternatives, 74 us with them, 55
 // without).  The last 256 MB of logits, what the large cache holds, are read so that they stay there, and the backward call goes backwards and finds
-// them; all else is read, and the gradient written, past the caches.  8192 rows of 32768 bf16: forward 93 us without alternatives (5.8 TB/s), 111
-// with 8, 128 with 32; forward with 8 and backward 266, with every access an ordinary one, forwards, 338.  4096 rows of fp32: 93 and 253, so 321.
-// Few rows are cut into segments, a block each, and joined by a second launch (4 rows of 32768 fp32, 20 alternatives: 10.7 us; as one block of 1024
-// threads 12.2); a call of one launch is bound by latency (1 x 4000: 5.1 us).
+// them; all else is read, and the gradient written, past the caches.  8192 rows of 32768 bf16: forward 92 us without alternatives (5.8 TB/s), 107
+// with 8, 125 with 32; forward with 8 and backward 261 to 266, with every access an ordinary one, forwards, 338.  4096 rows of fp32: 94 and 252, so 321.
+// Few rows are cut into segments, a block each, and joined by a second launch (4 rows of 32768 fp32, 20 alternatives: 10.6 us; as one block of 1024
+// threads 12.2); a call of one launch is bound by latency (1 x 4000: 5.6 us).
 #include <type_traits>
 
 #include "common.hpp"
@@ -247,7 +248,7 @@ template <int M> __device__ __forceinline__ int shortlist(const uint64_t (&key)[
 }
 
 // NT threads of a block, U vectors of 16 bytes to one in a chunk; a wave's list has kPlaces places, and kMaxTop more for a k best of a chunk.  Six blocks of 256
-// to a unit, two registers spilled for it (8192 x 32768 bf16, 8 alternatives, 103 us; five 106).
+// to a unit, two registers spilled for it (8192 x 32768 bf16 107.1 us with 8 alternatives, 124.4 with 32; five 106.1 and 130.6).
 constexpr int kPlaces = 256;
 template <class T, int NT, int U, bool TOP>
 __global__ __launch_bounds__(NT, NT == 256 ? 6 : 4) void logprob_fwd_kernel(LogprobFwdParams p) {
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? 6 : 4) void logprob_fwd_kernel(Logp
     if (lane < n) list[lane] = best_keys[wave * kMaxTop + lane];
     wave_sync();
   };
-  // The k best of the wave's part of the chunk to the end of the list, one by one, from memory: rows that come here are odd ones.
+  // The k best of the wave's part of the chunk to the end of the list, one by one, from memory.
   auto extract = [&](uint32_t c0) {
     uint64_t last = ~0ull;
 #pragma unroll 1
@@ -573,8 +574,9 @@ static int64_t kept_from(const LogprobArgs& a) {
   return rows < a.rows ? a.rows - rows : 0;
 }
 // How many segments rows are cut into: where there are too few for the chip and a row is more than 64 KB, as many as keep 4096 elements each, a block of 256 threads to one.
-// Up to two blocks of 512 threads to a unit, whole rows of more than 16 KB are one block's of 512 threads, else of 256, of 64 up to 2048 elements, and a thread's vectors in a chunk
-// are no more than the row needs (8192 x 4000 bf16, 4 alternatives, 47 with four, 29 with two; 8192 x 100 15.5 with four, 10.0 with one).  In us, 20 alternatives:
+// Up to two blocks of 512 threads to a unit, whole rows of more than 16 KB are one block's of 512 threads, else of 256, of 64 up to 2048 elements, and a
+// thread's vectors in a chunk are no more than the row needs (8192 x 4000 bf16, 4 alternatives, 47 with four, 29, now 26.6, with two; 8192 x 100 15.5 with four,
+// 10.4 with one).  In us, 20 alternatives:
 //                      cut   512   256 threads                            cut   512   256 threads
 //   4 x 32768 bf16    11.4  10.3                   64 x 131072 bf16      14.3  24.9
 //   4 x 32768 fp32    10.9  12.2                   256 x 131072 bf16     27.8  26.7

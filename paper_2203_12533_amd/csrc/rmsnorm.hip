@@ -6,8 +6,10 @@
 // Bound by memory: a row is read once into registers (a wave to a row of up to 2048 columns, a block beyond), four consecutive columns to a
 // lane, so that every load and store of 4, 2 or 1 byte an element covers whole lines; 32 lanes hold a block of 128 columns, whose largest
 // magnitude takes five moves between lanes.  8192 x 2048 bf16 with x' and 8 bits, nothing of it cached: forward 43.4 us (5.0 TB/s), backward 51 (5.3); rows
-// read like everything else 51 and 53.  One row: 4.7 us, a launch.  What the separate passes would move besides: x' once more for the norm, h once more for the
-// quantisation.  Sums, r and h are fp32; q rounds h once, and so does h in bf16.
+// read like everything else 51 and 53.  One row: 5.0 to 5.6 us, a launch.  Rows of 8193 columns on that do not fill 16384 hold some of theirs in memory (forward
+// with an 8-bit output 16 to 21 registers, backward 78 to 83): 4096 x 12000 bf16 132 and 333 us (4.8 and 2.4 TB/s), 4096 x 16384 161 and 211 (5.4 and 5.1).
+// What the separate passes would move besides: x' once more for the norm, h once more for the quantisation.  Sums, r and h are fp32; q rounds h once, and so
+// does h in bf16.
 #include <type_traits>
 
 #include "common.hpp"
